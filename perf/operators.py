@@ -1,0 +1,495 @@
+"""The serving operators: what is measured, and their plain forms.
+
+A server answers from a paged cache of latents. One step of it is four calls, and each case is
+one of them:
+
+  plan     laga_page_plan     pages, slots and positions of a step's tokens, from request lengths
+  release  laga_page_release  the pages of requests that ended go back to the pool
+  append   laga_cache_append  the tokens' normalised latent and rotated shared key into their slots
+  attend   laga_paged_attn    attention of the tokens over their requests' cached positions
+
+``run`` makes the call where ``own`` is true; otherwise it computes the same in elementary
+torch operations, in 32 bits, rounded once at the end. ``exact`` is the definition in 64 bits (whole
+numbers: plain loops on the host).
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+# (d_nope, d_rope, d_v) by name
+WIDTHS = {"v3": (128, 64, 128), "half": (64, 32, 64), "small": (32, 16, 32)}
+
+_ATTEND = dict(op="attend", requests=64, fresh=1, longest=8192, heads=16, d_c=512, widths="v3", page=64, pad=0,
+               rotate=True, dtype="bf16")
+
+
+def listed():
+    return [
+        # one token for each of a batch of requests: what every decoding step begins with
+        dict(op="plan", name="plan_decode_r64", requests=64, longest=8192, chunk=1, page=64, pad=0),
+        # a large mixed step: most requests decode, every 16th has a chunk of its prompt taken in
+        dict(op="plan", name="plan_mixed_r1000", requests=1000, longest=16384, chunk=700, page=32, pad=1001),
+        # a few requests of a batch ended
+        dict(op="release", name="release_r64", requests=64, longest=8192, every=9, page=64),
+        # half of a large batch of long requests ended, pages of 16 tokens
+        dict(op="release", name="release_r2000", requests=2000, longest=4096, every=2, page=16),
+        # the cache rows of one decoding step, latent and key sliced from one projection's output
+        dict(op="append", name="append_t64", tokens=64, d_c=512, widths="v3", page=64, gamma=True, joint=True,
+             dtype="bf16"),
+        # the cache rows of a prompt
+        dict(op="append", name="append_t16384", tokens=16384, d_c=512, widths="v3", page=64, gamma=True, joint=True,
+             dtype="bf16"),
+        # one request of 1000 tokens on one rank's 16 heads: the smallest call, latency counts
+        dict(_ATTEND, name="attend_one_s1000", requests=1, longest=1000),
+        # an ordinary decoding batch of ragged requests at the rank's share of heads
+        dict(_ATTEND, name="attend_r64_h16_s8192"),
+        # the same batch on one device that holds every head; a few padded rows
+        dict(_ATTEND, name="attend_r61_h128_s8192", requests=61, heads=128, pad=3),
+        # two very long requests, every head: the cache's length has to be split
+        dict(_ATTEND, name="attend_r2_h128_s100000", requests=2, heads=128, longest=100000),
+        # half-width heads, three draft tokens a request, pages of 48 that end inside a tile
+        dict(_ATTEND, name="attend_half_r33x3_s3001", requests=33, fresh=3, heads=24, longest=3001, d_c=256,
+             widths="half", page=48),
+        # the fp32 mode at the small widths
+        dict(_ATTEND, name="attend_fp32_small_r8_s500", requests=8, heads=4, longest=500, d_c=64, widths="small",
+             page=16, dtype="fp32"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["plan", "release", "append", "attend", "attend", "attend", "attend", "attend"])
+    page = rng.choice([1, 7, 16, 32, 48, 64, 64, 128, 200])
+    if op == "plan":
+        requests = _log_int(rng, 1, 2000)
+        return dict(op=op, requests=requests, longest=_log_int(rng, 16, 16384), chunk=rng.choice([1, 1, 4, 300, 700]),
+                    page=max(page, 16), pad=rng.choice([0, 3, 100]))
+    if op == "release":
+        return dict(op=op, requests=_log_int(rng, 1, 2000), longest=_log_int(rng, 16, 8192),
+                    every=rng.choice([1, 2, 9]), page=max(page, 16))
+    if op == "append":
+        widths = rng.choice(["v3", "v3", "v3", "half", "small"])
+        return dict(op=op, tokens=_log_int(rng, 1, 16384), d_c=_latent(rng, widths), widths=widths, page=page,
+                    gamma=rng.random() < 0.75, joint=rng.random() < 0.5, dtype=rng.choice(["bf16", "bf16", "fp32"]))
+    widths = rng.choice(["v3", "v3", "v3", "v3", "half", "small"])
+    c = dict(_ATTEND, requests=_log_int(rng, 1, 256), fresh=rng.choice([1, 1, 1, 2, 4]), widths=widths, page=page,
+             heads=rng.choice([1, 3, 8, 16, 16, 16, 24, 32, 40, 64, 128, 128]), longest=_log_int(rng, 1, 100000),
+             d_c=_latent(rng, widths), pad=rng.choice([0, 0, 5]), rotate=rng.random() < 0.7,
+             dtype=rng.choice(["bf16", "bf16", "bf16", "bf16", "fp32"]))
+    c["longest"] = max(c["longest"], c["fresh"])
+    # no more than the largest listed call takes (the fp32 products run at a sixteenth of the bf16 rate)
+    most = max(work(k)["flops"] for k in listed() if k["op"] == "attend")
+    while work(c)["flops"] * (16 if c["dtype"] == "fp32" else 1) > most or _tokens(c) * 4 * (c["d_c"] + 64) > 2 << 30:
+        if c["requests"] > 1 and rng.random() < 0.5:
+            c["requests"] = c["requests"] * 2 // 3
+        else:
+            c["longest"] = max(c["fresh"], c["longest"] * 2 // 3)
+    return c
+
+
+def _latent(rng, widths):
+    return {"v3": rng.choice([512, 512, 512, 512, 256, 1024]), "half": rng.choice([128, 256, 416]),
+            "small": rng.choice([32, 64])}[widths]
+
+
+def _torch_dtype(case):
+    return torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+
+
+def _lengths(case):
+    """Cached tokens of each request after the step: the first as long as the longest, the others
+    spread over the range between a tenth of it and the whole."""
+    out = []
+    for r in range(case["requests"]):
+        part = 1.0 - 0.9 * ((r * 0.6180339887498949) % 1.0)
+        out.append(max(case.get("fresh", 1), int(part * case["longest"])))
+    return out
+
+
+def _tokens(case):
+    return sum(_lengths(case))
+
+
+def _fresh(case):
+    """Tokens that each request brings to a planned step: one, or a chunk of its prompt for every
+    16th; every 7th brings none."""
+    out = []
+    for r in range(case["requests"]):
+        out.append(case["chunk"] - r % 5 if r % 16 == 3 and case["chunk"] > 5 else 0 if r % 7 == 5 else 1)
+    return out
+
+
+def _pages(n, page):
+    return (n + page - 1) // page
+
+
+def work(case):
+    if case["op"] == "plan":
+        fresh, before = _fresh(case), _lengths(case)
+        need = sum(_pages(n + f, case["page"]) - _pages(n, case["page"]) for n, f in zip(before, fresh))
+        rows = sum(fresh) + case["pad"]
+        return {"bytes": 4 * (4 * len(fresh) + 2 * need + 3 * rows), "flops": 4 * len(fresh) + 4 * rows}
+    if case["op"] == "release":
+        n = [_pages(v, case["page"]) for v in _lengths(case)[::case["every"]]]
+        return {"bytes": 4 * (3 * case["requests"] + 2 * sum(n)), "flops": 4 * case["requests"]}
+    e = 2 if case["dtype"] == "bf16" else 4
+    dn, dr, dv = WIDTHS[case["widths"]]
+    dc = case["d_c"]
+    if case["op"] == "append":
+        t = case["tokens"]
+        return {"bytes": t * (2 * e * (dc + dr) + 8), "flops": t * (5 * dc + 6 * dr)}
+    h, lengths, f = case["heads"], _lengths(case), case["fresh"]
+    rows = len(lengths) * f
+    seen = sum(f * n - f * (f - 1) // 2 for n in lengths)
+    return {"bytes": e * ((dc + dr) * sum(lengths) + dc * h * (dn + dv) + rows * h * (dn + dr + dv)) + 4 * rows * h,
+            "flops": 2 * seen * h * (2 * dc + dr) + 2 * rows * h * dc * (dn + dv)}
+
+
+def _pool(lengths, after, page, spare, gen):
+    """A pool's pages dealt at random: the table that holds ``lengths`` tokens a request, wide
+    enough for ``after``, and the stack of free pages."""
+    have = [_pages(n, page) for n in lengths]
+    width = max(1, max(_pages(n, page) for n in after))
+    n_pages = sum(_pages(n, page) for n in after) + spare
+    order = torch.randperm(n_pages, generator=gen).to(torch.int32)
+    table = torch.full((len(lengths), width), -1, dtype=torch.int32)
+    at = 0
+    for r, n in enumerate(have):
+        table[r, :n] = order[at:at + n]
+        at += n
+    free = torch.full((n_pages,), -1, dtype=torch.int32)
+    free[:n_pages - at] = order[at:]
+    return table, free, n_pages - at, n_pages
+
+
+def _int(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def _host(case, seed):
+    """Host tensors of a plan's or a release's inputs."""
+    gen = torch.Generator().manual_seed(seed)
+    order = torch.randperm(case["requests"], generator=gen).tolist()
+    spread, fresh = _lengths(case), _fresh(case) if case["op"] == "plan" else None
+    lengths = [spread[r] for r in order]
+    if case["op"] == "plan":
+        arg = [fresh[r] for r in order]
+        after = [n + f for n, f in zip(lengths, arg)]
+    else:
+        arg = [int(r % case["every"] == 0) for r in order]
+        after = lengths
+    table, free, count, n_pages = _pool(lengths, after, case["page"], 17, gen)
+    return lengths, arg, table, free, count, n_pages
+
+
+def _attend_inputs(case, seed):
+    gen, host = torch.Generator(device="cuda").manual_seed(seed), torch.Generator().manual_seed(seed)
+    dn, dr, dv = WIDTHS[case["widths"]]
+    dc, h, f, dt = case["d_c"], case["heads"], case["fresh"], _torch_dtype(case)
+    spread = _lengths(case)
+    lengths = [spread[r] for r in torch.randperm(case["requests"], generator=host).tolist()]
+    table, _, _, n_pages = _pool(lengths, lengths, case["page"], 3, host)
+
+    def normal(*shape, scale=1.0):
+        return torch.randn(shape, generator=gen, device="cuda").mul_(scale)
+
+    cache = torch.empty((n_pages, case["page"], dc + dr), dtype=dt, device="cuda")
+    per = max(1, (1 << 27) // (case["page"] * (dc + dr)))  # pages made at a time
+    for i in range(0, n_pages, per):
+        x = normal(min(per, n_pages - i), case["page"], dc + dr)
+        x[..., :dc] *= torch.rsqrt(x[..., :dc].square().mean(-1, keepdim=True) + 1e-6)
+        cache[i:i + per] = x.to(dt)
+    request = [r for r in range(len(lengths)) for _ in range(f)] + [-1] * case["pad"]
+    position = [n - f + i for n in lengths for i in range(f)] + [-1] * case["pad"]
+    return {"cache": cache, "table": table.cuda(), "request": _int(request), "position": _int(position),
+            "q": normal(len(position), h, dn + dr).to(dt), "w": normal(dc, h * (dn + dv), scale=dc ** -0.5).to(dt)}
+
+
+def _append_inputs(case, seed):
+    gen, host = torch.Generator(device="cuda").manual_seed(seed), torch.Generator().manual_seed(seed)
+    dr, dc, t, dt = WIDTHS[case["widths"]][1], case["d_c"], case["tokens"], _torch_dtype(case)
+    n_pages = _pages(t, case["page"]) + 5
+    x = torch.randn((t, dc + dr), generator=gen, device="cuda")
+    # each token's latent at its own scale, as a projection leaves it
+    x[:, :dc] *= torch.empty((t, 1), device="cuda").uniform_(math.log(0.1), math.log(10.0), generator=gen).exp_()
+    x = x.to(dt)
+    slots = torch.randperm(n_pages * case["page"], generator=host)[:t]
+    slots[t // 2:t // 2 + t // 32] = -1  # rows of padding among them
+    return {"latent": x[:, :dc] if case["joint"] else x[:, :dc].contiguous(),
+            "kpe": x[:, dc:] if case["joint"] else x[:, dc:].contiguous(),
+            "gamma": torch.empty((dc,), device="cuda").uniform_(0.5, 1.5, generator=gen).to(dt)
+            if case["gamma"] else None,
+            "position": torch.randint(0, 131072, (t,), generator=host).to(torch.int32).cuda(),
+            "slot": slots.to(torch.int32).cuda(),
+            "cache": torch.randn((n_pages, case["page"], dc + dr), generator=gen, device="cuda").to(dt)}
+
+
+def _paged(case, rows, table, n_pages):
+    import paper_2607_17644_amd as laga
+    dn, dr, dv = WIDTHS[case.get("widths", "v3")]
+    return laga.Paged(rows=rows, requests=table.shape[0], table_width=table.shape[1], n_pages=n_pages,
+                      page_size=case["page"], n_heads=case.get("heads", 16), d_c=case.get("d_c", 512), d_nope=dn,
+                      d_rope=dr, d_v=dv, softmax_scale=1.0 / math.sqrt(dn + dr),
+                      dtype=laga.DTYPE_FP32 if case.get("dtype") == "fp32" else laga.DTYPE_BF16)
+
+
+def prepare(case, seed):
+    def new(shape, dtype):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+    i32 = torch.int32
+    if case["op"] in ("plan", "release"):
+        lengths, arg, table, free, count, n_pages = _host(case, seed)
+        r = len(lengths)
+        s = {"case": case, "lengths": _int(lengths), "arg": _int(arg), "table": table.cuda(), "free": free.cuda(),
+             "count": _int([count]), "lengths_out": new((r,), i32), "count_out": new((1,), i32), "status": new((1,), i32)}
+        if case["op"] == "plan":
+            rows = s["rows"] = sum(arg) + case["pad"]
+            s.update(begin=new((r + 1,), i32), request=new((rows,), i32), position=new((rows,), i32),
+                     slot=new((rows,), i32))
+        else:
+            rows = r
+        if own:
+            import paper_2607_17644_amd as laga
+            s["p"] = _paged(case, rows, table, n_pages)
+            s["ws"] = new((max(1, laga.laga_paged_workspace_bytes(s["p"], laga.OP_PAGE_PLAN)),), torch.uint8)
+        return s
+    if case["op"] == "append":
+        s = {"case": case, "x": _append_inputs(case, seed)}
+        if own:
+            s["p"] = _paged(case, case["tokens"], torch.empty((1, 1)), s["x"]["cache"].shape[0])
+        return s
+    s = {"case": case, "x": _attend_inputs(case, seed)}
+    x = s["x"]
+    rows, h = x["q"].shape[:2]
+    if own:
+        import paper_2607_17644_amd as laga
+        s["p"] = p = _paged(case, rows, x["table"], x["cache"].shape[0])
+        s["ws"] = new((max(1, laga.laga_paged_workspace_bytes(p, laga.OP_PAGED_ATTN)),), torch.uint8)
+        s["out"] = new((rows, h, p.d_v), x["q"].dtype)
+        s["lse"] = new((rows, h), torch.float32)
+    return s
+
+
+def run(s):
+    if own:
+        return _call(s)
+    return {"plan": _plain_plan, "release": _plain_release, "append": _plain_append,
+            "attend": _plain_attend}[s["case"]["op"]](s)
+
+
+def _call(s):
+    import paper_2607_17644_amd as laga
+    op, p = s["case"]["op"], s["p"]
+    if op == "plan":
+        laga.laga_page_plan(p, s["lengths"], s["arg"], s["table"], s["free"], s["count"], lengths_out=s["lengths_out"],
+                            free_count_out=s["count_out"], row_begin=s["begin"], row_request=s["request"],
+                            position=s["position"], slot=s["slot"], status=s["status"], workspace=s["ws"])
+        return {k: s[k] for k in ("table", "lengths_out", "count_out", "begin", "request", "position", "slot", "status")}
+    if op == "release":
+        laga.laga_page_release(p, s["lengths"], s["arg"], s["table"], s["free"], s["count"],
+                               lengths_out=s["lengths_out"], free_count_out=s["count_out"], status=s["status"])
+        return {k: s[k] for k in ("free", "lengths_out", "count_out", "status")}
+    x = s["x"]
+    if op == "append":
+        laga.laga_cache_append(p, x["latent"], x["kpe"], x["position"], x["slot"], x["cache"], gamma=x["gamma"])
+        return {"cache": x["cache"]}
+    laga.laga_paged_attn(p, x["q"], x["w"], x["cache"], x["table"], x["position"], row_request=x["request"],
+                         rope_base=10000.0 if s["case"]["rotate"] else None, out=s["out"], lse=s["lse"],
+                         workspace=s["ws"])
+    return {"out": s["out"], "lse": s["lse"]}
+
+
+def _plain_plan(s):
+    page, rows, dev = s["case"]["page"], s["rows"], s["table"].device
+    before, fresh = s["lengths"].long(), s["arg"].long()
+    after = before + fresh
+    old, new = (before + page - 1) // page, (after + page - 1) // page
+    need = new - old
+    first = torch.cumsum(need, 0) - need
+    begin = torch.cat((torch.zeros(1, dtype=torch.long, device=dev), torch.cumsum(fresh, 0)))
+    count = s["count"].long()
+    j = torch.arange(s["table"].shape[1], device=dev)
+    fits = (new <= s["table"].shape[1]).all() & (begin[-1] <= rows) & (need.sum() <= count[0])
+    fill = (j >= old[:, None]) & (j < new[:, None]) & fits
+    at = (count - 1 - (first[:, None] + j - old[:, None])).clamp(0, s["free"].numel() - 1)
+    table = torch.where(fill, s["free"][at], s["table"])
+    # a row's request: how many requests with rows of their own begin at or before it
+    t = torch.arange(rows, device=dev)
+    marks = torch.zeros(rows + 1, dtype=torch.long, device=dev)
+    marks.index_add_(0, begin[:-1].clamp(max=rows), torch.ones_like(fresh))
+    request = (torch.cumsum(marks, 0)[:-1] - 1).clamp(min=0)
+    live = (t < begin[-1]) & fits
+    position = before[request] + t - begin[:-1][request]
+    slot = table[request, (position // page).clamp(max=table.shape[1] - 1)].long() * page + position % page
+    none = torch.full_like(t, -1)
+    i32 = torch.int32
+    return {"table": table, "lengths_out": torch.where(fits, after, before).to(i32),
+            "count_out": torch.where(fits, count - need.sum(), count).to(i32), "begin": begin.to(i32),
+            "request": torch.where(live, request, none).to(i32), "position": torch.where(live, position, none).to(i32),
+            "slot": torch.where(live, slot, none).to(i32), "status": (~fits).to(i32).reshape(1)}
+
+
+def _plain_release(s):
+    page, i32 = s["case"]["page"], torch.int32
+    before, drop = s["lengths"].long(), s["arg"] != 0
+    have = torch.where(drop, (before + page - 1) // page, torch.zeros_like(before))
+    j = torch.arange(s["table"].shape[1], device=s["table"].device)
+    count = s["count"].long()
+    at = count + (torch.cumsum(have, 0) - have)[:, None] + j
+    gone = j < have[:, None]
+    free = s["free"].clone()
+    free[at[gone]] = s["table"][gone]
+    return {"free": free, "lengths_out": torch.where(drop, torch.zeros_like(before), before).to(i32),
+            "count_out": (count + have.sum()).to(i32), "status": torch.zeros_like(count).to(i32)}
+
+
+def _turn(x, position, base):
+    """Pairs (2i, 2i + 1) of the last axis turned by position * base^(-2i / d); the angle in 64 bits."""
+    d = x.shape[-1]
+    freq = base ** (-torch.arange(0, d, 2, dtype=torch.float64, device=x.device) / d)
+    angle = position.double()[:, None] * freq
+    c, s = torch.cos(angle).float(), torch.sin(angle).float()
+    if x.dim() == 3:
+        c, s = c[:, None], s[:, None]
+    a, b = x[..., 0::2], x[..., 1::2]
+    return torch.stack((a * c - b * s, a * s + b * c), -1).flatten(-2)
+
+
+def _plain_append(s):
+    x = s["x"]
+    lat = x["latent"].float()
+    y = lat / torch.sqrt(lat.square().mean(-1, keepdim=True) + 1e-6)
+    if x["gamma"] is not None:
+        y = y * x["gamma"].float()
+    row = torch.cat((y, _turn(x["kpe"].float(), x["position"], 10000.0)), -1).to(x["cache"].dtype)
+    keep = x["slot"] >= 0
+    flat = x["cache"].view(-1, row.shape[-1])
+    flat[x["slot"][keep].long()] = row[keep]
+    return {"cache": x["cache"]}
+
+
+def _plain_attend(s):
+    case, x = s["case"], s["x"]
+    dn, dr, dv = WIDTHS[case["widths"]]
+    dc, h, page = case["d_c"], case["heads"], case["page"]
+    rows = x["q"].shape[0]
+    q = x["q"].float()
+    band = _turn(q[..., dn:], x["position"].clamp(min=0), 10000.0) if case["rotate"] else q[..., dn:]
+    w = x["w"].float().view(dc, h, dn + dv)
+    wk, wv = w[..., :dn].permute(1, 2, 0).contiguous(), w[..., dn:].permute(1, 0, 2).contiguous()
+    qa = torch.bmm(q[..., :dn].transpose(0, 1).contiguous(), wk).transpose(0, 1)  # [rows, h, dc]
+    query = torch.cat((qa, band), -1)
+    out = torch.zeros((rows, h, dv), device=q.device)
+    lse = torch.full((rows, h), -math.inf, device=q.device)
+    seen = x["table"].shape[1] * page
+    step = max(1, (1 << 29) // (seen * (dc + dr + h)))  # rows at a time
+    for i in range(0, rows - case["pad"], step):
+        t = slice(i, min(i + step, rows - case["pad"]))
+        keys = x["cache"][x["table"][x["request"][t].long()].clamp(min=0).long()]
+        keys = keys.reshape(keys.shape[0], seen, dc + dr).float()
+        z = torch.bmm(query[t].contiguous(), keys.transpose(1, 2).contiguous()) * (1.0 / math.sqrt(dn + dr))
+        hide = torch.arange(seen, device=q.device) > x["position"][t, None]
+        z = z.masked_fill(hide[:, None], -math.inf)
+        top = z.amax(-1, keepdim=True)
+        e = torch.exp(z - top)
+        total = e.sum(-1, keepdim=True)
+        o = torch.bmm(e / total, keys[..., :dc].contiguous())  # [rows, h, dc]
+        out[t] = torch.bmm(o.transpose(0, 1).contiguous(), wv).transpose(0, 1)
+        lse[t] = (top + torch.log(total))[..., 0]
+    return {"out": out.to(x["q"].dtype), "lse": lse}
+
+
+def exact(case, seed):
+    if case["op"] in ("plan", "release"):
+        return (_exact_plan if case["op"] == "plan" else _exact_release)(case, seed)
+    if case["op"] == "append":
+        x = _append_inputs(case, seed)
+        cache = x["cache"].double()
+        lat, kpe = x["latent"].double(), x["kpe"].double()
+        y = lat * torch.rsqrt(lat.pow(2).sum(-1, keepdim=True) / lat.shape[-1] + 1e-6)
+        if x["gamma"] is not None:
+            y = y * x["gamma"].double()
+        z = torch.view_as_complex(kpe.reshape(kpe.shape[0], -1, 2).contiguous())
+        k = torch.view_as_real(z * _phase(x["position"], kpe.shape[-1])).flatten(1)
+        t = torch.nonzero(x["slot"] >= 0)[:, 0]
+        slot = x["slot"][t].long()
+        cache[slot // case["page"], slot % case["page"]] = torch.cat((y, k), 1)[t]
+        return {"cache": cache}
+    return _exact_attend(case, seed)
+
+
+def _phase(position, d):
+    angle = position.double()[:, None] / 10000.0 ** (torch.arange(d // 2, dtype=torch.float64, device="cuda") * 2 / d)
+    return torch.polar(torch.ones_like(angle), angle)
+
+
+def _exact_plan(case, seed):
+    lengths, fresh, table, free, count, _ = _host(case, seed)
+    table, free, page = table.numpy().copy(), free.numpy(), case["page"]
+    begin, request, position, slot, after = [0], [], [], [], []
+    for r, (n, f) in enumerate(zip(lengths, fresh)):
+        for i in range(n, n + f):
+            if i % page == 0:
+                count -= 1
+                table[r, i // page] = free[count]
+            request.append(r)
+            position.append(i)
+            slot.append(int(table[r, i // page]) * page + i % page)
+        begin.append(begin[-1] + f)
+        after.append(n + f)
+    empty = [-1] * case["pad"]
+    return {"table": torch.from_numpy(table).cuda(), "lengths_out": _int(after), "count_out": _int([count]),
+            "begin": _int(begin), "request": _int(request + empty), "position": _int(position + empty),
+            "slot": _int(slot + empty), "status": _int([0])}
+
+
+def _exact_release(case, seed):
+    lengths, drop, table, free, count, _ = _host(case, seed)
+    table, free = table.numpy(), free.numpy().copy()
+    for r, n in enumerate(lengths):
+        if drop[r]:
+            for j in range(-(-n // case["page"])):
+                free[count] = table[r, j]
+                count += 1
+    return {"free": torch.from_numpy(free).cuda(),
+            "lengths_out": _int([0 if d else n for n, d in zip(lengths, drop)]), "count_out": _int([count]),
+            "status": _int([0])}
+
+
+def _exact_attend(case, seed):
+    """Keys and values of every cached position rebuilt for every head, one request at a time."""
+    x = _attend_inputs(case, seed)
+    dn, dr, dv = WIDTHS[case["widths"]]
+    dc, h, page = case["d_c"], case["heads"], case["page"]
+    q = x["q"].double()
+    if case["rotate"]:
+        z = torch.view_as_complex(q[..., dn:].reshape(*q.shape[:2], -1, 2).contiguous())
+        q[..., dn:] = torch.view_as_real(z * _phase(x["position"], dr)[:, None]).flatten(2)
+    w = x["w"].double().view(dc, h, dn + dv)
+    out = torch.zeros((q.shape[0], h, dv), dtype=torch.float64, device="cuda")
+    lse = torch.full((q.shape[0], h), -math.inf, dtype=torch.float64, device="cuda")
+    position, request = x["position"].tolist(), np.array(x["request"].tolist())
+    for r in range(case["requests"]):
+        mine = np.nonzero(request == r)[0].tolist()
+        n = max(position[t] for t in mine) + 1
+        rows = x["cache"][x["table"][r, :_pages(n, page)].long()].reshape(-1, dc + dr)[:n].double()
+        group = max(1, (1 << 28) // (n * (dn + dv)))  # heads at a time
+        for a in range(0, h, group):
+            b = min(h, a + group)
+            kv = (rows[:, :dc] @ w[:, a:b].reshape(dc, -1)).view(n, b - a, dn + dv)
+            for t in mine:
+                m = position[t] + 1
+                z = (kv[:m, :, :dn] * q[t, a:b, :dn]).sum(-1) + rows[:m, dc:] @ q[t, a:b, dn:].t()
+                z = z / math.sqrt(dn + dr)
+                lse[t, a:b] = torch.logsumexp(z, 0)
+                out[t, a:b] = (torch.exp(z - lse[t, a:b])[..., None] * kv[:m, :, dn:]).sum(0)
+    return {"out": out, "lse": lse}
