@@ -296,7 +296,8 @@ def _call(s):
         return {k: s[k] for k in ("table", "lengths_out", "count_out", "begin", "request", "position", "slot", "status")}
     if op == "release":
         laga.laga_page_release(p, s["lengths"], s["arg"], s["table"], s["free"], s["count"],
-                               lengths_out=s["lengths_out"], free_count_out=s["count_out"], status=s["status"])
+                               lengths_out=s["lengths_out"], free_count_out=s["count_out"], status=s["status"],
+                               workspace=s["ws"])
         return {k: s[k] for k in ("free", "lengths_out", "count_out", "status")}
     x = s["x"]
     if op == "append":
