@@ -17,6 +17,8 @@
  *                         dc_kv and dk_pe, and the W_kv_b shard gradient dW
  *   laga_out_proj_fwd/_bwd : Alg. 1 step 7, the output projection W_o after the
  *                         out all-to-all, and its backward
+ *   laga_page_plan/_release, laga_cache_append, laga_paged_attn : serving the trained
+ *                         block, new tokens against a paged cache of [c_kv || k_pe]
  *
  * Layouts (all row-major, contiguous, device memory, 16-byte aligned):
  *   c_kv   [B, S, d_c]                     element dtype
@@ -298,6 +300,120 @@ LAGA_API laga_status_t laga_out_proj_bwd(const laga_out_proj_t* p, const void* o
 /* Workspace of laga_out_proj_bwd (partial sums of dw_o over token ranges); 0 if none is
  * needed or p is invalid. */
 LAGA_API size_t laga_out_proj_workspace_bytes(const laga_out_proj_t* p);
+
+/* ---- Serving: new tokens against a paged cache of latents ----------------------
+ * A model that this block trained answers one token per request and step. What a step
+ * reads of the past is a cached position's row [c_kv || k_pe] (the normalised latent and
+ * the shared rotated key, which every head reads), held in pages of a pool:
+ *   cache       [n_pages][page_size, d_c + d_rope]  element dtype, rows contiguous, pages
+ *                                    page_stride elements apart (page offsets are 64-bit)
+ *   block_table [requests, table_width]  int32: position j of request r is in page
+ *                                    block_table[r][j / page_size], row j % page_size
+ *   lengths     [requests]           int32: cached positions of each request
+ *   free_pages  [n_pages]            int32: a stack, its free_count[0] first entries free
+ *   row_request, position, slot [rows] int32: of each of the step's new tokens its
+ *                                    request, its position in it, and page * page_size +
+ *                                    row where it is cached; -1 in rows of padding
+ * all on the device; a decoding step is laga_page_plan, laga_cache_append,
+ * laga_paged_attn (and laga_out_proj_fwd), none of which reads a length on the host, so a
+ * captured step serves every later one. Conventions as above, and:
+ *   - an index that the device finds out of range is never followed: a slot outside the
+ *     pool stores nothing; a row whose request or position lies outside the table, or one
+ *     of whose visible pages lies outside the pool, gets NaN in every output element;
+ *   - cached rows past a row's position, and table entries past a request's pages, are
+ *     never read: they may hold anything;
+ *   - repeated calls are bit-identical; the attention's sums over a row's keys are grouped
+ *     by how the call's tiles are shared out, so a row's last bits may depend on the other
+ *     rows' lengths and on n_heads.
+ * Limits: head dims and d_c as for the attention calls; page_size >= 1; page_stride 0 (read
+ * as page_size * (d_c + d_rope)) or at least that and a multiple of 8; n_pages * page_size,
+ * requests * table_width, rows * n_heads, rows * table_width * page_size / 32 and
+ * 16 * d_c * n_heads * (d_nope + d_v) below 2^31; table_width * page_size at most 2^30;
+ * else LAGA_ERR_UNSUPPORTED. A size <= 0 is LAGA_ERR_SHAPE. */
+typedef struct {
+  int64_t rows;        /* T: new tokens of the step, rows of padding included */
+  int64_t requests;    /* R */
+  int64_t table_width; /* entries of a request in block_table */
+  int64_t n_pages, page_size;
+  int64_t page_stride; /* elements between pages; 0: page_size * (d_c + d_rope) */
+  int64_t n_heads, d_c, d_nope, d_rope, d_v; /* as in laga_problem_t */
+  float softmax_scale;
+  int32_t dtype;       /* laga_dtype_t */
+  int32_t reserved;    /* must be 0 */
+} laga_paged_t;
+
+/* Bits of the status[0] that laga_page_plan and laga_page_release write (0: done). */
+enum {
+  LAGA_PLAN_ROWS = 1,    /* more new tokens than rows */
+  LAGA_PLAN_TABLE = 2,   /* a request would not fit in table_width pages */
+  LAGA_PLAN_PAGES = 4,   /* fewer free pages than needed; release: more than the stack holds */
+  LAGA_PLAN_INVALID = 8  /* a negative length or count, or free_count outside [0, n_pages] */
+};
+
+typedef enum { LAGA_OP_PAGE_PLAN = 3, LAGA_OP_PAGED_ATTN = 4 } laga_paged_op_t;
+
+/* Pages, slots and positions of a step that adds fresh[r] >= 0 tokens to request r:
+ *   request r's ceil((lengths[r] + fresh[r]) / page_size) - ceil(lengths[r] / page_size) new
+ *   pages are popped from the stack's end, requests in order, into block_table (its other
+ *   entries stay); lengths_out = lengths + fresh; free_count_out[0] = free_count[0] - pages;
+ *   row_begin [requests + 1]: the requests' first rows (exclusive sums of fresh); rows
+ *   row_begin[r] .. are request r's new tokens in order, rows from row_begin[requests] on are
+ *   padding (-1).
+ * lengths_out may be lengths and free_count_out free_count (in place). All or nothing: if
+ * the step does not fit, status[0] says why (LAGA_PLAN_*), lengths_out and free_count_out are
+ * the inputs, block_table stays, row_begin is 0 and every row padding (so the calls after it
+ * store nothing and return empty rows). Workspace: laga_paged_workspace_bytes(p,
+ * LAGA_OP_PAGE_PLAN). */
+LAGA_API laga_status_t laga_page_plan(const laga_paged_t* p, const int32_t* lengths,
+                                      const int32_t* fresh, int32_t* block_table,
+                                      const int32_t* free_pages, const int32_t* free_count,
+                                      int32_t* lengths_out, int32_t* free_count_out,
+                                      int32_t* row_begin, int32_t* row_request, int32_t* position,
+                                      int32_t* slot, int32_t* status, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/* The pages of every request with drop[r] != 0 go back on the stack, requests and their
+ * pages in order; its lengths_out is 0 (its table entries stay and mean nothing). In place
+ * as above; all or nothing as above. Same workspace. */
+LAGA_API laga_status_t laga_page_release(const laga_paged_t* p, const int32_t* lengths,
+                                         const int32_t* drop, const int32_t* block_table,
+                                         int32_t* free_pages, const int32_t* free_count,
+                                         int32_t* lengths_out, int32_t* free_count_out,
+                                         int32_t* status, void* workspace, size_t workspace_bytes,
+                                         void* stream);
+
+/* The cache rows of a step's tokens: with the producers' arithmetic (laga_prologue_fwd),
+ *   cache row slot[t] = [ gamma * x * rsqrt(mean(x^2) + eps) || R(position_offset + position[t]) k ]
+ * of x = latent_raw[t], k = kpe_raw[t] (element dtype; rows latent_stride and kpe_stride
+ * elements apart, multiples of 8 and at least d_c and d_rope: both may be columns of one
+ * projection's output). Rows whose slot lies outside the pool store nothing. Slots of one
+ * call must differ (of two tokens with one slot, either's elements may be stored).
+ * gamma may be NULL. */
+LAGA_API laga_status_t laga_cache_append(const laga_paged_t* p, const laga_prologue_t* cfg,
+                                         const void* latent_raw, int64_t latent_stride,
+                                         const void* gamma, const void* kpe_raw, int64_t kpe_stride,
+                                         const int32_t* position, const int32_t* slot, void* cache,
+                                         void* stream);
+
+/* Attention of rows over their requests' cached positions 0 .. position[t] (the row's own
+ * among them, appended before): laga_attn_fwd's result at that row, from the cache alone,
+ *   out [rows, n_heads, d_v] element dtype, lse [rows, n_heads] fp32 (may be NULL)
+ * for q [rows, n_heads, d_nope + d_rope]. With cfg, q's rope band is turned by the row's
+ * position_offset + position[t] first (q is not written; cfg's eps is not used); NULL: it
+ * has been. row_request NULL: row t is request t. A row at a negative position sees nothing:
+ * out 0, lse -infinity. Any number of rows may belong to one request.
+ * The product with W_kv_b's K columns is taken on the query's side and the one with its V
+ * columns after the softmax: element-dtype rounding of q W_k^T, of the probabilities (as in
+ * laga_attn_fwd) and of the normalised sum before W_v; statistics, products and joins of a
+ * row's parts in fp32. Workspace: laga_paged_workspace_bytes(p, LAGA_OP_PAGED_ATTN). */
+LAGA_API laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg,
+                                       const void* q, const void* w_kv_b, const void* cache,
+                                       const int32_t* block_table, const int32_t* row_request,
+                                       const int32_t* position, void* out, float* lse,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of op (laga_paged_op_t); 0 if p is invalid. */
+LAGA_API size_t laga_paged_workspace_bytes(const laga_paged_t* p, int op);
 
 /* Workspace bytes that op (laga_op_t) needs for problem p; 0 if none or if p
  * is invalid (check with the entry point itself for the error code). For the

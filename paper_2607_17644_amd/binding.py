@@ -20,6 +20,8 @@ DTYPE_BF16, DTYPE_FP32 = 0, 1
 DQ_FROM_STORE, DQ_RECOMPUTE = 0, 1
 KV_MATERIALIZED, KV_FUSED = 0, 1
 OP_FWD, OP_BWD, OP_PROLOGUE_BWD = 0, 1, 2
+OP_PAGE_PLAN, OP_PAGED_ATTN = 3, 4  # laga_paged_workspace_bytes
+PLAN_ROWS, PLAN_TABLE, PLAN_PAGES, PLAN_INVALID = 1, 2, 4, 8  # bits of a plan's status
 BWD_PREPARE, BWD_DKDV, BWD_DQ, BWD_FINISH = 0, 1, 2, 3
 
 _STATUS = {0: "LAGA_OK", 1: "LAGA_ERR_NULL", 2: "LAGA_ERR_SHAPE", 3: "LAGA_ERR_UNSUPPORTED",
@@ -71,6 +73,49 @@ class OutProj:
 
 class _CPrologue(ctypes.Structure):
     _fields_ = [("eps", ctypes.c_float), ("rope_base", ctypes.c_float), ("position_offset", ctypes.c_int64)]
+
+
+class _CPaged(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "requests", "table_width", "n_pages", "page_size",
+                                              "page_stride", "n_heads", "d_c", "d_nope", "d_rope", "d_v")] + [
+        ("softmax_scale", ctypes.c_float), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+@dataclasses.dataclass
+class Paged:
+    """Mirror of laga_paged_t: one serving step over a paged cache of latents."""
+    rows: int         # new tokens of the step, rows of padding included
+    requests: int
+    table_width: int  # block-table entries of a request
+    n_pages: int
+    page_size: int
+    n_heads: int
+    d_c: int
+    d_nope: int
+    d_rope: int
+    d_v: int
+    softmax_scale: float
+    dtype: int = DTYPE_BF16
+    page_stride: int = 0  # elements between pages; 0: pages are contiguous
+    reserved: int = 0
+
+    def c(self) -> _CPaged:
+        return _CPaged(self.rows, self.requests, self.table_width, self.n_pages, self.page_size, self.page_stride,
+                       self.n_heads, self.d_c, self.d_nope, self.d_rope, self.d_v, self.softmax_scale, self.dtype,
+                       self.reserved)
+
+    @property
+    def torch_dtype(self):
+        return torch.bfloat16 if self.dtype == DTYPE_BF16 else torch.float32
+
+    def shapes(self) -> dict:
+        T, R, H = self.rows, self.requests, self.n_heads
+        return {"cache": (self.n_pages, self.page_size, self.d_c + self.d_rope), "block_table": (R, self.table_width),
+                "free_pages": (self.n_pages,), "free_count": (1,), "free_count_out": (1,), "status": (1,),
+                "lengths": (R,), "lengths_out": (R,), "fresh": (R,), "drop": (R,), "row_begin": (R + 1,),
+                "row_request": (T,), "position": (T,), "slot": (T,), "latent_raw": (T, self.d_c),
+                "kpe_raw": (T, self.d_rope), "q": (T, H, self.d_nope + self.d_rope),
+                "w_kv_b": (self.d_c, H * (self.d_nope + self.d_v)), "out": (T, H, self.d_v), "lse": (T, H)}
 
 
 @dataclasses.dataclass
@@ -141,6 +186,17 @@ def _load():
     L.laga_prologue_fwd.argtypes = [P, Q, vp, vp, vp, vp, vp, vp, vp, vp]
     L.laga_prologue_bwd.restype = ctypes.c_int
     L.laga_prologue_bwd.argtypes = [P, Q, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    G = ctypes.POINTER(_CPaged)
+    L.laga_paged_workspace_bytes.restype = ctypes.c_size_t
+    L.laga_paged_workspace_bytes.argtypes = [G, ctypes.c_int]
+    L.laga_page_plan.restype = ctypes.c_int
+    L.laga_page_plan.argtypes = [G] + [vp] * 13 + [ctypes.c_size_t, vp]
+    L.laga_page_release.restype = ctypes.c_int
+    L.laga_page_release.argtypes = [G] + [vp] * 9 + [ctypes.c_size_t, vp]
+    L.laga_cache_append.restype = ctypes.c_int
+    L.laga_cache_append.argtypes = [G, Q, vp, ctypes.c_int64, vp, vp, ctypes.c_int64, vp, vp, vp, vp]
+    L.laga_paged_attn.restype = ctypes.c_int
+    L.laga_paged_attn.argtypes = [G, Q] + [vp] * 9 + [ctypes.c_size_t, vp]
     return L
 
 
@@ -373,3 +429,142 @@ def laga_prologue_bwd(p: Problem, latent_raw, rstd, dc_kv, dk_pe, dq=None, gamma
         _ptr(d_gamma, "d_gamma", (p.d_c,), torch.float32, required=gamma is not None),
         _ptr(workspace, "workspace", required=False), nbytes, _stream(stream)), "laga_prologue_bwd")
     return d_latent_raw, d_kpe_raw, d_gamma
+
+
+def laga_paged_workspace_bytes(p: Paged, op: int) -> int:
+    return int(_lib.laga_paged_workspace_bytes(ctypes.byref(p.c()), op))
+
+
+class _Device:
+    """The device of a serving call: every tensor has to be on it, and the call is made with it
+    current, on its current stream unless the caller names one."""
+
+    def __init__(self, first, name):
+        if not isinstance(first, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if not first.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        self.device = first.device
+
+    def ptr(self, t, name, shape, dtype, required=True):
+        ptr = _ptr(t, name, shape, dtype, required)
+        if t is not None and t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, expected {self.device}")
+        return ptr
+
+    def _strided(self, t, name, shape, dtype):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, expected {self.device}")
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+        if t.dtype != dtype:
+            raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+
+    def rows(self, t, name, shape, dtype):
+        """Pointer and row stride of a matrix whose rows are contiguous (columns of a wider one)."""
+        self._strided(t, name, shape, dtype)
+        if t.stride(1) != 1:
+            raise ValueError(f"{name} must have contiguous rows")
+        return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+
+    def cache(self, p, t):
+        """Pointer of the pool: rows contiguous in a page, pages p.page_stride elements apart."""
+        shape = p.shapes()["cache"]
+        self._strided(t, "cache", shape, p.torch_dtype)
+        want = (p.page_stride or shape[1] * shape[2], shape[2], 1)
+        if any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), want)):
+            raise ValueError(f"cache has strides {t.stride()}, expected {want}")
+        return t.data_ptr()
+
+    def stream(self, stream):
+        return _stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+
+    def int32(self, p, name, t):
+        return torch.empty(p.shapes()[name], dtype=torch.int32, device=self.device) if t is None else t
+
+
+def _plan_workspace(p, workspace, device):
+    if workspace is None:
+        workspace = torch.empty(max(1, laga_paged_workspace_bytes(p, OP_PAGE_PLAN)), dtype=torch.uint8, device=device)
+    return workspace
+
+
+def laga_page_plan(p: Paged, lengths, fresh, block_table, free_pages, free_count, lengths_out=None, free_count_out=None,
+                   row_begin=None, row_request=None, position=None, slot=None, status=None, workspace=None, stream=None):
+    """Pages, slots and positions of a step that adds fresh[r] tokens to request r; block_table is
+    updated in place. Returns (lengths_out, free_count_out, row_begin, row_request, position, slot,
+    status); lengths_out may be lengths, and free_count_out free_count. Nothing is read on the
+    host: status[0] (PLAN_*) says on the device whether the step fits."""
+    D, sh, i32 = _Device(lengths, "lengths"), p.shapes(), torch.int32
+    given = {"lengths_out": lengths_out, "free_count_out": free_count_out, "row_begin": row_begin,
+             "row_request": row_request, "position": position, "slot": slot, "status": status}
+    outs = {k: D.int32(p, k, t) for k, t in given.items()}
+    workspace = _plan_workspace(p, workspace, D.device)
+    with torch.cuda.device(D.device):
+        _check(_lib.laga_page_plan(
+            ctypes.byref(p.c()), D.ptr(lengths, "lengths", sh["lengths"], i32), D.ptr(fresh, "fresh", sh["fresh"], i32),
+            D.ptr(block_table, "block_table", sh["block_table"], i32),
+            D.ptr(free_pages, "free_pages", sh["free_pages"], i32), D.ptr(free_count, "free_count", (1,), i32),
+            *[D.ptr(t, k, sh[k], i32) for k, t in outs.items()], D.ptr(workspace, "workspace", None, None),
+            workspace.numel() * workspace.element_size(), D.stream(stream)), "laga_page_plan")
+    return tuple(outs.values())
+
+
+def laga_page_release(p: Paged, lengths, drop, block_table, free_pages, free_count, lengths_out=None,
+                      free_count_out=None, status=None, workspace=None, stream=None):
+    """The pages of the requests with drop[r] != 0 go back on the stack (free_pages is updated in
+    place); returns (lengths_out, free_count_out, status)."""
+    D, sh, i32 = _Device(lengths, "lengths"), p.shapes(), torch.int32
+    given = {"lengths_out": lengths_out, "free_count_out": free_count_out, "status": status}
+    outs = {k: D.int32(p, k, t) for k, t in given.items()}
+    workspace = _plan_workspace(p, workspace, D.device)
+    with torch.cuda.device(D.device):
+        _check(_lib.laga_page_release(
+            ctypes.byref(p.c()), D.ptr(lengths, "lengths", sh["lengths"], i32), D.ptr(drop, "drop", sh["drop"], i32),
+            D.ptr(block_table, "block_table", sh["block_table"], i32),
+            D.ptr(free_pages, "free_pages", sh["free_pages"], i32), D.ptr(free_count, "free_count", (1,), i32),
+            *[D.ptr(t, k, sh[k], i32) for k, t in outs.items()], D.ptr(workspace, "workspace", None, None),
+            workspace.numel() * workspace.element_size(), D.stream(stream)), "laga_page_release")
+    return tuple(outs.values())
+
+
+def laga_cache_append(p: Paged, latent_raw, kpe_raw, position, slot, cache, gamma=None, eps=1e-6, rope_base=10000.0,
+                      position_offset=0, stream=None):
+    """The cache rows of new tokens, normalised latent and rotated shared key, into their slots;
+    returns cache. latent_raw and kpe_raw may be columns of one wider matrix."""
+    D, sh, dt, i32 = _Device(cache, "cache"), p.shapes(), p.torch_dtype, torch.int32
+    lat, lat_stride = D.rows(latent_raw, "latent_raw", sh["latent_raw"], dt)
+    kpe, kpe_stride = D.rows(kpe_raw, "kpe_raw", sh["kpe_raw"], dt)
+    cfg = _CPrologue(eps, rope_base, position_offset)
+    with torch.cuda.device(D.device):
+        _check(_lib.laga_cache_append(
+            ctypes.byref(p.c()), ctypes.byref(cfg), lat, lat_stride, D.ptr(gamma, "gamma", (p.d_c,), dt, required=False),
+            kpe, kpe_stride, D.ptr(position, "position", sh["position"], i32), D.ptr(slot, "slot", sh["slot"], i32),
+            D.cache(p, cache), D.stream(stream)), "laga_cache_append")
+    return cache
+
+
+def laga_paged_attn(p: Paged, q, w_kv_b, cache, block_table, position, row_request=None, rope_base=None,
+                    position_offset=0, out=None, lse=None, workspace=None, stream=None):
+    """Attention of rows over the cached positions 0 .. position[t] of their requests; returns (out,
+    lse). With rope_base q's rope band is turned by the row's position first (without, it has been)."""
+    D, sh, dt, i32 = _Device(q, "q"), p.shapes(), p.torch_dtype, torch.int32
+    if out is None:
+        out = _new(p, "out", dt, D.device)
+    if lse is None:
+        lse = _new(p, "lse", torch.float32, D.device)
+    if workspace is None:
+        workspace = torch.empty(max(1, laga_paged_workspace_bytes(p, OP_PAGED_ATTN)), dtype=torch.uint8, device=D.device)
+    cfg = None if rope_base is None else _CPrologue(0.0, rope_base, position_offset)
+    with torch.cuda.device(D.device):
+        _check(_lib.laga_paged_attn(
+            ctypes.byref(p.c()), None if cfg is None else ctypes.byref(cfg), D.ptr(q, "q", sh["q"], dt),
+            D.ptr(w_kv_b, "w_kv_b", sh["w_kv_b"], dt), D.cache(p, cache),
+            D.ptr(block_table, "block_table", sh["block_table"], i32),
+            D.ptr(row_request, "row_request", sh["row_request"], i32, required=False),
+            D.ptr(position, "position", sh["position"], i32), D.ptr(out, "out", sh["out"], dt),
+            D.ptr(lse, "lse", sh["lse"], torch.float32), D.ptr(workspace, "workspace", None, None),
+            workspace.numel() * workspace.element_size(), D.stream(stream)), "laga_paged_attn")
+    return out, lse

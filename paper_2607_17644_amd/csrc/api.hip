@@ -1,4 +1,4 @@
-// C ABI of the per-rank LAGA attention block: validation, workspace layout and
+// C ABI of the per-rank LAGA attention block and its serving calls: validation, workspace layout and
 // dispatch to the gfx950 kernels. Declarations and conventions: include/laga.h.
 #include <math.h>
 #include <stdint.h>
@@ -9,6 +9,7 @@
 #include "gemm_plan.hpp"
 #include "kernels.hpp"
 #include "bwd_common.hpp"
+#include "paged.hpp"
 
 using namespace laga;
 
@@ -108,16 +109,22 @@ size_t prologue_ws_bytes(const Dims& d) {
   return round_up(sizeof(float) * (size_t)prologue_bwd_rows(tok) * d.d_c);
 }
 
+// positions: of the tokens past the offset
+laga_status_t validate_rope(const laga_prologue_t* cfg, int64_t positions, int d_rope) {
+  if (!cfg) return LAGA_ERR_NULL;
+  if (!isfinite(cfg->eps) || cfg->eps < 0.f || !isfinite(cfg->rope_base) || !(cfg->rope_base > 1.f) ||
+      cfg->position_offset < 0 || cfg->position_offset > ((int64_t)1 << 53) - 1 - positions)
+    return LAGA_ERR_SHAPE;
+  // the rotation kernels give each lane one 8-element chunk of a band: d_rope / 8 must divide 64
+  if (d_rope % 8 != 0 || 64 % (d_rope / 8) != 0) return LAGA_ERR_UNSUPPORTED;
+  return LAGA_OK;
+}
+
 laga_status_t validate_prologue(const laga_problem_t* p, const laga_prologue_t* cfg, Dims* d) {
   if (!cfg) return LAGA_ERR_NULL;
   laga_status_t s = validate(p, d);
   if (s != LAGA_OK) return s;
-  if (!isfinite(cfg->eps) || cfg->eps < 0.f || !isfinite(cfg->rope_base) || !(cfg->rope_base > 1.f) ||
-      cfg->position_offset < 0 || cfg->position_offset > ((int64_t)1 << 53) - 1 - d->S)
-    return LAGA_ERR_SHAPE;
-  // the rotation kernels give each lane one 8-element chunk of a band: d_rope / 8 must divide 64
-  if (d->dr % 8 != 0 || 64 % (d->dr / 8) != 0) return LAGA_ERR_UNSUPPORTED;
-  return LAGA_OK;
+  return validate_rope(cfg, d->S, d->dr);
 }
 
 PrologueArgs prologue_args(const laga_problem_t* p, const laga_prologue_t* cfg, const Dims& d) {
@@ -155,6 +162,86 @@ int out_proj_splits(const laga_out_proj_t* p, const OutDims& d) {
 size_t out_proj_ws_bytes(const laga_out_proj_t* p, const OutDims& d) {
   const int n = out_proj_splits(p, d);
   return n > 1 ? round_up(sizeof(float) * (size_t)n * d.F * d.D) : 0;
+}
+
+// Serving from a paged cache.
+struct PagedDims {
+  int T, R, width, n_pages, page, H, d_c, dn, dr, dv;
+  int64_t page_stride;
+};
+laga_status_t validate_paged(const laga_paged_t* p, PagedDims* d) {
+  if (!p) return LAGA_ERR_NULL;
+  for (int64_t x : {p->rows, p->requests, p->table_width, p->n_pages, p->page_size})
+    if (x <= 0) return LAGA_ERR_SHAPE;
+  if (p->reserved != 0) return LAGA_ERR_UNSUPPORTED;
+  // the model's sizes as for the attention calls
+  laga_problem_t m{};
+  m.batch = 1; m.seq_len = 1; m.n_heads = p->n_heads; m.d_c = p->d_c; m.d_nope = p->d_nope; m.d_rope = p->d_rope;
+  m.d_v = p->d_v; m.softmax_scale = p->softmax_scale; m.causal = 1; m.dtype = p->dtype;
+  Dims md;
+  const laga_status_t s = validate(&m, &md);
+  if (s != LAGA_OK) return s;
+  // each factor below 2^31 before any product is formed, so no product overflows int64
+  for (int64_t x : {p->rows, p->requests, p->table_width, p->n_pages, p->page_size})
+    if (x >= kMaxElems) return LAGA_ERR_UNSUPPORTED;
+  const int64_t cap = p->table_width * p->page_size, row = p->d_c + p->d_rope;
+  if (cap > kMaxElems / 2 || p->n_pages * p->page_size >= kMaxElems || p->requests * p->table_width >= kMaxElems ||
+      p->rows * p->n_heads >= kMaxElems || p->rows * ((cap + kTileKeys - 1) / kTileKeys) >= kMaxElems)
+    return LAGA_ERR_UNSUPPORTED;
+  if (p->page_stride != 0 && (p->page_stride < p->page_size * row || p->page_stride % 8 != 0 ||
+                              p->page_stride >= (int64_t)1 << 40))
+    return p->page_stride < p->page_size * row ? LAGA_ERR_SHAPE : LAGA_ERR_UNSUPPORTED;
+  d->T = (int)p->rows; d->R = (int)p->requests; d->width = (int)p->table_width; d->n_pages = (int)p->n_pages;
+  d->page = (int)p->page_size; d->H = md.H; d->d_c = md.d_c; d->dn = md.dn; d->dr = md.dr; d->dv = md.dv;
+  d->page_stride = p->page_stride ? p->page_stride : p->page_size * row;
+  return LAGA_OK;
+}
+size_t elem_size(const laga_paged_t* p) { return p->dtype == LAGA_DTYPE_BF16 ? 2 : 4; }
+
+// [schedule | absorbed queries | whole rows | partials: outputs, statistics]
+struct PagedWs {
+  size_t sched, qa, obar, part_o, part_ml, total;
+};
+PagedWs paged_layout(const laga_paged_t* p, const PagedDims& d, const PagedPlan& plan) {
+  PagedWs w{};
+  const size_t rows = (size_t)d.T * d.H, places = (size_t)2 * plan.workers * d.H;
+  size_t off = 0;
+  w.sched = off; off += round_up(sizeof(int32_t) * ((size_t)kSchedHeader + d.T + 1 + plan.workers));
+  w.qa = off; off += round_up(elem_size(p) * rows * (d.d_c + d.dr));
+  w.obar = off; off += round_up(elem_size(p) * rows * d.d_c);
+  w.part_o = off; off += round_up(sizeof(float) * places * d.d_c);
+  w.part_ml = off; off += round_up(sizeof(float) * places * 2);
+  w.total = off;
+  return w;
+}
+
+size_t plan_ws_bytes(const PagedDims& d) { return round_up(sizeof(int32_t) * plan_ws_ints(d.R)); }
+
+laga_status_t page_plan(const laga_paged_t* p, bool release, const int32_t* lengths, const int32_t* arg, int32_t* table,
+                        int32_t* free_pages, const int32_t* free_count, int32_t* lengths_out, int32_t* free_count_out,
+                        int32_t* row_begin, int32_t* row_request, int32_t* position, int32_t* slot, int32_t* status,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  PagedDims d;
+  const laga_status_t s = validate_paged(p, &d);
+  if (s != LAGA_OK) return s;
+  const void* need[] = {lengths, arg, table, free_pages, free_count, lengths_out, free_count_out, status};
+  const void* rows[] = {row_begin, row_request, position, slot};
+  for (const void* x : need)
+    if (!x) return LAGA_ERR_NULL;
+  for (const void* x : rows)
+    if (!release && !x) return LAGA_ERR_NULL;
+  for (const void* x : need)
+    if (misaligned(x)) return LAGA_ERR_ALIGN;
+  for (const void* x : rows)
+    if (misaligned(x)) return LAGA_ERR_ALIGN;
+  if (!workspace || workspace_bytes < plan_ws_bytes(d)) return LAGA_ERR_WORKSPACE;
+  if (misaligned(workspace)) return LAGA_ERR_ALIGN;
+  PlanArgs a{};
+  a.lengths = lengths; a.arg = arg; a.table = table; a.free_pages = free_pages; a.free_count = free_count;
+  a.lengths_out = lengths_out; a.free_count_out = free_count_out; a.row_begin = row_begin;
+  a.row_request = row_request; a.position = position; a.slot = slot; a.status = status; a.ws = (int32_t*)workspace;
+  a.rows = d.T; a.R = d.R; a.width = d.width; a.n_pages = d.n_pages; a.page = d.page; a.release = release;
+  return from_hip(launch_plan(a, (hipStream_t)stream));
 }
 
 template <typename T>
@@ -224,6 +311,94 @@ size_t laga_workspace_bytes(const laga_problem_t* p, int op) {
   if (op == LAGA_OP_BWD) return bwd_layout(p, d).total;
   if (op == LAGA_OP_PROLOGUE_BWD) return prologue_ws_bytes(d);
   return 0;
+}
+
+size_t laga_paged_workspace_bytes(const laga_paged_t* p, int op) {
+  PagedDims d;
+  if (validate_paged(p, &d) != LAGA_OK) return 0;
+  if (op == LAGA_OP_PAGE_PLAN) return plan_ws_bytes(d);
+  if (op == LAGA_OP_PAGED_ATTN)
+    return paged_layout(p, d, paged_plan(d.H, d.d_c, (int)elem_size(p))).total;
+  return 0;
+}
+
+laga_status_t laga_page_plan(const laga_paged_t* p, const int32_t* lengths, const int32_t* fresh, int32_t* block_table,
+                             const int32_t* free_pages, const int32_t* free_count, int32_t* lengths_out,
+                             int32_t* free_count_out, int32_t* row_begin, int32_t* row_request, int32_t* position,
+                             int32_t* slot, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+  return page_plan(p, false, lengths, fresh, block_table, const_cast<int32_t*>(free_pages), free_count, lengths_out,
+                   free_count_out, row_begin, row_request, position, slot, status, workspace, workspace_bytes, stream);
+}
+
+laga_status_t laga_page_release(const laga_paged_t* p, const int32_t* lengths, const int32_t* drop,
+                                const int32_t* block_table, int32_t* free_pages, const int32_t* free_count,
+                                int32_t* lengths_out, int32_t* free_count_out, int32_t* status, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  return page_plan(p, true, lengths, drop, const_cast<int32_t*>(block_table), free_pages, free_count, lengths_out,
+                   free_count_out, nullptr, nullptr, nullptr, nullptr, status, workspace, workspace_bytes, stream);
+}
+
+laga_status_t laga_cache_append(const laga_paged_t* p, const laga_prologue_t* cfg, const void* latent_raw,
+                                int64_t latent_stride, const void* gamma, const void* kpe_raw, int64_t kpe_stride,
+                                const int32_t* position, const int32_t* slot, void* cache, void* stream) {
+  PagedDims d;
+  laga_status_t s = validate_paged(p, &d);
+  if (s != LAGA_OK) return s;
+  s = validate_rope(cfg, d.width * (int64_t)d.page, d.dr);
+  if (s != LAGA_OK) return s;
+  if (!latent_raw || !kpe_raw || !position || !slot || !cache) return LAGA_ERR_NULL;
+  if (latent_stride < d.d_c || kpe_stride < d.dr) return LAGA_ERR_SHAPE;
+  if (latent_stride % 8 != 0 || kpe_stride % 8 != 0 || latent_stride >= kMaxElems || kpe_stride >= kMaxElems)
+    return LAGA_ERR_UNSUPPORTED;
+  if (misaligned(latent_raw) || misaligned(kpe_raw) || misaligned(gamma) || misaligned(position) || misaligned(slot) ||
+      misaligned(cache))
+    return LAGA_ERR_ALIGN;
+  AppendArgs a{};
+  a.latent = latent_raw; a.kpe = kpe_raw; a.gamma = gamma; a.latent_stride = latent_stride; a.kpe_stride = kpe_stride;
+  a.position = position; a.slot = slot; a.cache = cache; a.page_stride = d.page_stride;
+  a.position_offset = cfg->position_offset; a.T = d.T; a.d_c = d.d_c; a.d_rope = d.dr;
+  a.n_slots = d.n_pages * d.page; a.page = d.page; a.eps = cfg->eps; a.log2_base = log2((double)cfg->rope_base);
+  hipStream_t st = (hipStream_t)stream;
+  return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_append<bf16>(a, st) : launch_append<float>(a, st));
+}
+
+laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg, const void* q, const void* w_kv_b,
+                              const void* cache, const int32_t* block_table, const int32_t* row_request,
+                              const int32_t* position, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  PagedDims d;
+  laga_status_t s = validate_paged(p, &d);
+  if (s != LAGA_OK) return s;
+  if (cfg) {
+    s = validate_rope(cfg, d.width * (int64_t)d.page, d.dr);
+    if (s != LAGA_OK) return s;
+  }
+  if (!q || !w_kv_b || !cache || !block_table || !position || !out) return LAGA_ERR_NULL;
+  const void* ptrs[] = {q, w_kv_b, cache, block_table, row_request, position, out, lse};
+  for (const void* x : ptrs)
+    if (misaligned(x)) return LAGA_ERR_ALIGN;
+  // a row's request must be known: without row_request there is one row per request at most
+  if (!row_request && d.T > d.R) return LAGA_ERR_SHAPE;
+  const PagedPlan plan = paged_plan(d.H, d.d_c, (int)elem_size(p));
+  const PagedWs ws = paged_layout(p, d, plan);
+  if (!workspace || workspace_bytes < ws.total) return LAGA_ERR_WORKSPACE;
+  if (misaligned(workspace)) return LAGA_ERR_ALIGN;
+  char* wsb = (char*)workspace;
+  PagedArgs a{};
+  a.q = q; a.w = w_kv_b; a.cache = cache; a.table = block_table; a.row_request = row_request; a.position = position;
+  a.out = out; a.lse = lse; a.page_stride = d.page_stride; a.T = d.T; a.R = d.R; a.width = d.width;
+  a.n_pages = d.n_pages; a.page = d.page; a.H = d.H; a.d_c = d.d_c; a.d_nope = d.dn; a.d_rope = d.dr; a.d_v = d.dv;
+  a.scale_log2 = p->softmax_scale * 1.4426950408889634f;
+  if (cfg) {
+    a.rotate = 1;
+    a.position_offset = cfg->position_offset;
+    a.log2_base = log2((double)cfg->rope_base);
+  }
+  a.sched = (int32_t*)(wsb + ws.sched); a.qa = wsb + ws.qa; a.obar = wsb + ws.obar;
+  a.part_o = (float*)(wsb + ws.part_o); a.part_ml = (float*)(wsb + ws.part_ml);
+  a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.min_per = plan.min_per;
+  hipStream_t st = (hipStream_t)stream;
+  return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_paged_attn<bf16>(a, st) : launch_paged_attn<float>(a, st));
 }
 
 laga_status_t laga_prologue_fwd(const laga_problem_t* p, const laga_prologue_t* cfg, const void* latent_raw,

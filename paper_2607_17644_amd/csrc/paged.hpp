@@ -1,0 +1,130 @@
+// Serving from a paged cache of latents: the arguments of its launchers and the rules, from
+// integers alone, that size their grids and workspace (host and device use the same ones).
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include "kernels.hpp"
+
+namespace laga {
+
+// ---------------------------------------------------------------- pages
+// The step's plan and the release of pages (paged_cache.hip). Both are a scan over the
+// requests (one workgroup) and an expansion of its sums to rows and pages.
+struct PlanArgs {
+  const int32_t* lengths;     // [R] cached tokens
+  const int32_t* arg;         // [R] fresh tokens (plan), or != 0 where the request ends (release)
+  int32_t* table;             // [R][width]
+  int32_t* free_pages;        // [n_pages], a stack
+  const int32_t* free_count;  // [1]
+  int32_t* lengths_out;       // [R]; may be lengths
+  int32_t* free_count_out;    // [1]; may be free_count
+  int32_t* row_begin;         // [R + 1]  (plan)
+  int32_t* row_request;       // [rows]   (plan)
+  int32_t* position;          // [rows]   (plan)
+  int32_t* slot;              // [rows]   (plan)
+  int32_t* status;            // [1]
+  int32_t* ws;                // plan_ws_ints(R)
+  int rows, R, width, n_pages, page;
+  int release;
+};
+// workspace: [count, pages, rows, ok] then pages_before[R + 1] and the lengths as they were [R]
+constexpr int kPlanHeader = 4;
+inline size_t plan_ws_ints(long long R) { return kPlanHeader + (size_t)(R + 1) + (size_t)R; }
+hipError_t launch_plan(const PlanArgs& a, hipStream_t st);
+
+struct AppendArgs {
+  const void *latent, *kpe, *gamma;  // [T, d_c], [T, d_rope], [d_c] or NULL
+  int64_t latent_stride, kpe_stride;  // elements between rows
+  const int32_t *position, *slot;     // [T]
+  void* cache;
+  int64_t page_stride, position_offset;
+  int T, d_c, d_rope, n_slots, page;
+  float eps;
+  double log2_base;
+};
+template <typename T>
+hipError_t launch_append(const AppendArgs& a, hipStream_t st);
+
+// 8 contiguous elements to and from fp32 (bf16 rounds to nearest even)
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
+  const frag_t<T> x = *reinterpret_cast<const frag_t<T>*>(p);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = to_f32(x[e]);
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+  frag_t<T> x;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = to_elem<T>(v[e]);
+  *reinterpret_cast<frag_t<T>*>(p) = x;
+}
+
+// ---------------------------------------------------------------- attention
+// Every row t sees the cached positions 0 .. position[t] of its request. Their tiles of
+// kTileKeys keys, row after row, are one sequence of tiles; worker w of a head block takes
+// tiles [w * per, (w + 1) * per) of it, whatever rows they belong to, so ragged rows load the
+// GPU evenly and a long row is split over as many workers as its length asks for. A row that
+// one worker takes whole is finished there; of any other row each worker leaves a partial
+// (running maximum, sum, unnormalised output) in the one of its two places that the row's end
+// of its range owns.
+constexpr int kTileKeys = 32;
+constexpr int kCus = 256;  // compute units of an MI355X
+
+struct PagedArgs {
+  const void* q;               // [T, H, d_nope + d_rope]
+  const void* w;               // W_kv_b [d_c, H * (d_nope + d_v)]
+  const void* cache;           // pages of [page][d_c + d_rope], page_stride elements apart
+  const int32_t* table;        // [R][width]
+  const int32_t* row_request;  // [T] or NULL (row t is request t)
+  const int32_t* position;     // [T]
+  void* out;                   // [T, H, d_v]
+  float* lse;                  // [T, H] or NULL
+  int64_t page_stride, position_offset;
+  int T, R, width, n_pages, page, H, d_c, d_nope, d_rope, d_v;
+  float scale_log2;  // softmax_scale * log2(e)
+  int rotate;        // 1: q_rope is turned by its row's position first
+  double log2_base;
+  // workspace
+  int32_t* sched;    // [per, total] then tiles_before[T + 1] and first_row[workers]
+  void* qa;          // [T][H][d_c + d_rope]: W_k q_nope, then q_rope
+  void* obar;        // [T][H][d_c]: normalised rows that one worker took whole
+  float* part_o;     // [2 * workers][H][d_c]
+  float* part_ml;    // [2 * workers][H][2]
+  int heads_per_wg;  // heads of a head block
+  int workers;       // of each head block
+  int min_per;       // fewest tiles that a worker takes
+};
+constexpr int kSchedHeader = 4;
+
+__host__ __device__ inline int tiles_of(int visible) { return (visible + kTileKeys - 1) / kTileKeys; }
+// Tiles per worker: even shares, and no fewer than min_per.
+__host__ __device__ inline int tiles_per_worker(int total, int workers, int min_per) {
+  const int even = (int)(((int64_t)total + workers - 1) / workers);
+  return even > min_per ? even : min_per;
+}
+// The partial place of worker w's share of the row whose tiles begin at row_first: a row that
+// was begun before the worker's range (or with it) is its first, any other its last.
+__host__ __device__ inline int partial_place(int w, int per, int row_first) {
+  return 2 * w + (row_first > (int64_t)w * per ? 1 : 0);
+}
+
+struct PagedPlan {
+  int heads_per_wg, head_blocks, workers, min_per;
+};
+inline PagedPlan paged_plan(int H, int d_c, int elem_size) {
+  PagedPlan p;
+  p.heads_per_wg = 32;
+  p.head_blocks = (H + p.heads_per_wg - 1) / p.heads_per_wg;
+  const int wgs = (elem_size == 2 && d_c <= 128 ? 2 : 1) * kCus;  // what runs at once
+  const int w = wgs / p.head_blocks / 8 * 8;  // whole rounds over the 8 XCDs
+  p.workers = w > 8 ? w : 8;
+  p.min_per = 4;
+  return p;
+}
+
+template <typename T>
+hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t st);
+
+}  // namespace laga

@@ -1,0 +1,574 @@
+// Attention of new tokens over a paged cache of latents, in the absorbed form: with head h's
+// columns [W_k || W_v] of W_kv_b,
+//
+//   qa = W_k q_nope,  z_j = scale (qa . c_j + q_rope . k_j),  o = sum_j softmax(z)_j c_j,  out = W_v^T o
+//
+// so that a cached position is one row [c_j || k_j] that every head reads, and no per-head key
+// or value exists. Three launches: the products qa and the turned q_rope (absorb_kernel), the
+// attention split over the cache (split_kernel), and the join of split rows with the product
+// by W_v (join_kernel). Bound by the cache's bytes for few heads (2 (2 d_c + d_rope) flop per
+// head for each row of d_c + d_rope elements).
+#include <math.h>
+
+#define LAGA_LDS_DMA_ASM 1
+#include "common.hpp"
+#include "paged.hpp"
+#include "rope.hpp"
+
+namespace laga {
+namespace {
+
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// What the row t may see: positions [0, visible); bad: its request or its position lies
+// outside the table (the row's results are NaN, nothing is read for it).
+struct RowState {
+  int request, visible;
+  bool bad;
+};
+__device__ __forceinline__ RowState row_state(const PagedArgs& a, int t) {
+  const int p = a.position[t];
+  if (p < 0) return {0, 0, false};
+  const int r = a.row_request ? a.row_request[t] : t;
+  if ((unsigned)r >= (unsigned)a.R || p >= a.width * a.page) return {0, 0, true};
+  return {r, p + 1, false};
+}
+
+// ---------------------------------------------------------------- absorb
+// qa^T = W_k q_nope^T per head: A = rows of W_kv_b (their d_nope elements of a head are
+// contiguous), B = the tokens' q_nope, both straight from global memory (each is used once
+// per 32 tokens). A wave has 32 rows of W for all the tokens of its share. Bound by reading W.
+// The last workgroups turn q_rope, and the very last one lays out the tiles.
+constexpr int kAbsorbWaves = 4;
+
+template <typename T, int DN>
+__device__ void absorb_product(const PagedArgs& a, int blk, int cblocks, int tpart, int tparts) {
+  const int l = threadIdx.x & 63, n = l & 31, g = l >> 5;
+  const int h = blk / cblocks, c0 = (blk % cblocks * kAbsorbWaves + (threadIdx.x >> 6)) * 32;
+  if (c0 >= a.d_c) return;
+  const int W = a.d_c + a.d_rope, dqk = DN + a.d_rope;
+  const T* w = (const T*)a.w + (int64_t)(c0 + n) * a.H * (DN + a.d_v) + (int64_t)h * (DN + a.d_v) + 8 * g;
+  frag_t<T> wf[DN / 16];
+#pragma unroll
+  for (int ks = 0; ks < DN / 16; ++ks) wf[ks] = *reinterpret_cast<const frag_t<T>*>(w + 16 * ks);
+  for (int t0 = tpart * 32; t0 < a.T; t0 += tparts * 32) {
+    const int t = min(t0 + n, a.T - 1);
+    const T* q = (const T*)a.q + ((int64_t)t * a.H + h) * dqk + 8 * g;
+    f32x16 acc = {};
+#pragma unroll
+    for (int ks = 0; ks < DN / 16; ++ks) mma(acc, wf[ks], *reinterpret_cast<const frag_t<T>*>(q + 16 * ks));
+    if (t0 + n < a.T) {
+      T* o = (T*)a.qa + ((int64_t)t * a.H + h) * W + c0 + 4 * g;
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr) {
+        typename FragOf<T>::half v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = to_elem<T>(acc[4 * rr + e]);
+        *reinterpret_cast<typename FragOf<T>::half*>(o + 8 * rr) = v;
+      }
+    }
+  }
+}
+
+// q_rope of one token, every head: a thread keeps one pair's angle
+template <typename T>
+__device__ void absorb_band(const PagedArgs& a, int t) {
+  const int pairs = a.d_rope / 2, i = threadIdx.x % pairs;
+  const int W = a.d_c + a.d_rope, dqk = a.d_nope + a.d_rope;
+  float cs = 1.f, sn = 0.f;
+  if (a.rotate) rope_sincos(a.position_offset + a.position[t], rope_freq(i, a.d_rope, a.log2_base), cs, sn);
+  for (int h = threadIdx.x / pairs; h < a.H; h += 64 * kAbsorbWaves / pairs) {
+    const T* x = (const T*)a.q + ((int64_t)t * a.H + h) * dqk + a.d_nope + 2 * i;
+    T* y = (T*)a.qa + ((int64_t)t * a.H + h) * W + a.d_c + 2 * i;
+    const float x0 = to_f32(x[0]), x1 = to_f32(x[1]);
+    y[0] = to_elem<T>(x0 * cs - x1 * sn);
+    y[1] = to_elem<T>(x0 * sn + x1 * cs);
+  }
+}
+
+// Tiles before each row, tiles per worker, and the row in which each worker's share begins.
+__device__ void lay_out_tiles(const PagedArgs& a) {
+  constexpr int NT = 64 * kAbsorbWaves;
+  __shared__ int sm[kAbsorbWaves];
+  const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
+  int32_t* before = a.sched + kSchedHeader;
+  int32_t* first_row = before + a.T + 1;
+  int sum = 0;
+  for (int base = 0; base < a.T; base += NT) {
+    const int t = base + tid;
+    int n = 0;
+    if (t < a.T) n = tiles_of(row_state(a, t).visible);
+    int inc = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(inc, o);
+      if (l >= o) inc += up;
+    }
+    if (l == 63) sm[wave] = inc;
+    __syncthreads();
+    int b = sum;
+    for (int w = 0; w < kAbsorbWaves; ++w) {
+      if (w < wave) b += sm[w];
+      sum += sm[w];
+    }
+    __syncthreads();
+    if (t < a.T) before[t] = b + inc - n;
+  }
+  const int per = tiles_per_worker(sum, a.workers, a.min_per);
+  if (tid == 0) {
+    before[a.T] = sum;
+    a.sched[0] = per;
+    a.sched[1] = sum;
+  }
+  __syncthreads();
+  for (int w = tid; w < a.workers; w += NT) {
+    const int64_t start = (int64_t)w * per;
+    int lo = 0;
+    if (start < sum) {
+      int hi = a.T;  // last row whose tiles begin at or before start
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (before[mid] <= start) lo = mid; else hi = mid;
+      }
+    }
+    first_row[w] = lo;
+  }
+}
+
+template <typename T, int DN>
+__global__ __launch_bounds__(64 * kAbsorbWaves) void absorb_kernel(PagedArgs a, int cblocks, int tparts) {
+  // the few long jobs first
+  const int others = a.T + 1, id = blockIdx.x;
+  if (id == 0) lay_out_tiles(a);
+  else if (id < others) absorb_band<T>(a, id - 1);
+  else absorb_product<T, DN>(a, (id - others) / tparts, cblocks, (id - others) % tparts, tparts);
+}
+
+// ---------------------------------------------------------------- split attention
+// One workgroup of four waves takes 32 heads of a worker's tiles of 32 keys:
+//   S^T = K Q^T: the contraction over d_c + d_rope is dealt to the four waves (K fragments
+//     from LDS, the wave's part of Q in registers), whose partial S^T meet in LDS, so that every
+//     wave holds all of S^T and runs the same softmax, a lane per head;
+//   O^T += C^T P^T: the columns of c are dealt to the waves in blocks of 32, P^T straight from
+//     the S^T accumulators, C^T by transposing reads of the same LDS tile.
+// So a wave reads each byte of the tile once per product and holds a quarter of Q and O.
+// Tiles arrive by direct copies in a ring of NS stages. A key past the row's end, or whose page
+// lies outside the pool, is copied from a row of zeros: whatever the cache holds there is never
+// read; the first has probability zero, the second makes the row NaN.
+__device__ const __attribute__((aligned(16))) unsigned char kZeroRow[4608] = {};  // the widest row and its padding
+
+// LDS rows of P 16-byte chunks: [c || k || padding]. bf16: chunk c of row r at c ^ swz<24>(r),
+// conflict-free for both kinds of read at P % 16 == 8 (rows start half-way round the banks in
+// turn, as 24-chunk rows do); fp32: an odd pitch.
+template <typename T, int ND>
+struct SplitCfg {
+  static constexpr int E = 16 / sizeof(T);
+  static constexpr int P = (128 * ND + 64) / E + (sizeof(T) == 4 ? 1 : 0);
+  static constexpr int NI = (kTileKeys * P + 63) / 64;  // copies of 64 chunks per tile
+  static constexpr int PER = NI / 4;                     // of each wave, at least
+  static constexpr int TILE = NI * 64 * E;               // elements
+  static constexpr int kRing = 140 * 1024 / (NI * 1024);
+  static constexpr int NS = kRing < 1 ? 1 : kRing > 4 ? 4 : kRing;
+  static constexpr int KS = 2 * ND + 1;                  // contraction steps of 16 per wave
+};
+constexpr int kWindow = 512;  // page ids of a row held in LDS
+
+template <typename T, int ND>
+__global__ __launch_bounds__(256) void split_kernel(PagedArgs a, int head_blocks) {
+  using C = SplitCfg<T, ND>;
+  constexpr int NS = C::NS, P = C::P, E = C::E;
+  __shared__ __attribute__((aligned(16))) T ring[NS * C::TILE];
+  __shared__ f32x4 s_part[4 * 4 * 64];
+  __shared__ int32_t s_page[kWindow];
+  __shared__ uint32_t s_bad[NS];
+
+  const int l = threadIdx.x & 63, n = l & 31, g = l >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // the head blocks of a worker follow each other on one XCD: its L2 serves all but the first
+  const int id = blockIdx.x, hb = id / 8 % head_blocks, w = id / (8 * head_blocks) * 8 + id % 8;
+  const int h0 = hb * a.heads_per_wg, nh = min(a.heads_per_wg, a.H - h0);
+  const int W = a.d_c + a.d_rope;
+  const int per = a.sched[0], total = a.sched[1];
+  const int64_t start = (int64_t)w * per;
+  if (start >= total) return;
+  const int end = (int)min((int64_t)total, start + per);
+  const int32_t* before = a.sched + kSchedHeader;
+  int t = before[a.T + 1 + w];
+
+  for (int at = (int)start; at < end; ++t) {
+    const int row_first = before[t], row_end = before[t + 1];
+    if (row_end <= at) continue;
+    const int it0 = at - row_first, it1 = min(end, row_end) - row_first;
+    at = min(end, row_end);
+    const RowState rs = row_state(a, t);
+    const int32_t* pages = a.table + (int64_t)rs.request * a.width;
+
+    // this wave's part of the queries: step i covers elements 16 (wave + 4 i) ..
+    frag_t<T> qf[C::KS];
+    {
+      const T* q = (const T*)a.qa + ((int64_t)t * a.H + h0 + min(n, nh - 1)) * W + 8 * g;
+#pragma unroll
+      for (int i = 0; i < C::KS; ++i) {
+        const int c = 16 * (wave + 4 * i);
+        qf[i] = frag_t<T>{};
+        if (c < W) qf[i] = *reinterpret_cast<const frag_t<T>*>(q + c);
+      }
+    }
+    f32x16 oacc[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i) oacc[i] = f32x16{};
+    float m = -INFINITY, lsum = 0.f;
+
+    int win = -1;  // first page of the window
+    // copies of tile `it` into stage st, after a barrier that freed it
+    auto fetch = [&](int it, int st) {
+      const int k0 = it * kTileKeys, last = (min(k0 + kTileKeys, rs.visible) - 1) / a.page;
+      if (win < 0 || last >= win + kWindow) {  // the same for every thread
+        lds_barrier();
+        win = k0 / a.page;
+        const int have = (rs.visible - 1) / a.page + 1;
+        for (int i = threadIdx.x; i < kWindow; i += 256) s_page[i] = win + i < have ? pages[win + i] : -1;
+        lds_barrier();
+      }
+      const int key = k0 + n;
+      const bool live = key < rs.visible;
+      const int pg = live ? key / a.page : win, off = live ? key % a.page : 0;
+      const int pid = s_page[pg - win];
+      const bool ok = live && (unsigned)pid < (unsigned)a.n_pages;
+      const T* src = ok ? (const T*)a.cache + (int64_t)pid * a.page_stride + (int64_t)off * W : (const T*)kZeroRow;
+      const uint32_t bad = (uint32_t)__ballot(live && !ok);
+      if (threadIdx.x == 0) s_bad[st] = bad;
+      const uint32_t lo = (uint32_t)(uintptr_t)src, hi = (uint32_t)((uintptr_t)src >> 32);
+#pragma unroll
+      for (int jj = 0; jj < (C::NI + 3) / 4; ++jj) {
+        const int j = wave + 4 * jj;
+        if (C::NI % 4 == 0 || j < C::NI) {
+          const int p = j * 64 + l;
+          int row = p / P, c = p - row * P;
+          if (C::NI * 64 > kTileKeys * P && row >= kTileKeys) row = 0, c = 0;
+          if constexpr (sizeof(T) == 2) c ^= swz<24>(row);
+          const uintptr_t base = (uintptr_t)(uint32_t)__shfl((int)lo, row) |
+                                 ((uintptr_t)(uint32_t)__shfl((int)hi, row) << 32);
+          const unsigned char* from = c * E < W ? (const unsigned char*)base : kZeroRow;
+          g2lds16(from + c * 16, ring + st * C::TILE + j * 64 * E);
+        }
+      }
+    };
+
+    lds_barrier();  // the tiles and pages of the row before are read
+#pragma unroll
+    for (int i = 0; i < NS - 1; ++i)
+      if (it0 + i < it1) fetch(it0 + i, i);
+    int st = 0;
+    for (int it = it0; it < it1; ++it) {
+      if constexpr (NS == 1) {
+        lds_barrier();  // the tile before is read
+        fetch(it, 0);
+        wait_vmem();
+      } else {
+        // tile `it` has landed: only the tiles issued after it may be in flight
+        if (it + 1 < it1 && NS >= 3) {
+          if (it + 2 < it1 && NS >= 4) wait_vmem_le<2 * C::PER>();
+          else wait_vmem_le<C::PER>();
+        } else {
+          wait_vmem();
+        }
+      }
+      lds_barrier();  // ... every wave's copies, and the stage before is read
+      if constexpr (NS > 1)
+        if (it + NS - 1 < it1) fetch(it + NS - 1, st == 0 ? NS - 1 : st - 1);
+      const T* tile = ring + st * C::TILE;
+
+      f32x16 s = {};
+#pragma unroll
+      for (int i = 0; i < C::KS; ++i) {
+        const int ks = wave + 4 * i;
+        frag_t<T> k;
+        if constexpr (sizeof(T) == 2) k = *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + (((2 * ks + g) ^ swz<24>(n)) * E));
+        else k = *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + 16 * ks + 8 * g);
+        mma(s, k, qf[i]);
+      }
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+        s_part[(wave * 4 + rr) * 64 + l] = f32x4{s[4 * rr], s[4 * rr + 1], s[4 * rr + 2], s[4 * rr + 3]};
+      lds_barrier();
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr) {
+        f32x4 v = s_part[rr * 64 + l];
+#pragma unroll
+        for (int u = 1; u < 4; ++u) v += s_part[(u * 4 + rr) * 64 + l];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * rr + e] = v[e];
+      }
+      const int lim = rs.visible - it * kTileKeys - 4 * g;
+      const uint32_t bad = s_bad[st];
+      if (lim + 4 * g < kTileKeys || bad) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int k = (r >> 2) * 8 + (r & 3);
+          s[r] = k < lim ? (bad >> (k + 4 * g) & 1 ? NAN : s[r]) : -INFINITY;
+        }
+      }
+      // online softmax in base 2, the maximum raised only past a margin (kRescaleLog2)
+      float mraw = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mraw = fmaxf(mraw, s[r]);
+      const float m_new = fmaxf(m, wave_xor32_max(mraw) * a.scale_log2);
+      const bool bump = m_new > m + kRescaleLog2;
+      const float alpha = bump ? fast_exp2(m - m_new) : 1.f;
+      m = bump ? m_new : m;
+      const float m_use = m == -INFINITY ? 0.f : m;
+      float ps = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = fast_exp2(__builtin_fmaf(s[r], a.scale_log2, -m_use));
+        ps += s[r];
+      }
+      lsum = lsum * alpha + ps;
+      if (__ballot(bump)) {
+#pragma unroll
+        for (int i = 0; i < ND; ++i) oacc[i] *= alpha;
+      }
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        const frag_t<T> pf = acc_to_frag<T>(s, kk);
+        const int ra = 16 * kk + 4 * g;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+          const int c0 = 32 * (wave + 4 * i);
+          frag_t<T> cf;
+          if constexpr (sizeof(T) == 2) {
+            const int sl = l & 15, col = c0 + 16 * ((l >> 4) & 1) + 4 * (sl & 3);
+            const int r0 = ra + (sl >> 2), r1 = r0 + 8;
+            typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+            const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                (lds_bf16x4*)(tile + r0 * P * E + (((col / E) ^ swz<24>(r0)) * E) + col % E));
+            const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                (lds_bf16x4*)(tile + r1 * P * E + (((col / E) ^ swz<24>(r1)) * E) + col % E));
+            cf = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+          } else {
+            cf = TrRead<float>::get((const float*)tile, P * E, ra, ra + 8, c0);
+          }
+          mma(oacc[i], cf, pf);
+        }
+      }
+      st = st + 1 == NS ? 0 : st + 1;
+    }
+
+    // lane: head n, columns 32 (wave + 4 i) + 8 (r / 4) + 4 g + r % 4
+    const float ltot = wave_xor32_sum(lsum);
+    const bool whole = it0 == 0 && it1 == row_end - row_first;
+    const int h = h0 + n;
+    if (n >= nh) {
+      // a lane of padding
+    } else if (whole) {
+      const float inv = 1.f / ltot;
+      T* o = (T*)a.obar + ((int64_t)t * a.H + h) * a.d_c + 4 * g;
+#pragma unroll
+      for (int i = 0; i < ND; ++i)
+        if (32 * (wave + 4 * i) < a.d_c)
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr) {
+            typename FragOf<T>::half v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = to_elem<T>(oacc[i][4 * rr + e] * inv);
+            *reinterpret_cast<typename FragOf<T>::half*>(o + 32 * (wave + 4 * i) + 8 * rr) = v;
+          }
+      if (wave == 0 && g == 0 && a.lse) a.lse[(int64_t)t * a.H + h] = (m + fast_log2(ltot)) * kLn2;
+    } else {
+      const int64_t place = (int64_t)partial_place(w, per, row_first) * a.H + h;
+      float* o = a.part_o + place * a.d_c + 4 * g;
+#pragma unroll
+      for (int i = 0; i < ND; ++i)
+        if (32 * (wave + 4 * i) < a.d_c)
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr)
+            *reinterpret_cast<f32x4*>(o + 32 * (wave + 4 * i) + 8 * rr) =
+                f32x4{oacc[i][4 * rr], oacc[i][4 * rr + 1], oacc[i][4 * rr + 2], oacc[i][4 * rr + 3]};
+      if (wave == 0 && g == 0) {
+        a.part_ml[2 * place] = m;
+        a.part_ml[2 * place + 1] = ltot;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- join
+// One workgroup: kJoinRows rows of one head. Their normalised o is put together in LDS from the
+// workers' partials (weights exp2(m - max m) / sum, partials in the order of their keys), then
+// out^T = W_v^T o^T with W_v read through LDS once for all the rows.
+constexpr int kJoinRows = 32, kJoinChunk = 32;  // rows; contraction steps of W_v staged at a time
+
+template <typename T, int DV>
+__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
+  constexpr int E = 16 / sizeof(T);
+  constexpr int PV = DV + 16 / (int)sizeof(T);  // pitch of the W_v stage
+  constexpr int NVB = DV / 32, PARTS = 4 / NVB;  // 32-column blocks of out; waves that share one
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ int s_place[kJoinRows], s_n[kJoinRows], s_f0[kJoinRows];
+  const int W = a.d_c, po = W + E;  // pitch of o
+  T* so = (T*)smem;
+  T* sw = so + kJoinRows * po;
+  float* sf = (float*)(sw + kJoinChunk * PV);  // factors of the partials
+  const int tid = threadIdx.x, l = tid & 63, n = l & 31, g = l >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = blockIdx.x / tblocks, t0 = blockIdx.x % tblocks * kJoinRows, nt = min(kJoinRows, a.T - t0);
+  const int32_t* before = a.sched + kSchedHeader;
+  const int per = a.sched[0];
+
+  // rows: how many partials (0: whole, -1: nothing visible, -2: bad), the first one's place
+  if (tid < nt) {
+    const int t = t0 + tid, b = before[t], e = before[t + 1];
+    int cnt, f0 = 0;
+    if (b == e) {
+      cnt = row_state(a, t).bad ? -2 : -1;
+      if (a.lse) a.lse[(int64_t)t * a.H + h] = cnt == -2 ? NAN : -INFINITY;
+    } else {
+      const int w0 = b / per, w1 = (e - 1) / per;
+      cnt = w0 == w1 ? 0 : w1 - w0 + 1;
+      f0 = w0 - before[t0] / per + tid;  // the partials of the rows before have at most these places
+    }
+    s_n[tid] = cnt;
+    s_f0[tid] = f0;
+    s_place[tid] = b;
+  }
+  __syncthreads();
+  for (int i = wave; i < nt; i += 4) {
+    const int cnt = s_n[i];
+    if (cnt <= 0) continue;
+    const int b = s_place[i], w0 = b / per;
+    float mx = -INFINITY;
+    for (int k = l; k < cnt; k += 64)
+      mx = fmaxf(mx, a.part_ml[2 * ((int64_t)partial_place(w0 + k, per, b) * a.H + h)]);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    const float m_use = mx == -INFINITY ? 0.f : mx;
+    float sum = 0.f;
+    for (int k = l; k < cnt; k += 64) {
+      const float* ml = a.part_ml + 2 * ((int64_t)partial_place(w0 + k, per, b) * a.H + h);
+      const float f = fast_exp2(ml[0] - m_use);
+      sf[s_f0[i] + k] = f;
+      sum = __builtin_fmaf(f, ml[1], sum);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+    const float inv = 1.f / sum;
+    for (int k = l; k < cnt; k += 64) sf[s_f0[i] + k] *= inv;
+    if (l == 0 && a.lse) a.lse[(int64_t)(t0 + i) * a.H + h] = (mx + fast_log2(sum)) * kLn2;
+  }
+  __syncthreads();
+
+  const int groups = W / 8;
+  for (int x = tid; x < kJoinRows * groups; x += 256) {
+    const int i = x / groups, c = x % groups * 8;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    if (i < nt) {
+      const int cnt = s_n[i];
+      if (cnt == 0) {
+        load8((const T*)a.obar + ((int64_t)(t0 + i) * a.H + h) * W + c, v);
+      } else if (cnt == -2) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = NAN;
+      } else if (cnt > 0) {
+        const int b = s_place[i], w0 = b / per;
+#pragma unroll 4
+        for (int k = 0; k < cnt; ++k) {
+          float y[8];
+          load8(a.part_o + ((int64_t)partial_place(w0 + k, per, b) * a.H + h) * W + c, y);
+          const float f = sf[s_f0[i] + k];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(f, y[e], v[e]);
+        }
+      }
+    }
+    store8(so + i * po + c, v);
+  }
+
+  const int vb = wave % NVB, part = wave / NVB;
+  const int64_t ldw = (int64_t)a.H * (a.d_nope + DV);
+  const T* wv = (const T*)a.w + (int64_t)h * (a.d_nope + DV) + a.d_nope;
+  f32x16 acc = {};
+  for (int c0 = 0; c0 < W; c0 += kJoinChunk) {
+    __syncthreads();
+    for (int x = tid; x < kJoinChunk * (DV / E); x += 256) {
+      const int r = x / (DV / E), c = x % (DV / E) * E;
+      *reinterpret_cast<chunk16*>(sw + r * PV + c) = *reinterpret_cast<const chunk16*>(wv + (c0 + r) * ldw + c);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int ks = 0; ks < kJoinChunk / 16; ++ks) {
+      if ((c0 / 16 + ks) % PARTS != part) continue;  // wave-uniform
+      const frag_t<T> wf = TrRead<T>::get(sw, PV, 16 * ks + 8 * g, 16 * ks + 8 * g + 4, 32 * vb);
+      mma(acc, wf, lds_frag<T>(so + n * po + c0 + 16 * ks + 8 * g));
+    }
+  }
+  if constexpr (PARTS > 1) {
+    __syncthreads();
+    float* red = (float*)smem;  // (o has been read)
+    if (part > 0)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) red[(wave * 16 + r) * 64 + l] = acc[r];
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int u = 1; u < PARTS; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] += red[((vb + u * NVB) * 16 + r) * 64 + l];
+  }
+  if (n < nt) {
+    T* o = (T*)a.out + ((int64_t)(t0 + n) * a.H + h) * DV + 32 * vb + 4 * g;
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr) {
+      typename FragOf<T>::half v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = to_elem<T>(acc[4 * rr + e]);
+      *reinterpret_cast<typename FragOf<T>::half*>(o + 8 * rr) = v;
+    }
+  }
+}
+
+template <typename T, int DV>
+size_t join_lds(const PagedArgs& a) {
+  const size_t rows = sizeof(T) * ((size_t)kJoinRows * (a.d_c + 16 / sizeof(T)) + kJoinChunk * (DV + 16 / sizeof(T)));
+  const size_t red = sizeof(float) * 4 * 16 * 64;
+  const size_t front = rows > red || DV == 128 ? rows : red;
+  return front + sizeof(float) * (a.workers + 2 * kJoinRows);
+}
+
+template <typename T, int DN>
+hipError_t launch_paged_t(const PagedArgs& a, hipStream_t st) {
+  const int cblocks = (a.d_c + 32 * kAbsorbWaves - 1) / (32 * kAbsorbWaves);
+  const int64_t blocks = (int64_t)a.H * cblocks;
+  const int ttiles = (a.T + 31) / 32;
+  const int want = (int)((4 * kCus + blocks - 1) / blocks), tparts = ttiles < want ? ttiles : want;
+  absorb_kernel<T, DN><<<(unsigned)(a.T + 1 + blocks * tparts), 64 * kAbsorbWaves, 0, st>>>(a, cblocks, tparts);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int hb = (a.H + a.heads_per_wg - 1) / a.heads_per_wg;
+  const unsigned wgs = (unsigned)(hb * a.workers);
+  if (a.d_c <= 128) split_kernel<T, 1><<<wgs, 256, 0, st>>>(a, hb);
+  else if (a.d_c <= 256) split_kernel<T, 2><<<wgs, 256, 0, st>>>(a, hb);
+  else if (a.d_c <= 512) split_kernel<T, 4><<<wgs, 256, 0, st>>>(a, hb);
+  else split_kernel<T, 8><<<wgs, 256, 0, st>>>(a, hb);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int tblocks = (a.T + kJoinRows - 1) / kJoinRows;
+  join_kernel<T, DN><<<(unsigned)((int64_t)a.H * tblocks), 256, join_lds<T, DN>(a), st>>>(a, tblocks);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t st) {
+  if (a.d_nope == 128) return launch_paged_t<T, 128>(a, st);
+  if (a.d_nope == 64) return launch_paged_t<T, 64>(a, st);
+  return launch_paged_t<T, 32>(a, st);
+}
+
+template hipError_t launch_paged_attn<bf16>(const PagedArgs&, hipStream_t);
+template hipError_t launch_paged_attn<float>(const PagedArgs&, hipStream_t);
+
+}  // namespace laga

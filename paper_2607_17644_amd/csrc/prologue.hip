@@ -6,13 +6,12 @@
 //
 // Rotation of pair i (elements 2i, 2i+1 of a band d_rope wide) at position p: by the
 // angle p * base^(-2i/d_rope), counter-clockwise ((x0, x1) -> (x0 c - x1 s, x0 s + x1 c));
-// the backward applies the transpose. The angle is formed and reduced modulo 2 pi in
-// double precision, then its sine and cosine are taken in single precision on the
-// reduced angle (|a| <= pi), so positions far beyond 2^24 keep full accuracy.
+// the backward applies the transpose (the angle: rope.hpp).
 #include <math.h>
 #include <stdint.h>
 
 #include "kernels.hpp"
+#include "rope.hpp"
 
 namespace laga {
 namespace {
@@ -59,15 +58,8 @@ __device__ __forceinline__ float wave_sum(float x) {
 // cos / sin of the four pairs 4j..4j+3 of a band at position pos
 __device__ __forceinline__ void rope_cs(int64_t pos, int j, int d_rope, double log2_base, float (&c)[4],
                                         float (&s)[4]) {
-  constexpr double kTwoPi = 6.283185307179586476925286766559;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int i = 4 * j + k;
-    const double freq = exp2(-(2.0 * i / d_rope) * log2_base);
-    double a = (double)pos * freq;
-    a -= kTwoPi * rint(a / kTwoPi);
-    sincosf((float)a, &s[k], &c[k]);
-  }
+  for (int k = 0; k < 4; ++k) rope_sincos(pos, rope_freq(4 * j + k, d_rope, log2_base), c[k], s[k]);
 }
 
 // rotate the 8 elements (4 pairs) at p in place; sgn = +1 forward, -1 transpose

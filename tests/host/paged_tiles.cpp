@@ -1,0 +1,65 @@
+// How the paged attention shares out its tiles: every tile of every row belongs to one worker;
+// of a row that several workers share, each leaves its partial in a place that no other share
+// uses; and the join, which counts a row's workers from its tiles alone, finds as many partials as
+// were left, with room for their factors.
+#include <stdio.h>
+
+#include <vector>
+
+#include "paged.hpp"
+
+int main() {
+  long long shares = 0, bad = 0;
+  unsigned seed = 1;
+  auto rnd = [&](unsigned n) { return (seed = seed * 1664525u + 1013904223u) / 65536u % n; };
+  for (int heads : {1, 16, 33, 128, 129, 1000})
+    for (int d_c : {32, 128, 256, 512, 1024})
+      for (int es : {2, 4}) {
+        const laga::PagedPlan p = laga::paged_plan(heads, d_c, es);
+        if (p.workers < 8 || p.workers % 8 || p.head_blocks * p.heads_per_wg < heads ||
+            (p.head_blocks - 1) * p.heads_per_wg >= heads || p.min_per < 1)
+          ++bad;
+        for (int rows : {1, 2, 7, 64, 300, 5000})
+          for (int longest : {0, 1, 2, 40, 700, 9000}) {
+            std::vector<long long> before(rows + 1, 0);
+            for (int t = 0; t < rows; ++t) {
+              const int visible = rnd(4) == 0 ? 0 : longest ? (int)rnd(32 * longest) + 1 : 0;
+              before[t + 1] = before[t] + laga::tiles_of(visible);
+            }
+            const int total = (int)before[rows], per = laga::tiles_per_worker(total, p.workers, p.min_per);
+            if ((long long)per * p.workers < total) ++bad;
+            std::vector<int> place(2 * p.workers, -1), partials(rows, 0);
+            long long done = 0;
+            for (int w = 0; w < p.workers; ++w) {
+              const long long start = (long long)w * per, end = start + per < total ? start + per : total;
+              for (int t = 0; t < rows; ++t) {
+                const long long a = before[t] > start ? before[t] : start, b = before[t + 1] < end ? before[t + 1] : end;
+                if (a >= b) continue;
+                ++shares;
+                done += b - a;
+                if (a == before[t] && b == before[t + 1]) continue;  // whole
+                const int at = laga::partial_place(w, per, (int)before[t]);
+                if (at < 0 || at >= 2 * p.workers || place[at] >= 0) ++bad;
+                else place[at] = t;
+                ++partials[t];
+              }
+            }
+            if (done != total) ++bad;
+            for (int t0 = 0; t0 < rows; t0 += 32) {
+              int next = 0;  // factors: each row's after those of the row before
+              for (int t = t0; t < rows && t < t0 + 32; ++t) {
+                if (before[t] == before[t + 1]) continue;
+                const int w0 = (int)(before[t] / per), w1 = (int)((before[t + 1] - 1) / per);
+                if (partials[t] != (w0 == w1 ? 0 : w1 - w0 + 1)) ++bad;
+                for (int w = w0; w <= w1 && w1 > w0; ++w)
+                  if (place[laga::partial_place(w, per, (int)before[t])] != t) ++bad;
+                const int f0 = w0 - (int)(before[t0] / per) + (t - t0);
+                if (f0 < next || f0 + (w1 - w0 + 1) > p.workers + 2 * 32) ++bad;
+                next = f0 + (w1 - w0 + 1);
+              }
+            }
+          }
+      }
+  printf("%lld shares, %lld wrong\n", shares, bad);
+  return bad != 0;
+}
