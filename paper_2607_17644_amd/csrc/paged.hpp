@@ -89,7 +89,8 @@ struct PagedArgs {
   // workspace
   int32_t* sched;    // [per, total] then tiles_before[T + 1] and first_row[workers]
   void* qa;          // [T][H][d_c + d_rope]: W_k q_nope, then q_rope
-  void* obar;        // [T][H][d_c]: normalised rows that one worker took whole
+  void* qa_lo;       // bf16: what qa's rounding left, rounded
+  float* obar;       // [T][H][d_c]: normalised rows that one worker took whole
   float* part_o;     // [2 * workers][H][d_c]
   float* part_ml;    // [2 * workers][H][2]
   int heads_per_wg;  // heads of a head block

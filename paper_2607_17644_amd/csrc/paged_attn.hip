@@ -20,6 +20,12 @@ namespace {
 
 constexpr float kLn2 = 0.69314718055994530942f;
 
+// bf16: what the call computes on the way (q W_k^T and the turned band, the probabilities, the
+// normalised sums before W_v) goes into the products as two bf16 operands, x ~ hi + lo to 16
+// bits, so that only the inputs and the result have 8. One operand each would round out three
+// more times: against fp64 3.0e-3 of out's norm instead of 1.7e-3, its own rounding.
+template <typename T> constexpr bool kTwo = sizeof(T) == 2;
+
 // What the row t may see: positions [0, visible); bad: its request or its position lies
 // outside the table (the row's results are NaN, nothing is read for it).
 struct RowState {
@@ -58,13 +64,17 @@ __device__ void absorb_product(const PagedArgs& a, int blk, int cblocks, int tpa
 #pragma unroll
     for (int ks = 0; ks < DN / 16; ++ks) mma(acc, wf[ks], *reinterpret_cast<const frag_t<T>*>(q + 16 * ks));
     if (t0 + n < a.T) {
-      T* o = (T*)a.qa + ((int64_t)t * a.H + h) * W + c0 + 4 * g;
+      const int64_t at = ((int64_t)t * a.H + h) * W + c0 + 4 * g;
 #pragma unroll
       for (int rr = 0; rr < 4; ++rr) {
-        typename FragOf<T>::half v;
+        typename FragOf<T>::half v, low;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = to_elem<T>(acc[4 * rr + e]);
-        *reinterpret_cast<typename FragOf<T>::half*>(o + 8 * rr) = v;
+        for (int e = 0; e < 4; ++e) {
+          v[e] = to_elem<T>(acc[4 * rr + e]);
+          low[e] = to_elem<T>(acc[4 * rr + e] - to_f32(v[e]));
+        }
+        *reinterpret_cast<typename FragOf<T>::half*>((T*)a.qa + at + 8 * rr) = v;
+        if constexpr (kTwo<T>) *reinterpret_cast<typename FragOf<T>::half*>((T*)a.qa_lo + at + 8 * rr) = low;
       }
     }
   }
@@ -79,10 +89,15 @@ __device__ void absorb_band(const PagedArgs& a, int t) {
   if (a.rotate) rope_sincos(a.position_offset + a.position[t], rope_freq(i, a.d_rope, a.log2_base), cs, sn);
   for (int h = threadIdx.x / pairs; h < a.H; h += 64 * kAbsorbWaves / pairs) {
     const T* x = (const T*)a.q + ((int64_t)t * a.H + h) * dqk + a.d_nope + 2 * i;
-    T* y = (T*)a.qa + ((int64_t)t * a.H + h) * W + a.d_c + 2 * i;
+    const int64_t at = ((int64_t)t * a.H + h) * W + a.d_c + 2 * i;
     const float x0 = to_f32(x[0]), x1 = to_f32(x[1]);
-    y[0] = to_elem<T>(x0 * cs - x1 * sn);
-    y[1] = to_elem<T>(x0 * sn + x1 * cs);
+    const float y[2] = {x0 * cs - x1 * sn, x0 * sn + x1 * cs};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const T v = to_elem<T>(y[e]);
+      ((T*)a.qa)[at + e] = v;
+      if constexpr (kTwo<T>) ((T*)a.qa_lo)[at + e] = to_elem<T>(y[e] - to_f32(v));
+    }
   }
 }
 
@@ -204,14 +219,18 @@ __global__ __launch_bounds__(256) void split_kernel(PagedArgs a, int head_blocks
     const int32_t* pages = a.table + (int64_t)rs.request * a.width;
 
     // this wave's part of the queries: step i covers elements 16 (wave + 4 i) ..
-    frag_t<T> qf[C::KS];
+    frag_t<T> qf[C::KS], ql[kTwo<T> ? C::KS : 1];
     {
-      const T* q = (const T*)a.qa + ((int64_t)t * a.H + h0 + min(n, nh - 1)) * W + 8 * g;
+      const int64_t q = ((int64_t)t * a.H + h0 + min(n, nh - 1)) * W + 8 * g;
 #pragma unroll
       for (int i = 0; i < C::KS; ++i) {
         const int c = 16 * (wave + 4 * i);
         qf[i] = frag_t<T>{};
-        if (c < W) qf[i] = *reinterpret_cast<const frag_t<T>*>(q + c);
+        if (c < W) qf[i] = *reinterpret_cast<const frag_t<T>*>((const T*)a.qa + q + c);
+        if constexpr (kTwo<T>) {
+          ql[i] = frag_t<T>{};
+          if (c < W) ql[i] = *reinterpret_cast<const frag_t<T>*>((const T*)a.qa_lo + q + c);
+        }
       }
     }
     f32x16 oacc[ND];
@@ -287,6 +306,7 @@ __global__ __launch_bounds__(256) void split_kernel(PagedArgs a, int head_blocks
         if constexpr (sizeof(T) == 2) k = *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + (((2 * ks + g) ^ swz<24>(n)) * E));
         else k = *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + 16 * ks + 8 * g);
         mma(s, k, qf[i]);
+        if constexpr (kTwo<T>) mma(s, k, ql[i]);
       }
 #pragma unroll
       for (int rr = 0; rr < 4; ++rr)
@@ -332,6 +352,13 @@ __global__ __launch_bounds__(256) void split_kernel(PagedArgs a, int head_blocks
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
         const frag_t<T> pf = acc_to_frag<T>(s, kk);
+        frag_t<T> pl;
+        if constexpr (kTwo<T>) {
+          f32x16 low;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) low[8 * kk + e] = s[8 * kk + e] - to_f32(pf[e]);
+          pl = acc_to_frag<T>(low, kk);
+        }
         const int ra = 16 * kk + 4 * g;
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
@@ -350,6 +377,7 @@ __global__ __launch_bounds__(256) void split_kernel(PagedArgs a, int head_blocks
             cf = TrRead<float>::get((const float*)tile, P * E, ra, ra + 8, c0);
           }
           mma(oacc[i], cf, pf);
+          if constexpr (kTwo<T>) mma(oacc[i], cf, pl);
         }
       }
       st = st + 1 == NS ? 0 : st + 1;
@@ -363,17 +391,15 @@ __global__ __launch_bounds__(256) void split_kernel(PagedArgs a, int head_blocks
       // a lane of padding
     } else if (whole) {
       const float inv = 1.f / ltot;
-      T* o = (T*)a.obar + ((int64_t)t * a.H + h) * a.d_c + 4 * g;
+      float* o = a.obar + ((int64_t)t * a.H + h) * a.d_c + 4 * g;
 #pragma unroll
       for (int i = 0; i < ND; ++i)
         if (32 * (wave + 4 * i) < a.d_c)
 #pragma unroll
-          for (int rr = 0; rr < 4; ++rr) {
-            typename FragOf<T>::half v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = to_elem<T>(oacc[i][4 * rr + e] * inv);
-            *reinterpret_cast<typename FragOf<T>::half*>(o + 32 * (wave + 4 * i) + 8 * rr) = v;
-          }
+          for (int rr = 0; rr < 4; ++rr)
+            *reinterpret_cast<f32x4*>(o + 32 * (wave + 4 * i) + 8 * rr) =
+                f32x4{oacc[i][4 * rr] * inv, oacc[i][4 * rr + 1] * inv, oacc[i][4 * rr + 2] * inv,
+                      oacc[i][4 * rr + 3] * inv};
       if (wave == 0 && g == 0 && a.lse) a.lse[(int64_t)t * a.H + h] = (m + fast_log2(ltot)) * kLn2;
     } else {
       const int64_t place = (int64_t)partial_place(w, per, row_first) * a.H + h;
@@ -408,7 +434,8 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
   __shared__ int s_place[kJoinRows], s_n[kJoinRows], s_f0[kJoinRows];
   const int W = a.d_c, po = W + E;  // pitch of o
   T* so = (T*)smem;
-  T* sw = so + kJoinRows * po;
+  T* sl = so + kJoinRows * po;  // its low halves (bf16)
+  T* sw = kTwo<T> ? sl + kJoinRows * po : sl;
   float* sf = (float*)(sw + kJoinChunk * PV);  // factors of the partials
   const int tid = threadIdx.x, l = tid & 63, n = l & 31, g = l >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -467,7 +494,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
     if (i < nt) {
       const int cnt = s_n[i];
       if (cnt == 0) {
-        load8((const T*)a.obar + ((int64_t)(t0 + i) * a.H + h) * W + c, v);
+        load8(a.obar + ((int64_t)(t0 + i) * a.H + h) * W + c, v);
       } else if (cnt == -2) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = NAN;
@@ -484,6 +511,11 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
       }
     }
     store8(so + i * po + c, v);
+    if constexpr (kTwo<T>) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] -= to_f32(to_elem<T>(v[e]));
+      store8(sl + i * po + c, v);
+    }
   }
 
   const int vb = wave % NVB, part = wave / NVB;
@@ -502,6 +534,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
       if ((c0 / 16 + ks) % PARTS != part) continue;  // wave-uniform
       const frag_t<T> wf = TrRead<T>::get(sw, PV, 16 * ks + 8 * g, 16 * ks + 8 * g + 4, 32 * vb);
       mma(acc, wf, lds_frag<T>(so + n * po + c0 + 16 * ks + 8 * g));
+      if constexpr (kTwo<T>) mma(acc, wf, lds_frag<T>(sl + n * po + c0 + 16 * ks + 8 * g));
     }
   }
   if constexpr (PARTS > 1) {
@@ -531,7 +564,8 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
 
 template <typename T, int DV>
 size_t join_lds(const PagedArgs& a) {
-  const size_t rows = sizeof(T) * ((size_t)kJoinRows * (a.d_c + 16 / sizeof(T)) + kJoinChunk * (DV + 16 / sizeof(T)));
+  const size_t rows = sizeof(T) * ((kTwo<T> ? 2 : 1) * (size_t)kJoinRows * (a.d_c + 16 / sizeof(T)) +
+                                   kJoinChunk * (DV + 16 / sizeof(T)));
   const size_t red = sizeof(float) * 4 * 16 * 64;
   const size_t front = rows > red || DV == 128 ? rows : red;
   return front + sizeof(float) * (a.workers + 2 * kJoinRows);
