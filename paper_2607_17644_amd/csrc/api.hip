@@ -319,7 +319,7 @@ size_t laga_paged_workspace_bytes(const laga_paged_t* p, int op) {
   if (validate_paged(p, &d) != LAGA_OK) return 0;
   if (op == LAGA_OP_PAGE_PLAN) return plan_ws_bytes(d);
   if (op == LAGA_OP_PAGED_ATTN)
-    return paged_layout(p, d, paged_plan(d.H, d.d_c, (int)elem_size(p))).total;
+    return paged_layout(p, d, paged_plan(d.H, d.d_c, d.dr, (int)elem_size(p))).total;
   return 0;
 }
 
@@ -380,7 +380,7 @@ laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg,
     if (misaligned(x)) return LAGA_ERR_ALIGN;
   // a row's request must be known: without row_request there is one row per request at most
   if (!row_request && d.T > d.R) return LAGA_ERR_SHAPE;
-  const PagedPlan plan = paged_plan(d.H, d.d_c, (int)elem_size(p));
+  const PagedPlan plan = paged_plan(d.H, d.d_c, d.dr, (int)elem_size(p));
   const PagedWs ws = paged_layout(p, d, plan);
   if (!workspace || workspace_bytes < ws.total) return LAGA_ERR_WORKSPACE;
   if (misaligned(workspace)) return LAGA_ERR_ALIGN;
@@ -397,7 +397,7 @@ laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg,
   }
   a.sched = (int32_t*)(wsb + ws.sched); a.qa = wsb + ws.qa; a.qa_lo = wsb + ws.qa_lo; a.obar = (float*)(wsb + ws.obar);
   a.part_o = (float*)(wsb + ws.part_o); a.part_ml = (float*)(wsb + ws.part_ml);
-  a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.min_per = plan.min_per;
+  a.lse_fix = plan.wide; a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.min_per = plan.min_per;
   hipStream_t st = (hipStream_t)stream;
   return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_paged_attn<bf16>(a, st) : launch_paged_attn<float>(a, st));
 }

@@ -93,6 +93,7 @@ struct PagedArgs {
   float* obar;       // [T][H][d_c]: normalised rows that one worker took whole
   float* part_o;     // [2 * workers][H][d_c]
   float* part_ml;    // [2 * workers][H][2]
+  int lse_fix;       // the wide kernel's: lse lacks the low halves of q W_k^T (it is added in the join)
   int heads_per_wg;  // heads of a head block
   int workers;       // of each head block
   int min_per;       // fewest tiles that a worker takes
@@ -112,12 +113,15 @@ __host__ __device__ inline int partial_place(int w, int per, int row_first) {
 }
 
 struct PagedPlan {
+  bool wide;  // paged_wide.hip: bf16 with d_c = 512 and d_rope = 64
   int heads_per_wg, head_blocks, workers, min_per;
 };
-inline PagedPlan paged_plan(int H, int d_c, int elem_size) {
+inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
   PagedPlan p;
-  p.heads_per_wg = 32;
-  p.head_blocks = (H + p.heads_per_wg - 1) / p.heads_per_wg;
+  p.wide = elem_size == 2 && d_c == 512 && d_rope == 64;
+  const int most = p.wide ? 128 : 32;  // heads of a workgroup
+  p.head_blocks = (H + most - 1) / most;
+  p.heads_per_wg = p.wide ? (H + p.head_blocks - 1) / p.head_blocks : most;
   const int wgs = (elem_size == 2 && d_c <= 128 ? 2 : 1) * kCus;  // what runs at once
   const int w = wgs / p.head_blocks / 8 * 8;  // whole rounds over the 8 XCDs
   p.workers = w > 8 ? w : 8;
@@ -125,6 +129,7 @@ inline PagedPlan paged_plan(int H, int d_c, int elem_size) {
   return p;
 }
 
+void launch_paged_wide(const PagedArgs& a, int head_blocks, hipStream_t st);
 template <typename T>
 hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t st);
 

@@ -12,33 +12,11 @@
 
 #define LAGA_LDS_DMA_ASM 1
 #include "common.hpp"
-#include "paged.hpp"
+#include "paged_dev.hpp"
 #include "rope.hpp"
 
 namespace laga {
 namespace {
-
-constexpr float kLn2 = 0.69314718055994530942f;
-
-// bf16: what the call computes on the way (q W_k^T and the turned band, the probabilities, the
-// normalised sums before W_v) goes into the products as two bf16 operands, x ~ hi + lo to 16
-// bits, so that only the inputs and the result have 8. One operand each would round out three
-// more times: against fp64 3.0e-3 of out's norm instead of 1.7e-3, its own rounding.
-template <typename T> constexpr bool kTwo = sizeof(T) == 2;
-
-// What the row t may see: positions [0, visible); bad: its request or its position lies
-// outside the table (the row's results are NaN, nothing is read for it).
-struct RowState {
-  int request, visible;
-  bool bad;
-};
-__device__ __forceinline__ RowState row_state(const PagedArgs& a, int t) {
-  const int p = a.position[t];
-  if (p < 0) return {0, 0, false};
-  const int r = a.row_request ? a.row_request[t] : t;
-  if ((unsigned)r >= (unsigned)a.R || p >= a.width * a.page) return {0, 0, true};
-  return {r, p + 1, false};
-}
 
 // ---------------------------------------------------------------- absorb
 // qa^T = W_k q_nope^T per head: A = rows of W_kv_b (their d_nope elements of a head are
@@ -170,7 +148,6 @@ __global__ __launch_bounds__(64 * kAbsorbWaves) void absorb_kernel(PagedArgs a, 
 // Tiles arrive by direct copies in a ring of NS stages. A key past the row's end, or whose page
 // lies outside the pool, is copied from a row of zeros: whatever the cache holds there is never
 // read; the first has probability zero, the second makes the row NaN.
-__device__ const __attribute__((aligned(16))) unsigned char kZeroRow[4608] = {};  // the widest row and its padding
 
 // LDS rows of P 16-byte chunks: [c || k || padding]. bf16: chunk c of row r at c ^ swz<24>(r),
 // conflict-free for both kinds of read at P % 16 == 8 (rows start half-way round the banks in
@@ -420,155 +397,189 @@ __global__ __launch_bounds__(256) void split_kernel(PagedArgs a, int head_blocks
 }
 
 // ---------------------------------------------------------------- join
-// One workgroup: kJoinRows rows of one head. Their normalised o is put together in LDS from the
-// workers' partials (weights exp2(m - max m) / sum, partials in the order of their keys), then
-// out^T = W_v^T o^T with W_v read through LDS once for all the rows.
-constexpr int kJoinRows = 32, kJoinChunk = 32;  // rows; contraction steps of W_v staged at a time
-
-template <typename T, int DV>
-__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
-  constexpr int E = 16 / sizeof(T);
-  constexpr int PV = DV + 16 / (int)sizeof(T);  // pitch of the W_v stage
-  constexpr int NVB = DV / 32, PARTS = 4 / NVB;  // 32-column blocks of out; waves that share one
+// out^T = W_v^T o^T for some rows of one head. The four waves take a quarter of the contraction
+// each; a lane's column of o^T is one row's partials j, j + SUB, ... (SUB lanes share a row,
+// rows of the 32 columns: 32 / SUB), weighted by exp2(m - max m) / sum and added up in registers; as the
+// product is linear, the SUB columns are added after it. So one row split over all workers has
+// its partials read by 32 lanes at once, and a batch of whole rows keeps 32 rows per product.
+// W_v's rows arrive by direct copies meanwhile. Bound by the latency of those two reads.
+template <typename T, int DV, int NB, int NST>  // NB 32-column blocks of out; NST steps of 16 per wave
+__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, int tblocks) {
+  constexpr int E = 16 / sizeof(T), CPR = 32 * NB / E;  // 16-byte chunks of a staged row
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  __shared__ int s_place[kJoinRows], s_n[kJoinRows], s_f0[kJoinRows];
-  const int W = a.d_c, po = W + E;  // pitch of o
-  T* so = (T*)smem;
-  T* sl = so + kJoinRows * po;  // its low halves (bf16)
-  T* sw = kTwo<T> ? sl + kJoinRows * po : sl;
-  float* sf = (float*)(sw + kJoinChunk * PV);  // factors of the partials
-  const int tid = threadIdx.x, l = tid & 63, n = l & 31, g = l >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h = blockIdx.x / tblocks, t0 = blockIdx.x % tblocks * kJoinRows, nt = min(kJoinRows, a.T - t0);
+  __shared__ float s_dot[4][32];
+  T* sw = (T*)smem;
+  const int l = threadIdx.x & 63, n = l & 31, g = l >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int sub = 1 << sub_log2, j = n & (sub - 1);
+  constexpr int VB = DV / (32 * NB);
+  const int vb = blockIdx.x % VB, h = blockIdx.x / VB / tblocks;
+  const int t0 = blockIdx.x / VB % tblocks * (32 >> sub_log2), t = t0 + (n >> sub_log2);
+  const int dc = a.d_c, nch = dc * CPR;
+  const int64_t ldw = (int64_t)a.H * (a.d_nope + DV);
+  const T* wv = (const T*)a.w + (int64_t)h * (a.d_nope + DV) + a.d_nope + 32 * NB * vb;
+  for (int p0 = wave * 64; p0 < nch; p0 += 256) {
+    const int r = (p0 + l) / CPR;
+    int c = (p0 + l) % CPR;
+    if constexpr (sizeof(T) == 2) c ^= swz<CPR>(r);
+    g2lds16(wv + r * ldw + c * E, sw + p0 * E);
+  }
+
+  // this lane's share of its row's partials
   const int32_t* before = a.sched + kSchedHeader;
   const int per = a.sched[0];
-
-  // rows: how many partials (0: whole, -1: nothing visible, -2: bad), the first one's place
-  if (tid < nt) {
-    const int t = t0 + tid, b = before[t], e = before[t + 1];
-    int cnt, f0 = 0;
-    if (b == e) {
-      cnt = row_state(a, t).bad ? -2 : -1;
-      if (a.lse) a.lse[(int64_t)t * a.H + h] = cnt == -2 ? NAN : -INFINITY;
+  int first = 0, last = 0, w0 = 0;  // its partials: workers first, first + sub, .. < last
+  bool whole = false;
+  float fill = 0.f;
+  float lse = -INFINITY;
+  if (t < a.T) {
+    first = before[t];
+    last = before[t + 1];
+    if (first == last) {
+      if (row_state(a, t).bad) fill = lse = NAN;
+      last = 0;
+      w0 = 0;
     } else {
-      const int w0 = b / per, w1 = (e - 1) / per;
-      cnt = w0 == w1 ? 0 : w1 - w0 + 1;
-      f0 = w0 - before[t0] / per + tid;  // the partials of the rows before have at most these places
+      w0 = first / per;
+      last = (last - 1) / per + 1;
+      whole = last == w0 + 1;
     }
-    s_n[tid] = cnt;
-    s_f0[tid] = f0;
-    s_place[tid] = b;
   }
-  __syncthreads();
-  for (int i = wave; i < nt; i += 4) {
-    const int cnt = s_n[i];
-    if (cnt <= 0) continue;
-    const int b = s_place[i], w0 = b / per;
-    float mx = -INFINITY;
-    for (int k = l; k < cnt; k += 64)
-      mx = fmaxf(mx, a.part_ml[2 * ((int64_t)partial_place(w0 + k, per, b) * a.H + h)]);
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-    const float m_use = mx == -INFINITY ? 0.f : mx;
-    float sum = 0.f;
-    for (int k = l; k < cnt; k += 64) {
-      const float* ml = a.part_ml + 2 * ((int64_t)partial_place(w0 + k, per, b) * a.H + h);
-      const float f = fast_exp2(ml[0] - m_use);
-      sf[s_f0[i] + k] = f;
-      sum = __builtin_fmaf(f, ml[1], sum);
-    }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
-    const float inv = 1.f / sum;
-    for (int k = l; k < cnt; k += 64) sf[s_f0[i] + k] *= inv;
-    if (l == 0 && a.lse) a.lse[(int64_t)(t0 + i) * a.H + h] = (mx + fast_log2(sum)) * kLn2;
+  const int row_first = first;
+  auto place = [&](int w) { return ((int64_t)partial_place(w, per, row_first) * a.H + h); };
+  float scale = 1.f;
+  if (last > 0 && whole) {
+    if (a.lse) lse = a.lse[(int64_t)t * a.H + h];
+    scale = 1.f;
   }
-  __syncthreads();
+  float mx = -INFINITY, sum = 0.f;
+  if (!whole)
+    for (int w = w0 + j; w < last; w += sub) mx = fmaxf(mx, a.part_ml[2 * place(w)]);
+  for (int o = sub >> 1; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  const float m_use = mx == -INFINITY ? 0.f : mx;
+  if (!whole)
+    for (int w = w0 + j; w < last; w += sub)
+      sum = __builtin_fmaf(fast_exp2(a.part_ml[2 * place(w)] - m_use), a.part_ml[2 * place(w) + 1], sum);
+  for (int o = sub >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if (!whole && last > 0) {
+    scale = 1.f / sum;
+    lse = (mx + fast_log2(sum)) * kLn2;
+  }
 
-  const int groups = W / 8;
-  for (int x = tid; x < kJoinRows * groups; x += 256) {
-    const int i = x / groups, c = x % groups * 8;
-    float v[8];
+  // step i of this wave: columns 16 (NST wave + i) + {4 g .. + 3, 8 + 4 g .. + 3}
+  float v[NST][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    if (i < nt) {
-      const int cnt = s_n[i];
-      if (cnt == 0) {
-        load8(a.obar + ((int64_t)(t0 + i) * a.H + h) * W + c, v);
-      } else if (cnt == -2) {
+  for (int i = 0; i < NST; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = NAN;
-      } else if (cnt > 0) {
-        const int b = s_place[i], w0 = b / per;
-#pragma unroll 4
-        for (int k = 0; k < cnt; ++k) {
-          float y[8];
-          load8(a.part_o + ((int64_t)partial_place(w0 + k, per, b) * a.H + h) * W + c, y);
-          const float f = sf[s_f0[i] + k];
+    for (int e = 0; e < 8; ++e) v[i][e] = j == 0 ? fill : 0.f;
+  const int c0 = 16 * NST * wave + 4 * g;
+  for (int w = w0 + j; w < last; w += sub) {
+    const float* o = whole ? a.obar + ((int64_t)t * a.H + h) * dc : a.part_o + place(w) * dc;
+    const float f = whole ? 1.f : scale * fast_exp2(a.part_ml[2 * place(w)] - m_use);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(f, y[e], v[e]);
-        }
+    for (int i = 0; i < NST; ++i) {
+      if (16 * (NST * wave + i) >= dc) continue;  // wave-uniform
+      const f32x4 x = *reinterpret_cast<const f32x4*>(o + c0 + 16 * i), y = *reinterpret_cast<const f32x4*>(o + c0 + 16 * i + 8);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[i][e] = __builtin_fmaf(f, x[e], v[i][e]);
+        v[i][4 + e] = __builtin_fmaf(f, y[e], v[i][4 + e]);
       }
     }
-    store8(so + i * po + c, v);
-    if constexpr (kTwo<T>) {
+  }
+  if (a.lse && a.lse_fix && vb == 0) {
+    float dot = 0.f;
+    if (t < a.T) {
+      const T* q = (const T*)a.qa_lo + ((int64_t)t * a.H + h) * (dc + a.d_rope) + c0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] -= to_f32(to_elem<T>(v[e]));
-      store8(sl + i * po + c, v);
+      for (int i = 0; i < NST; ++i) {
+        if (16 * (NST * wave + i) >= dc) continue;
+        typedef typename FragOf<T>::half half4;
+        const half4 x = *reinterpret_cast<const half4*>(q + 16 * i), y = *reinterpret_cast<const half4*>(q + 16 * i + 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dot += v[i][e] * to_f32(x[e]) + v[i][4 + e] * to_f32(y[e]);
+      }
     }
+    dot = wave_xor32_sum(dot);
+    for (int o = sub >> 1; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
+    if (g == 0) s_dot[wave][n] = dot;
   }
 
-  const int vb = wave % NVB, part = wave / NVB;
-  const int64_t ldw = (int64_t)a.H * (a.d_nope + DV);
-  const T* wv = (const T*)a.w + (int64_t)h * (a.d_nope + DV) + a.d_nope;
-  f32x16 acc = {};
-  for (int c0 = 0; c0 < W; c0 += kJoinChunk) {
-    __syncthreads();
-    for (int x = tid; x < kJoinChunk * (DV / E); x += 256) {
-      const int r = x / (DV / E), c = x % (DV / E) * E;
-      *reinterpret_cast<chunk16*>(sw + r * PV + c) = *reinterpret_cast<const chunk16*>(wv + (c0 + r) * ldw + c);
-    }
-    __syncthreads();
+  wait_vmem();
+  lds_barrier();
+  f32x16 acc[NB];
 #pragma unroll
-    for (int ks = 0; ks < kJoinChunk / 16; ++ks) {
-      if ((c0 / 16 + ks) % PARTS != part) continue;  // wave-uniform
-      const frag_t<T> wf = TrRead<T>::get(sw, PV, 16 * ks + 8 * g, 16 * ks + 8 * g + 4, 32 * vb);
-      mma(acc, wf, lds_frag<T>(so + n * po + c0 + 16 * ks + 8 * g));
-      if constexpr (kTwo<T>) mma(acc, wf, lds_frag<T>(sl + n * po + c0 + 16 * ks + 8 * g));
+  for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
+#pragma unroll
+  for (int i = 0; i < NST; ++i) {
+    const int ks = NST * wave + i;
+    if (16 * ks >= dc) continue;
+    frag_t<T> hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      hi[e] = to_elem<T>(v[i][e]);
+      lo[e] = to_elem<T>(v[i][e] - to_f32(hi[e]));
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int ra = 16 * ks + 4 * g;
+      frag_t<T> wf;
+      if constexpr (sizeof(T) == 2) wf = swz_tr_frag<CPR>((const bf16*)sw, ra, ra + 8, 32 * b);
+      else wf = TrRead<float>::get((const float*)sw, 32 * NB, ra, ra + 8, 32 * b);
+      mma(acc[b], wf, hi);
+      if constexpr (kTwo<T>) mma(acc[b], wf, lo);
     }
   }
-  if constexpr (PARTS > 1) {
-    __syncthreads();
-    float* red = (float*)smem;  // (o has been read)
-    if (part > 0)
+  for (int o = sub >> 1; o > 0; o >>= 1)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) red[(wave * 16 + r) * 64 + l] = acc[r];
-    __syncthreads();
-    if (part > 0) return;
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int u = 1; u < PARTS; ++u)
+      for (int r = 0; r < 16; ++r) acc[b][r] += __shfl_xor(acc[b][r], o);
+  lds_barrier();  // W_v is read
+  f32x4* red = (f32x4*)smem;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[r] += red[((vb + u * NVB) * 16 + r) * 64 + l];
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr)
+      red[((wave * NB + b) * 4 + rr) * 64 + l] = f32x4{acc[b][4 * rr], acc[b][4 * rr + 1], acc[b][4 * rr + 2], acc[b][4 * rr + 3]};
+  lds_barrier();
+  if (a.lse && vb == 0 && wave == 0 && g == 0 && j == 0 && t < a.T) {
+    if (a.lse_fix)
+      lse += (((s_dot[0][n] + s_dot[1][n]) + s_dot[2][n]) + s_dot[3][n]) * a.scale_log2 * kLn2;
+    if (a.lse_fix || !whole) a.lse[(int64_t)t * a.H + h] = lse;
   }
-  if (n < nt) {
-    T* o = (T*)a.out + ((int64_t)(t0 + n) * a.H + h) * DV + 32 * vb + 4 * g;
+  // 4 NB groups of four columns per lane, dealt to the waves
+  if (t >= a.T || j != 0) return;
+  T* o = (T*)a.out + ((int64_t)t * a.H + h) * DV + 32 * NB * vb + 4 * g;
 #pragma unroll
-    for (int rr = 0; rr < 4; ++rr) {
-      typename FragOf<T>::half v;
+  for (int x = 0; x < NB; ++x) {
+    const int i = wave + 4 * x, b = i / 4, rr = i % 4;
+    f32x4 y = red[(b * 4 + rr) * 64 + l];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = to_elem<T>(acc[4 * rr + e]);
-      *reinterpret_cast<typename FragOf<T>::half*>(o + 8 * rr) = v;
-    }
+    for (int u = 1; u < 4; ++u) y += red[((u * NB + b) * 4 + rr) * 64 + l];
+    typename FragOf<T>::half z;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = to_elem<T>(y[e]);
+    *reinterpret_cast<typename FragOf<T>::half*>(o + 32 * b + 8 * rr) = z;
   }
 }
 
-template <typename T, int DV>
-size_t join_lds(const PagedArgs& a) {
-  const size_t rows = sizeof(T) * ((kTwo<T> ? 2 : 1) * (size_t)kJoinRows * (a.d_c + 16 / sizeof(T)) +
-                                   kJoinChunk * (DV + 16 / sizeof(T)));
-  const size_t red = sizeof(float) * 4 * 16 * 64;
-  const size_t front = rows > red || DV == 128 ? rows : red;
-  return front + sizeof(float) * (a.workers + 2 * kJoinRows);
+// Lanes per row: as many as leave 32 / SUB >= T rows, and more while the launch is small and a
+// row may have that many partials.
+template <typename T, int DV, int NB>
+hipError_t launch_join(const PagedArgs& a, hipStream_t st) {
+  int sl = 0;
+  while (sl < 5 && (a.T << sl) <= 16) ++sl;
+  auto blocks = [&] { return (int)(((int64_t)a.T + (32 >> sl) - 1) / (32 >> sl)); };
+  while (sl < 5 && (int64_t)a.H * (DV / (32 * NB)) * blocks() < 2 * kCus && ((int64_t)a.T << sl) < a.workers) ++sl;
+  const unsigned wgs = (unsigned)((int64_t)a.H * (DV / (32 * NB)) * blocks());
+  const size_t w = (size_t)a.d_c * 32 * NB * sizeof(T), red = (size_t)NB * 16384, lds = w > red ? w : red;
+  const int tb = blocks();
+  if (a.d_c <= 128) join_kernel<T, DV, NB, 2><<<wgs, 256, lds, st>>>(a, sl, tb);
+  else if (a.d_c <= 256) join_kernel<T, DV, NB, 4><<<wgs, 256, lds, st>>>(a, sl, tb);
+  else if (a.d_c <= 512) join_kernel<T, DV, NB, 8><<<wgs, 256, lds, st>>>(a, sl, tb);
+  else join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, sl, tb);
+  return hipGetLastError();
 }
 
 template <typename T, int DN>
@@ -582,15 +593,14 @@ hipError_t launch_paged_t(const PagedArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   const int hb = (a.H + a.heads_per_wg - 1) / a.heads_per_wg;
   const unsigned wgs = (unsigned)(hb * a.workers);
-  if (a.d_c <= 128) split_kernel<T, 1><<<wgs, 256, 0, st>>>(a, hb);
+  if (a.lse_fix) launch_paged_wide(a, hb, st);
+  else if (a.d_c <= 128) split_kernel<T, 1><<<wgs, 256, 0, st>>>(a, hb);
   else if (a.d_c <= 256) split_kernel<T, 2><<<wgs, 256, 0, st>>>(a, hb);
   else if (a.d_c <= 512) split_kernel<T, 4><<<wgs, 256, 0, st>>>(a, hb);
   else split_kernel<T, 8><<<wgs, 256, 0, st>>>(a, hb);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int tblocks = (a.T + kJoinRows - 1) / kJoinRows;
-  join_kernel<T, DN><<<(unsigned)((int64_t)a.H * tblocks), 256, join_lds<T, DN>(a), st>>>(a, tblocks);
-  return hipGetLastError();
+  return launch_join<T, DN, 1>(a, st);
 }
 
 }  // namespace

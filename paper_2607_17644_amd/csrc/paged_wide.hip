@@ -1,0 +1,354 @@
+// Split attention over the paged cache for bf16 with d_c = 512 and d_rope = 64: a wave owns 32
+// heads over the whole row, so every byte of a tile that it reads from LDS feeds 32 heads and
+// no partial scores cross waves. (paged_attn.hip has the form for any width.)
+#define LAGA_LDS_DMA_ASM 1
+#include "paged_dev.hpp"
+
+namespace laga {
+namespace {
+
+// A workgroup's four waves are HG groups of 32 heads x KP = 4 / HG parts of the keys: the waves
+// of one part share a tile (HG = 4: more than 64 heads), the parts take every KP-th tile and
+// meet at the row's end. A part's ring has HG stages, so that four tiles fit in LDS; with HG = 1
+// a wave fills and reads its one stage by itself, and the other three waves' copies and
+// products overlap with its wait.
+//   S^T = K Q^T, O^T += C^T P^T, a lane per head, as in the general kernel
+// Registers: Q (36 fragments of a row's 576 elements), the low halves of its band, and O (512 columns
+// x 32 heads) in the accumulation registers. The low halves of q W_k^T have no room: their effect on
+// lse is added to first order where the rows are joined, as scale * lo . o (the second is below 1e-6).
+constexpr int kDc = 512, kDr = 64, kRow = kDc + kDr;
+constexpr int kMain = kTileKeys * kDc, kBand = kTileKeys * kDr, kTile = kMain + kBand;  // elements
+// The softmax's reference is the maximum of the part's first tile and stays, so that no sum is ever rescaled
+// (O would have to leave the accumulation registers for it): bf16 and fp32 hold 2^kHead as
+// they hold 1, and probabilities, sums and their parts keep their precision. Where a later score passes it by
+// more, the row's share is swept again, for its maximum and then with it.
+constexpr float kHead = 64.f;
+constexpr int kPages = 128;  // page ids of a row that a wave keeps in LDS
+
+// A product of the chain S^T. Written out, because S^T has to stay in ordinary registers (the
+// accumulation ones are all O's); scores_done waits until the chain's last product is written.
+__device__ __forceinline__ void score_step(f32x16& s, const bf16x8& k, const bf16x8& q, bool first) {
+  if (first) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "v"(q));
+  else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "v"(q));
+}
+__device__ __forceinline__ void scores_done(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 15" : "+v"(s)); }
+
+// The lane, formed anew wherever it is asked for: values derived from one kept all the way would fill
+// the registers, and a spilled one's reload waits for the copies in flight.
+__device__ __forceinline__ int fresh_lane() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+template <typename V>
+__device__ __forceinline__ V lds_at(uint32_t address) {
+  return *(__attribute__((address_space(3))) const V*)(uintptr_t)address;
+}
+
+template <int HG>
+__global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_blocks) {
+  constexpr int KP = 4 / HG, NS = HG;
+  __shared__ __attribute__((aligned(16))) bf16 ring[4 * kTile];
+  __shared__ int32_t s_page[4][kPages];
+  __shared__ float s_m[4][32], s_l[4][32];
+  __shared__ int s_high[4];
+
+  const int l = threadIdx.x & 63, n = l & 31, g = l >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hg = wave % HG, kp = wave / HG;
+  // the head blocks of a worker follow each other on one XCD: its L2 serves all but the first
+  const int id = blockIdx.x, hb = id / 8 % head_blocks, w = id / (8 * head_blocks) * 8 + id % 8;
+  const int h0 = hb * a.heads_per_wg + 32 * hg;
+  const int nh = min(32, min(a.H, (hb + 1) * a.heads_per_wg) - h0);  // <= 0: this wave only copies
+  const int per = a.sched[0], total = a.sched[1];
+  const int64_t start = (int64_t)w * per;
+  if (start >= total) return;
+  const int end = (int)min((int64_t)total, start + per);
+  const int32_t* before = a.sched + kSchedHeader;
+  int t = before[a.T + 1 + w];
+  int32_t* win_ids = s_page[wave];
+
+  for (int at = (int)start; at < end; ++t) {
+    const int row_first = before[t], row_end = before[t + 1];
+    if (row_end <= at) continue;
+    const int it0 = at - row_first, it1 = min(end, row_end) - row_first;
+    at = min(end, row_end);
+    const RowState rs = row_state(a, t);
+    const int visible = min(rs.visible, it1 * kTileKeys);  // to the end of this share
+    const int32_t* pages = a.table + (int64_t)rs.request * a.width;
+
+    bf16x8 qf[kRow / 16], ql[kDr / 16];
+    {
+      const int64_t q = ((int64_t)t * a.H + (nh > 0 ? h0 + min(n, nh - 1) : 0)) * kRow + 8 * g;
+#pragma unroll
+      for (int i = 0; i < kRow / 16; ++i) qf[i] = *reinterpret_cast<const bf16x8*>((const bf16*)a.qa + q + 16 * i);
+#pragma unroll
+      for (int i = 0; i < kDr / 16; ++i)
+        ql[i] = *reinterpret_cast<const bf16x8*>((const bf16*)a.qa_lo + q + kDc + 16 * i);
+    }
+    f32x16 oacc[kDc / 32];
+    float m = -INFINITY, lsum;
+    bool high;
+    int win;
+    // this wave's share of the copies of tile `it` into buf; returns its keys with no page
+    auto fetch = [&](int it, bf16* buf) -> uint32_t {
+      const int l = fresh_lane(), n = l & 31;
+      const int k0 = it * kTileKeys, last = (min(k0 + kTileKeys, visible) - 1) / a.page;
+      if (k0 < visible && (win < 0 || last >= win + kPages)) {
+        win = k0 / a.page;
+        const int have = (visible - 1) / a.page + 1;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = l; i < kPages; i += 64) win_ids[i] = win + i < have ? pages[win + i] : -1;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+      const int key = k0 + n;
+      const bool live = key < visible;
+      const int pg = live ? key / a.page : win, off = live ? key % a.page : 0;
+      const int pid = win_ids[pg - win];  // (0 of the last window for a tile past the end)
+      const bool ok = live && (unsigned)pid < (unsigned)a.n_pages;
+      const bf16* src =
+          ok ? (const bf16*)a.cache + (int64_t)pid * a.page_stride + (int64_t)off * kRow : (const bf16*)kZeroRow;
+      const int lo = (int)(uint32_t)(uintptr_t)src, hi = (int)(uint32_t)((uintptr_t)src >> 32);
+#pragma unroll
+      for (int j = 0; j < kTileKeys / HG; ++j) {
+        const int r = hg + HG * j;
+        const uintptr_t base = (uintptr_t)(uint32_t)__builtin_amdgcn_readlane(lo, r) |
+                               ((uintptr_t)(uint32_t)__builtin_amdgcn_readlane(hi, r) << 32);
+        g2lds16_so((const void*)base, (uint32_t)((l ^ swz<16>(r)) * 16), buf + r * kDc);
+      }
+#pragma unroll
+      for (int j = 0; j < 4 / HG; ++j) {
+        const int i = hg + HG * j, r = 8 * i + (l >> 3);
+        const uintptr_t base =
+            (uintptr_t)(uint32_t)__shfl(lo, r) | ((uintptr_t)(uint32_t)__shfl(hi, r) << 32);
+        g2lds16((const bf16*)base + kDc + (((l & 7) ^ swz<8>(r)) * 8), buf + kMain + i * 512);
+      }
+      return (uint32_t)__ballot(live && !ok);
+    };
+    // fragments are read three products ahead, in a pinned order
+    constexpr int PF = 3, NQ = kRow / 16, NV = 2 * (kDc / 32);
+    // Chunk c of a tile's row r is at c ^ swz<16>(r) (c part; c ^ swz<8>(r) in the band). This lane
+    // reads the fragment of contraction step i in row n at (k ^ 32 (i % 8)) + 256 (i / 8), of
+    // the band's step i at b ^ 32 i, and for the transposing reads of column block i, rows vr
+    // and vr + 8, at (v ^ 64 (i % 4)) + 256 (i / 4) and likewise v8.
+    struct Reads { uint32_t k, b, v, v8; };
+    auto reads_of = [&](const bf16* buf) {
+      const uint32_t at = lds_address(buf);
+      const int l = fresh_lane(), n = l & 31, g = l >> 5;
+      const int sl = l & 15, vr = 4 * g + (sl >> 2), vc = 2 * ((l >> 4) & 1) + ((sl & 3) >> 1);
+      return Reads{at + 2 * n * kDc + ((g ^ swz<16>(n)) * 16), at + 2 * (kMain + n * kDr) + ((g ^ swz<8>(n)) * 16),
+                   at + 2 * vr * kDc + ((vc ^ swz<16>(vr)) * 16) + 8 * (sl & 1),
+                   at + 2 * (vr + 8) * kDc + ((vc ^ swz<16>(vr + 8)) * 16) + 8 * (sl & 1)};
+    };
+    auto k_frag = [&](const Reads& x, int i) {
+      return i < kDc / 16 ? lds_at<bf16x8>((x.k ^ (32 * (i % 8))) + 256 * (i / 8)) : lds_at<bf16x8>(x.b ^ (32 * (i - kDc / 16)));
+    };
+    auto v_frag = [&](const Reads& x, int i) {  // column block i % 16, keys 16 (i / 16) ..
+      const uint32_t flip = 64 * (i % 4), add = 256 * (i % 16 / 4) + 32 * kDc * (i / 16);
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)((x.v ^ flip) + add));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)((x.v8 ^ flip) + add));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // S^T of a tile, and its largest score over the lane's head
+    auto scores = [&](int it, const Reads& x, uint32_t bad, f32x16& s) {
+      bf16x8 k[PF + 1];
+#pragma unroll
+      for (int i = 0; i < PF; ++i) k[i] = k_frag(x, i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        if (i + PF < NQ) k[(i + PF) % (PF + 1)] = k_frag(x, i + PF);
+        score_step(s, k[i % (PF + 1)], qf[i], i == 0);
+        if (i >= kDc / 16) score_step(s, k[i % (PF + 1)], ql[i - kDc / 16], false);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      scores_done(s);
+      const int lim = visible - it * kTileKeys;
+      if (lim < kTileKeys || bad) {
+        const int g = fresh_lane() >> 5;  // (and keeps the branch)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int k = (r >> 2) * 8 + (r & 3) + 4 * g;
+          s[r] = k < lim ? (bad >> k & 1 ? NAN : s[r]) : -INFINITY;
+        }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
+      return wave_xor32_max(mx) * a.scale_log2;
+    };
+    // O and the sums with a tile's probabilities
+    auto update = [&](int it, const bf16* buf, uint32_t bad) {
+      const Reads x = reads_of(buf);
+      f32x16 s;
+      const float mx = scores(it, x, bad, s);
+      m = m == -INFINITY ? mx : m;  // (nothing but zeros or NaN is summed up so far)
+      high |= __ballot(mx > m + kHead) != 0;
+      const float m_use = m == -INFINITY ? 0.f : m;
+      float ps = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = fast_exp2(__builtin_fmaf(s[r], a.scale_log2, -m_use));
+        ps += s[r];
+      }
+      lsum += ps;
+      bf16x8 pf[2], pl[2];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        pf[kk] = acc_to_frag<bf16>(s, kk);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[8 * kk + e] -= to_f32(pf[kk][e]);
+        pl[kk] = acc_to_frag<bf16>(s, kk);
+      }
+      bf16x8 v[PF + 1];
+#pragma unroll
+      for (int i = 0; i < PF; ++i) v[i] = v_frag(x, i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (i + PF < NV) v[(i + PF) % (PF + 1)] = v_frag(x, i + PF);
+        mma(oacc[i % 16], v[i % (PF + 1)], pf[i / 16]);
+        mma(oacc[i % 16], v[i % (PF + 1)], pl[i / 16]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // the tiles of this wave's part, in order; a tile past the share's end (a part's last step) is
+    // copied from zeros and all masked
+    const int steps = (it1 - it0 + KP - 1) / KP;
+    auto sweep = [&](auto&& body) {
+      win = -1;
+      lds_barrier();  // the tiles of the sweep before, and its parts, are read
+      if constexpr (HG == 1) {
+        bf16* buf = ring + kp * kTile;
+        for (int it = it0 + kp, i = 0; i < steps; ++i, it += KP) {
+          const uint32_t bad = fetch(it, buf);
+          wait_vmem();
+          body(it, buf, bad);
+        }
+      } else {
+        constexpr int PER = (kTileKeys + 4) / HG;  // copies of a wave per tile
+        uint32_t bads[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) bads[i] = 0;
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i)
+          if (i < steps) bads[i] = fetch(it0 + i * KP + kp, ring + (i * KP + kp) * kTile);
+        int st = 0;
+        for (int step = 0; step < steps; ++step) {
+          const int it = it0 + step * KP + kp;
+          if (step + 2 < steps && NS >= 4) wait_vmem_le<2 * PER>();
+          else if (step + 1 < steps && NS >= 3) wait_vmem_le<PER>();
+          else wait_vmem();
+          lds_barrier();  // every wave's copies of the step's tiles; the stage before is read
+          if (step + NS - 1 < steps)
+            bads[NS - 1] = fetch(it + (NS - 1) * KP, ring + ((st == 0 ? NS - 1 : st - 1) * KP + kp) * kTile);
+          body(it, ring + (st * KP + kp) * kTile, bads[0]);
+#pragma unroll
+          for (int i = 0; i < NS - 1; ++i) bads[i] = bads[i + 1];
+          st = st + 1 == NS ? 0 : st + 1;
+        }
+      }
+    };
+    for (bool again = false;; again = true) {
+#pragma unroll
+      for (int i = 0; i < kDc / 32; ++i) oacc[i] = f32x16{};
+      lsum = 0.f;
+      high = false;
+      sweep(update);
+      if (again) break;
+      if (l == 0) s_high[wave] = high;
+      lds_barrier();
+      if (!(s_high[0] | s_high[1] | s_high[2] | s_high[3])) break;
+      sweep([&](int it, const bf16* buf, uint32_t bad) {
+        f32x16 s;
+        m = fmaxf(m, scores(it, reads_of(buf), bad, s));
+      });
+    }
+
+    // lane: head n, columns 32 i + 8 (r / 4) + 4 g + r % 4
+    const bool whole = it0 == 0 && it1 == row_end - row_first;
+    float ltot = wave_xor32_sum(lsum), f = 1.f;
+    if constexpr (KP > 1) {
+      if (g == 0) { s_m[wave][n] = m; s_l[wave][n] = ltot; }
+      lds_barrier();  // (and every wave has read its tiles)
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < KP; ++u) mx = fmaxf(mx, s_m[u * HG + hg][n]);
+      const float m_use = mx == -INFINITY ? 0.f : mx;
+      ltot = 0.f;
+#pragma unroll
+      for (int u = 0; u < KP; ++u)
+        ltot = __builtin_fmaf(s_l[u * HG + hg][n], fast_exp2(s_m[u * HG + hg][n] - m_use), ltot);
+      f = fast_exp2(m - m_use);
+      m = mx;
+    }
+    if (whole) f *= 1.f / ltot;
+    const int h = h0 + n;
+    float* o = whole ? a.obar + ((int64_t)t * a.H + h) * kDc
+                     : a.part_o + ((int64_t)partial_place(w, per, row_first) * a.H + h) * kDc;
+    o += 4 * g;
+    if constexpr (KP == 1) {
+      if (n < nh) {
+#pragma unroll
+        for (int i = 0; i < kDc / 32; ++i)
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr)
+            *reinterpret_cast<f32x4*>(o + 32 * i + 8 * rr) =
+                f32x4{oacc[i][4 * rr] * f, oacc[i][4 * rr + 1] * f, oacc[i][4 * rr + 2] * f, oacc[i][4 * rr + 3] * f};
+      }
+    } else {
+      // parts of eight column blocks at a time through the tiles' LDS; each wave adds up its
+      // 8 / KP blocks of them, parts in order
+      f32x4* x = (f32x4*)ring;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (half > 0) lds_barrier();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr) {
+            const f32x16& v = oacc[8 * half + i];
+            x[((wave * 8 + i) * 4 + rr) * 64 + l] = f32x4{v[4 * rr] * f, v[4 * rr + 1] * f, v[4 * rr + 2] * f, v[4 * rr + 3] * f};
+          }
+        lds_barrier();
+#pragma unroll
+        for (int j = 0; j < 8 / KP; ++j) {
+          const int i = kp * (8 / KP) + j;
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr) {
+            f32x4 v = x[((hg * 8 + i) * 4 + rr) * 64 + l];
+#pragma unroll
+            for (int u = 1; u < KP; ++u) v += x[(((u * HG + hg) * 8 + i) * 4 + rr) * 64 + l];
+            if (n < nh) *reinterpret_cast<f32x4*>(o + 32 * (8 * half + i) + 8 * rr) = v;
+          }
+        }
+      }
+    }
+    if (kp == 0 && g == 0 && n < nh) {
+      if (!whole) {
+        float* ml = a.part_ml + 2 * ((int64_t)partial_place(w, per, row_first) * a.H + h);
+        ml[0] = m;
+        ml[1] = ltot;
+      } else if (a.lse) {
+        a.lse[(int64_t)t * a.H + h] = (m + fast_log2(ltot)) * kLn2;
+      }
+    }
+  }
+}
+
+}  // namespace
+
+void launch_paged_wide(const PagedArgs& a, int head_blocks, hipStream_t st) {
+  const unsigned wgs = (unsigned)(head_blocks * a.workers);
+  if (a.heads_per_wg > 64) wide_kernel<4><<<wgs, 256, 0, st>>>(a, head_blocks);
+  else if (a.heads_per_wg > 32) wide_kernel<2><<<wgs, 256, 0, st>>>(a, head_blocks);
+  else wide_kernel<1><<<wgs, 256, 0, st>>>(a, head_blocks);
+}
+
+}  // namespace laga

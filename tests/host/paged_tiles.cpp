@@ -1,7 +1,6 @@
 // How the paged attention shares out its tiles: every tile of every row belongs to one worker;
 // of a row that several workers share, each leaves its partial in a place that no other share
-// uses; and the join, which counts a row's workers from its tiles alone, finds as many partials as
-// were left, with room for their factors.
+// uses; and the join, which counts a row's workers from its tiles alone, finds those partials.
 #include <stdio.h>
 
 #include <vector>
@@ -15,7 +14,7 @@ int main() {
   for (int heads : {1, 16, 33, 128, 129, 1000})
     for (int d_c : {32, 128, 256, 512, 1024})
       for (int es : {2, 4}) {
-        const laga::PagedPlan p = laga::paged_plan(heads, d_c, es);
+        const laga::PagedPlan p = laga::paged_plan(heads, d_c, 64, es);
         if (p.workers < 8 || p.workers % 8 || p.head_blocks * p.heads_per_wg < heads ||
             (p.head_blocks - 1) * p.heads_per_wg >= heads || p.min_per < 1)
           ++bad;
@@ -45,18 +44,12 @@ int main() {
               }
             }
             if (done != total) ++bad;
-            for (int t0 = 0; t0 < rows; t0 += 32) {
-              int next = 0;  // factors: each row's after those of the row before
-              for (int t = t0; t < rows && t < t0 + 32; ++t) {
-                if (before[t] == before[t + 1]) continue;
-                const int w0 = (int)(before[t] / per), w1 = (int)((before[t + 1] - 1) / per);
-                if (partials[t] != (w0 == w1 ? 0 : w1 - w0 + 1)) ++bad;
-                for (int w = w0; w <= w1 && w1 > w0; ++w)
-                  if (place[laga::partial_place(w, per, (int)before[t])] != t) ++bad;
-                const int f0 = w0 - (int)(before[t0] / per) + (t - t0);
-                if (f0 < next || f0 + (w1 - w0 + 1) > p.workers + 2 * 32) ++bad;
-                next = f0 + (w1 - w0 + 1);
-              }
+            for (int t = 0; t < rows; ++t) {
+              if (before[t] == before[t + 1]) continue;
+              const int w0 = (int)(before[t] / per), w1 = (int)((before[t + 1] - 1) / per);
+              if (partials[t] != (w0 == w1 ? 0 : w1 - w0 + 1)) ++bad;
+              for (int w = w0; w <= w1 && w1 > w0; ++w)
+                if (place[laga::partial_place(w, per, (int)before[t])] != t) ++bad;
             }
           }
       }
