@@ -390,6 +390,7 @@ laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg,
   a.out = out; a.lse = lse; a.page_stride = d.page_stride; a.T = d.T; a.R = d.R; a.width = d.width;
   a.n_pages = d.n_pages; a.page = d.page; a.H = d.H; a.d_c = d.d_c; a.d_nope = d.dn; a.d_rope = d.dr; a.d_v = d.dv;
   a.scale_log2 = p->softmax_scale * 1.4426950408889634f;
+  page_division(d.page, &a.page_magic, &a.page_shift);
   if (cfg) {
     a.rotate = 1;
     a.position_offset = cfg->position_offset;

@@ -83,6 +83,7 @@ struct PagedArgs {
   float* lse;                  // [T, H] or NULL
   int64_t page_stride, position_offset;
   int T, R, width, n_pages, page, H, d_c, d_nope, d_rope, d_v;
+  uint32_t page_magic, page_shift;  // key / page = key * page_magic >> page_shift for 0 <= key < 2^31
   float scale_log2;  // softmax_scale * log2(e)
   int rotate;        // 1: q_rope is turned by its row's position first
   double log2_base;
@@ -110,6 +111,16 @@ __host__ __device__ inline int tiles_per_worker(int total, int workers, int min_
 // was begun before the worker's range (or with it) is its first, any other its last.
 __host__ __device__ inline int partial_place(int w, int per, int row_first) {
   return 2 * w + (row_first > (int64_t)w * per ? 1 : 0);
+}
+
+// With s = ceil(log2(page)) and M = ceil(2^(31 + s) / page) < 2^32: M page = 2^(31 + s) + e with
+// e < page <= 2^s, so key M / 2^(31 + s) = key / page + key e / (page 2^(31 + s)), and the second
+// term is below 1 / page for key < 2^31: it never carries over to the next whole number.
+inline void page_division(int page, uint32_t* magic, uint32_t* shift) {
+  uint32_t s = 0;
+  while (((int64_t)1 << s) < page) ++s;
+  *shift = 31 + s;
+  *magic = (uint32_t)((((uint64_t)1 << (31 + s)) + page - 1) / page);
 }
 
 struct PagedPlan {

@@ -216,19 +216,20 @@ __global__ __launch_bounds__(256) void split_kernel(PagedArgs a, int head_blocks
     float m = -INFINITY, lsum = 0.f;
 
     int win = -1;  // first page of the window
+    auto page_of = [&](int key) { return (int)((uint64_t)(uint32_t)key * a.page_magic >> a.page_shift); };
     // copies of tile `it` into stage st, after a barrier that freed it
     auto fetch = [&](int it, int st) {
-      const int k0 = it * kTileKeys, last = (min(k0 + kTileKeys, rs.visible) - 1) / a.page;
+      const int k0 = it * kTileKeys, last = page_of(min(k0 + kTileKeys, rs.visible) - 1);
       if (win < 0 || last >= win + kWindow) {  // the same for every thread
         lds_barrier();
-        win = k0 / a.page;
-        const int have = (rs.visible - 1) / a.page + 1;
+        win = page_of(k0);
+        const int have = page_of(rs.visible - 1) + 1;
         for (int i = threadIdx.x; i < kWindow; i += 256) s_page[i] = win + i < have ? pages[win + i] : -1;
         lds_barrier();
       }
       const int key = k0 + n;
       const bool live = key < rs.visible;
-      const int pg = live ? key / a.page : win, off = live ? key % a.page : 0;
+      const int pg = live ? page_of(key) : win, off = live ? key - pg * a.page : 0;
       const int pid = s_page[pg - win];
       const bool ok = live && (unsigned)pid < (unsigned)a.n_pages;
       const T* src = ok ? (const T*)a.cache + (int64_t)pid * a.page_stride + (int64_t)off * W : (const T*)kZeroRow;
@@ -446,25 +447,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, in
     }
   }
   const int row_first = first;
-  auto place = [&](int w) { return ((int64_t)partial_place(w, per, row_first) * a.H + h); };
-  float scale = 1.f;
-  if (last > 0 && whole) {
-    if (a.lse) lse = a.lse[(int64_t)t * a.H + h];
-    scale = 1.f;
-  }
-  float mx = -INFINITY, sum = 0.f;
-  if (!whole)
-    for (int w = w0 + j; w < last; w += sub) mx = fmaxf(mx, a.part_ml[2 * place(w)]);
-  for (int o = sub >> 1; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-  const float m_use = mx == -INFINITY ? 0.f : mx;
-  if (!whole)
-    for (int w = w0 + j; w < last; w += sub)
-      sum = __builtin_fmaf(fast_exp2(a.part_ml[2 * place(w)] - m_use), a.part_ml[2 * place(w) + 1], sum);
-  for (int o = sub >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if (!whole && last > 0) {
-    scale = 1.f / sum;
-    lse = (mx + fast_log2(sum)) * kLn2;
-  }
+  if (whole && a.lse) lse = a.lse[(int64_t)t * a.H + h];
 
   // step i of this wave: columns 16 (NST wave + i) + {4 g .. + 3, 8 + 4 g .. + 3}
   float v[NST][8];
@@ -473,19 +456,51 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, in
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[i][e] = j == 0 ? fill : 0.f;
   const int c0 = 16 * NST * wave + 4 * g;
+  // this lane's partials under their own running maximum: nothing waits for another lane's
+  float mx = -INFINITY, sum = 0.f;
   for (int w = w0 + j; w < last; w += sub) {
-    const float* o = whole ? a.obar + ((int64_t)t * a.H + h) * dc : a.part_o + place(w) * dc;
-    const float f = whole ? 1.f : scale * fast_exp2(a.part_ml[2 * place(w)] - m_use);
+    const int64_t p = (int64_t)partial_place(w, per, row_first) * a.H + h;
+    const float* o = whole ? a.obar + ((int64_t)t * a.H + h) * dc : a.part_o + p * dc;
+    f32x4 x[NST], y[NST];
 #pragma unroll
     for (int i = 0; i < NST; ++i) {
       if (16 * (NST * wave + i) >= dc) continue;  // wave-uniform
-      const f32x4 x = *reinterpret_cast<const f32x4*>(o + c0 + 16 * i), y = *reinterpret_cast<const f32x4*>(o + c0 + 16 * i + 8);
+      x[i] = *reinterpret_cast<const f32x4*>(o + c0 + 16 * i);
+      y[i] = *reinterpret_cast<const f32x4*>(o + c0 + 16 * i + 8);
+    }
+    float f = 1.f, old = 1.f;
+    if (!whole) {
+      const float m = a.part_ml[2 * p], l = a.part_ml[2 * p + 1], m_new = fmaxf(mx, m);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      f = fast_exp2(m - m_use);
+      old = mx == -INFINITY ? 0.f : fast_exp2(mx - m_use);
+      mx = m_new;
+      sum = __builtin_fmaf(sum, old, f * l);
+    }
+#pragma unroll
+    for (int i = 0; i < NST; ++i) {
+      if (16 * (NST * wave + i) >= dc) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        v[i][e] = __builtin_fmaf(f, x[e], v[i][e]);
-        v[i][4 + e] = __builtin_fmaf(f, y[e], v[i][4 + e]);
+        v[i][e] = __builtin_fmaf(f, x[i][e], v[i][e] * old);
+        v[i][4 + e] = __builtin_fmaf(f, y[i][e], v[i][4 + e] * old);
       }
     }
+  }
+  // and brought to the row's
+  if (last > 0 && !whole) {  // (the same for the lanes of a row)
+    float all = mx;
+    for (int o = sub >> 1; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o));
+    const float m_use = all == -INFINITY ? 0.f : all;
+    float f = mx == -INFINITY ? 0.f : fast_exp2(mx - m_use);
+    sum *= f;
+    for (int o = sub >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    lse = (all + fast_log2(sum)) * kLn2;
+    f /= sum;
+#pragma unroll
+    for (int i = 0; i < NST; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] *= f;
   }
   if (a.lse && a.lse_fix && vb == 0) {
     float dot = 0.f;
@@ -600,6 +615,11 @@ hipError_t launch_paged_t(const PagedArgs& a, hipStream_t st) {
   else split_kernel<T, 8><<<wgs, 256, 0, st>>>(a, hb);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
+  // all of out's columns in one workgroup where W_v's rows of a head fit in LDS beside another workgroup's
+  // (o is then read once), and by 32 where the launch would be small
+  constexpr int NB = DN / 32;
+  if (sizeof(T) == 2 && NB > 1 && a.d_c <= 512 && (int64_t)a.H * ((a.T + 31) / 32) >= kCus / 2)
+    return launch_join<T, DN, NB>(a, st);
   return launch_join<T, DN, 1>(a, st);
 }
 

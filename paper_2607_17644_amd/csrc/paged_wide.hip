@@ -40,6 +40,28 @@ __device__ __forceinline__ int fresh_lane() {
   asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
   return l;
 }
+// What is the same in every lane, in scalar registers.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const char* uniform(const char* p) {
+  return (const char*)((uintptr_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)p) |
+                       ((uintptr_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uintptr_t)p >> 32)) << 32));
+}
+// Direct copies of 1 KB (common.hpp, g2lds16_so and g2lds16). NT: the data are used by this workgroup alone, and
+// pass the caches by (6.9 against 5.9 TB/s for a pool read once, 334 MB).
+template <bool NT>
+__device__ __forceinline__ void copy_row(const void* at, uint32_t off, void* lds) {
+  const void* base = uniform((const char*)at);
+  if constexpr (!NT) return g2lds16_so(base, off, lds);
+  const uint32_t m = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(m)
+               : "memory", "m0");
+}
+template <bool NT>
+__device__ __forceinline__ void copy_lanes(const void* g, void* lds) {
+  if constexpr (!NT) return g2lds16(g, lds);
+  const uint32_t m = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(g), "s"(m) : "memory", "m0");
+}
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
@@ -49,7 +71,7 @@ __device__ __forceinline__ V lds_at(uint32_t address) {
   return *(__attribute__((address_space(3))) const V*)(uintptr_t)address;
 }
 
-template <int HG>
+template <int HG, bool NT>
 __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_blocks) {
   constexpr int KP = 4 / HG, NS = HG;
   __shared__ __attribute__((aligned(16))) bf16 ring[4 * kTile];
@@ -64,22 +86,22 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
   const int id = blockIdx.x, hb = id / 8 % head_blocks, w = id / (8 * head_blocks) * 8 + id % 8;
   const int h0 = hb * a.heads_per_wg + 32 * hg;
   const int nh = min(32, min(a.H, (hb + 1) * a.heads_per_wg) - h0);  // <= 0: this wave only copies
-  const int per = a.sched[0], total = a.sched[1];
+  const int per = uniform(a.sched[0]), total = uniform(a.sched[1]);
   const int64_t start = (int64_t)w * per;
   if (start >= total) return;
   const int end = (int)min((int64_t)total, start + per);
   const int32_t* before = a.sched + kSchedHeader;
-  int t = before[a.T + 1 + w];
+  int t = uniform(before[a.T + 1 + w]);
   int32_t* win_ids = s_page[wave];
 
   for (int at = (int)start; at < end; ++t) {
-    const int row_first = before[t], row_end = before[t + 1];
+    const int row_first = uniform(before[t]), row_end = uniform(before[t + 1]);
     if (row_end <= at) continue;
     const int it0 = at - row_first, it1 = min(end, row_end) - row_first;
     at = min(end, row_end);
     const RowState rs = row_state(a, t);
-    const int visible = min(rs.visible, it1 * kTileKeys);  // to the end of this share
-    const int32_t* pages = a.table + (int64_t)rs.request * a.width;
+    const int visible = min(uniform(rs.visible), it1 * kTileKeys);  // to the end of this share
+    const int32_t* pages = a.table + (int64_t)uniform(rs.request) * a.width;
 
     bf16x8 qf[kRow / 16], ql[kDr / 16];
     {
@@ -94,45 +116,67 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
     float m = -INFINITY, lsum;
     bool high;
     int win;
-    // this wave's share of the copies of tile `it` into buf; returns its keys with no page
+    auto page_of = [&](int key) { return (int)((uint64_t)(uint32_t)key * a.page_magic >> a.page_shift); };
+    // This wave's share of the copies of tile `it` into buf; returns the tile's keys with no page.
+    // Rows are 1152 bytes apart where the tile lies in one page; else, and in a row's last tile (and with
+    // HG = 1, whose copies wait for memory and not for their addresses), each row's place comes
+    // from the lane of its key.
+    constexpr int NMAIN = kTileKeys / HG, NCOPY = NMAIN + 4 / HG;
     auto fetch = [&](int it, bf16* buf) -> uint32_t {
       const int l = fresh_lane(), n = l & 31;
-      const int k0 = it * kTileKeys, last = (min(k0 + kTileKeys, visible) - 1) / a.page;
-      if (k0 < visible && (win < 0 || last >= win + kPages)) {
-        win = k0 / a.page;
-        const int have = (visible - 1) / a.page + 1;
+      const int k0 = it * kTileKeys, p0 = page_of(k0), o0 = k0 - p0 * a.page;
+      if (k0 < visible && (win < 0 || page_of(min(k0 + kTileKeys, visible) - 1) >= win + kPages)) {
+        win = p0;
+        const int have = page_of(visible - 1) + 1;
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = l; i < kPages; i += 64) win_ids[i] = win + i < have ? pages[win + i] : -1;
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
       }
+      if (HG > 1 && k0 + kTileKeys <= visible && o0 + kTileKeys <= a.page) {
+        const int pid = __builtin_amdgcn_readfirstlane(win_ids[p0 - win]);
+        const bool ok = (unsigned)pid < (unsigned)a.n_pages;
+        const char* base = uniform(ok ? (const char*)((const bf16*)a.cache + (int64_t)pid * a.page_stride + (int64_t)o0 * kRow)
+                                      : (const char*)kZeroRow);
+        const int step = __builtin_amdgcn_readfirstlane(ok ? 2 * kRow : 0);
+#pragma unroll
+        for (int j = 0; j < NMAIN; ++j) {
+          const int r = hg + HG * j;
+          copy_row<NT>(base + r * step, (uint32_t)((l ^ swz<16>(r)) * 16), buf + r * kDc);
+        }
+#pragma unroll
+        for (int j = 0; j < 4 / HG; ++j) {
+          const int i = hg + HG * j, r = l >> 3;  // (rows 8 apart are swizzled by the flip of one bit)
+          copy_row<NT>(base + 8 * i * step + 2 * kDc, r * step + ((l & 7) ^ swz<8>(r) ^ (i & 1)) * 16, buf + kMain + i * 512);
+        }
+        return ok ? 0u : ~0u;
+      }
       const int key = k0 + n;
       const bool live = key < visible;
-      const int pg = live ? key / a.page : win, off = live ? key % a.page : 0;
+      const int pg = live ? page_of(key) : win, off = live ? key - pg * a.page : 0;
       const int pid = win_ids[pg - win];  // (0 of the last window for a tile past the end)
       const bool ok = live && (unsigned)pid < (unsigned)a.n_pages;
       const bf16* src =
           ok ? (const bf16*)a.cache + (int64_t)pid * a.page_stride + (int64_t)off * kRow : (const bf16*)kZeroRow;
       const int lo = (int)(uint32_t)(uintptr_t)src, hi = (int)(uint32_t)((uintptr_t)src >> 32);
 #pragma unroll
-      for (int j = 0; j < kTileKeys / HG; ++j) {
+      for (int j = 0; j < NMAIN; ++j) {
         const int r = hg + HG * j;
         const uintptr_t base = (uintptr_t)(uint32_t)__builtin_amdgcn_readlane(lo, r) |
                                ((uintptr_t)(uint32_t)__builtin_amdgcn_readlane(hi, r) << 32);
-        g2lds16_so((const void*)base, (uint32_t)((l ^ swz<16>(r)) * 16), buf + r * kDc);
+        copy_row<NT>((const void*)base, (uint32_t)((l ^ swz<16>(r)) * 16), buf + r * kDc);
       }
 #pragma unroll
       for (int j = 0; j < 4 / HG; ++j) {
         const int i = hg + HG * j, r = 8 * i + (l >> 3);
-        const uintptr_t base =
-            (uintptr_t)(uint32_t)__shfl(lo, r) | ((uintptr_t)(uint32_t)__shfl(hi, r) << 32);
-        g2lds16((const bf16*)base + kDc + (((l & 7) ^ swz<8>(r)) * 8), buf + kMain + i * 512);
+        const uintptr_t base = (uintptr_t)(uint32_t)__shfl(lo, r) | ((uintptr_t)(uint32_t)__shfl(hi, r) << 32);
+        copy_lanes<NT>((const bf16*)base + kDc + (((l & 7) ^ swz<8>(r)) * 8), buf + kMain + i * 512);
       }
       return (uint32_t)__ballot(live && !ok);
     };
-    // fragments are read three products ahead, in a pinned order
-    constexpr int PF = 3, NQ = kRow / 16, NV = 2 * (kDc / 32);
+    // fragments are read PF (PV) products ahead, in a pinned order
+    constexpr int PF = 5, NQ = kRow / 16, PV = 4, NV = 2 * (kDc / 32);
     // Chunk c of a tile's row r is at c ^ swz<16>(r) (c part; c ^ swz<8>(r) in the band). This lane
     // reads the fragment of contraction step i in row n at (k ^ 32 (i % 8)) + 256 (i / 8), of
     // the band's step i at b ^ 32 i, and for the transposing reads of column block i, rows vr
@@ -206,15 +250,22 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
         for (int e = 0; e < 8; ++e) s[8 * kk + e] -= to_f32(pf[kk][e]);
         pl[kk] = acc_to_frag<bf16>(s, kk);
       }
-      bf16x8 v[PF + 1];
+      // two column blocks at a time, so that no product waits for the one before it
+      bf16x8 v[PV + 2];
 #pragma unroll
-      for (int i = 0; i < PF; ++i) v[i] = v_frag(x, i);
+      for (int i = 0; i < PV; ++i) v[i] = v_frag(x, i);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (i + PF < NV) v[(i + PF) % (PF + 1)] = v_frag(x, i + PF);
-        mma(oacc[i % 16], v[i % (PF + 1)], pf[i / 16]);
-        mma(oacc[i % 16], v[i % (PF + 1)], pl[i / 16]);
+      for (int i = 0; i < NV; i += 2) {
+        if (i + PV < NV) {
+          v[(i + PV) % (PV + 2)] = v_frag(x, i + PV);
+          v[(i + PV + 1) % (PV + 2)] = v_frag(x, i + PV + 1);
+        }
+        const bf16x8 &v0 = v[i % (PV + 2)], &v1 = v[(i + 1) % (PV + 2)];
+        mma(oacc[i % 16], v0, pf[i / 16]);
+        mma(oacc[i % 16 + 1], v1, pf[i / 16]);
+        mma(oacc[i % 16], v0, pl[i / 16]);
+        mma(oacc[i % 16 + 1], v1, pl[i / 16]);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -232,27 +283,24 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
           body(it, buf, bad);
         }
       } else {
-        constexpr int PER = (kTileKeys + 4) / HG;  // copies of a wave per tile
         uint32_t bads[NS];
 #pragma unroll
         for (int i = 0; i < NS; ++i) bads[i] = 0;
 #pragma unroll
-        for (int i = 0; i < NS - 1; ++i)
-          if (i < steps) bads[i] = fetch(it0 + i * KP + kp, ring + (i * KP + kp) * kTile);
+        for (int i = 0; i < NS - 1; ++i) bads[i] = fetch(it0 + i * KP + kp, ring + (i * KP + kp) * kTile);
         int st = 0;
         for (int step = 0; step < steps; ++step) {
           const int it = it0 + step * KP + kp;
-          if (step + 2 < steps && NS >= 4) wait_vmem_le<2 * PER>();
-          else if (step + 1 < steps && NS >= 3) wait_vmem_le<PER>();
-          else wait_vmem();
+          wait_vmem_le<(NS - 2) * NCOPY>();
           lds_barrier();  // every wave's copies of the step's tiles; the stage before is read
-          if (step + NS - 1 < steps)
-            bads[NS - 1] = fetch(it + (NS - 1) * KP, ring + ((st == 0 ? NS - 1 : st - 1) * KP + kp) * kTile);
+          // (past the end the copies are of zeros, into a stage that is not read)
+          bads[NS - 1] = fetch(it + (NS - 1) * KP, ring + ((st == 0 ? NS - 1 : st - 1) * KP + kp) * kTile);
           body(it, ring + (st * KP + kp) * kTile, bads[0]);
 #pragma unroll
           for (int i = 0; i < NS - 1; ++i) bads[i] = bads[i + 1];
           st = st + 1 == NS ? 0 : st + 1;
         }
+        wait_vmem();
       }
     };
     for (bool again = false;; again = true) {
@@ -346,9 +394,10 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
 
 void launch_paged_wide(const PagedArgs& a, int head_blocks, hipStream_t st) {
   const unsigned wgs = (unsigned)(head_blocks * a.workers);
-  if (a.heads_per_wg > 64) wide_kernel<4><<<wgs, 256, 0, st>>>(a, head_blocks);
-  else if (a.heads_per_wg > 32) wide_kernel<2><<<wgs, 256, 0, st>>>(a, head_blocks);
-  else wide_kernel<1><<<wgs, 256, 0, st>>>(a, head_blocks);
+  if (head_blocks > 1) wide_kernel<4, false><<<wgs, 256, 0, st>>>(a, head_blocks);
+  else if (a.heads_per_wg > 64) wide_kernel<4, true><<<wgs, 256, 0, st>>>(a, head_blocks);
+  else if (a.heads_per_wg > 32) wide_kernel<2, true><<<wgs, 256, 0, st>>>(a, head_blocks);
+  else wide_kernel<1, true><<<wgs, 256, 0, st>>>(a, head_blocks);
 }
 
 }  // namespace laga

@@ -53,6 +53,16 @@ int main() {
             }
           }
       }
+  // division by the page size
+  for (int page : {1, 2, 3, 7, 16, 31, 48, 64, 200, 1000, 4096, 65535, 1 << 20, (1 << 29) + 1, 1 << 30}) {
+    uint32_t magic, shift;
+    laga::page_division(page, &magic, &shift);
+    for (int i = 0; i < 20000; ++i) {
+      const long long q = rnd(65536) * 65536ll + rnd(65536), k = i % 3 ? q % 0x7fffffff : q / page % (0x7fffffff / page) * page;
+      for (long long key : {k, k - 1, k + page - 1, 0x7fffffffll - i})
+        if (key >= 0 && key <= 0x7fffffff && (long long)((uint64_t)(uint32_t)key * magic >> shift) != key / page) ++bad;
+    }
+  }
   printf("%lld shares, %lld wrong\n", shares, bad);
   return bad != 0;
 }
