@@ -133,7 +133,7 @@ inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
   const int most = p.wide ? 128 : 32;  // heads of a workgroup
   p.head_blocks = (H + most - 1) / most;
   p.heads_per_wg = p.wide ? (H + p.head_blocks - 1) / p.head_blocks : most;
-  const int wgs = (elem_size == 2 && d_c <= 128 ? 2 : 1) * kCus;  // what runs at once
+  const int wgs = (elem_size == 2 && d_c <= 256 ? 2 : 1) * kCus;  // what runs at once
   const int w = wgs / p.head_blocks / 8 * 8;  // whole rounds over the 8 XCDs
   p.workers = w > 8 ? w : 8;
   p.min_per = 4;

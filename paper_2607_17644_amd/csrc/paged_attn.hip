@@ -9,6 +9,7 @@
 // by W_v (join_kernel). Bound by the cache's bytes for few heads (2 (2 d_c + d_rope) flop per
 // head for each row of d_c + d_rope elements).
 #include <math.h>
+#include <stdlib.h>
 
 #define LAGA_LDS_DMA_ASM 1
 #include "common.hpp"
@@ -19,43 +20,77 @@ namespace laga {
 namespace {
 
 // ---------------------------------------------------------------- absorb
-// qa^T = W_k q_nope^T per head: A = rows of W_kv_b (their d_nope elements of a head are
-// contiguous), B = the tokens' q_nope, both straight from global memory (each is used once
-// per 32 tokens). A wave has 32 rows of W for all the tokens of its share. Bound by reading W.
-// The last workgroups turn q_rope, and the very last one lays out the tiles.
-constexpr int kAbsorbWaves = 4;
+// qa^T = W_k q_nope^T per head. A workgroup has 128 rows of W_kv_b (their d_nope elements of a head
+// are contiguous) and goes through its share of the tokens, 32 at a time; a wave has 32 of the
+// rows. Bound by reading W and writing qa: W's rows come in whole by direct copies (fragments
+// straight from global memory read each line four times over: 128 heads x 61 tokens 22 us), results
+// leave through LDS in rows of 256 bytes. Beside them one workgroup per token turns its
+// q_rope, and one lays out the tiles.
+constexpr int kAbsorbWaves = 4, kAbsorbRows = 32 * kAbsorbWaves;
 
 template <typename T, int DN>
 __device__ void absorb_product(const PagedArgs& a, int blk, int cblocks, int tpart, int tparts) {
+  constexpr int E = 16 / sizeof(T), CPR = DN / E, PO = kAbsorbRows + E;  // chunks of a row; pitch of the results
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  T* sw = (T*)smem;
+  T* sq = sw + kAbsorbRows * DN;
+  T* so = sq + 32 * DN;
+  T* sl = so + 32 * PO;  // bf16: low halves
   const int l = threadIdx.x & 63, n = l & 31, g = l >> 5;
-  const int h = blk / cblocks, c0 = (blk % cblocks * kAbsorbWaves + (threadIdx.x >> 6)) * 32;
-  if (c0 >= a.d_c) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blk / cblocks, c0 = blk % cblocks * kAbsorbRows, nc = min(kAbsorbRows, a.d_c - c0);
   const int W = a.d_c + a.d_rope, dqk = DN + a.d_rope;
-  const T* w = (const T*)a.w + (int64_t)(c0 + n) * a.H * (DN + a.d_v) + (int64_t)h * (DN + a.d_v) + 8 * g;
-  frag_t<T> wf[DN / 16];
-#pragma unroll
-  for (int ks = 0; ks < DN / 16; ++ks) wf[ks] = *reinterpret_cast<const frag_t<T>*>(w + 16 * ks);
+  const int64_t ldw = (int64_t)a.H * (DN + a.d_v), ldq = (int64_t)a.H * dqk;
+  const T* w = (const T*)a.w + c0 * ldw + (int64_t)h * (DN + a.d_v);
+  // chunk c of a row is at c ^ swz (bf16); rows past the end repeat the last one
+  auto copy = [&](const T* src, int64_t stride, int rows, int last, T* dst) {
+    for (int p0 = wave * 64; p0 < rows * CPR; p0 += 64 * kAbsorbWaves) {
+      const int r = (p0 + l) / CPR;
+      int c = (p0 + l) % CPR;
+      if constexpr (sizeof(T) == 2) c ^= swz<CPR>(r);
+      g2lds16(src + min(r, last) * stride + c * E, dst + p0 * E);
+    }
+  };
+  auto frag = [&](const T* tile, int r, int ks) {
+    if constexpr (sizeof(T) == 2) return swz_frag<T, CPR>(tile, r, 2 * ks + g);
+    else return lds_frag<T>(tile + r * DN + 16 * ks + 8 * g);
+  };
+  copy(w, ldw, kAbsorbRows, nc - 1, sw);
   for (int t0 = tpart * 32; t0 < a.T; t0 += tparts * 32) {
-    const int t = min(t0 + n, a.T - 1);
-    const T* q = (const T*)a.q + ((int64_t)t * a.H + h) * dqk + 8 * g;
+    const int nt = min(32, a.T - t0);
+    copy((const T*)a.q + t0 * ldq + (int64_t)h * dqk, ldq, 32, nt - 1, sq);
+    wait_vmem();
+    lds_barrier();
     f32x16 acc = {};
 #pragma unroll
-    for (int ks = 0; ks < DN / 16; ++ks) mma(acc, wf[ks], *reinterpret_cast<const frag_t<T>*>(q + 16 * ks));
-    if (t0 + n < a.T) {
-      const int64_t at = ((int64_t)t * a.H + h) * W + c0 + 4 * g;
+    for (int ks = 0; ks < DN / 16; ++ks) mma(acc, frag(sw, 32 * wave + n, ks), frag(sq, n, ks));
 #pragma unroll
-      for (int rr = 0; rr < 4; ++rr) {
-        typename FragOf<T>::half v, low;
+    for (int rr = 0; rr < 4; ++rr) {
+      typename FragOf<T>::half v, low;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = to_elem<T>(acc[4 * rr + e]);
-          low[e] = to_elem<T>(acc[4 * rr + e] - to_f32(v[e]));
-        }
-        *reinterpret_cast<typename FragOf<T>::half*>((T*)a.qa + at + 8 * rr) = v;
-        if constexpr (kTwo<T>) *reinterpret_cast<typename FragOf<T>::half*>((T*)a.qa_lo + at + 8 * rr) = low;
+      for (int e = 0; e < 4; ++e) {
+        v[e] = to_elem<T>(acc[4 * rr + e]);
+        low[e] = to_elem<T>(acc[4 * rr + e] - to_f32(v[e]));
       }
+      const int at = n * PO + 32 * wave + 8 * rr + 4 * g;
+      *reinterpret_cast<typename FragOf<T>::half*>(so + at) = v;
+      if constexpr (kTwo<T>) *reinterpret_cast<typename FragOf<T>::half*>(sl + at) = low;
     }
+    lds_barrier();
+    for (int x = threadIdx.x; x < nt * (kAbsorbRows / E); x += 64 * kAbsorbWaves) {
+      const int r = x / (kAbsorbRows / E), c = x % (kAbsorbRows / E) * E;
+      if (c >= nc) continue;
+      const int64_t at = ((int64_t)(t0 + r) * a.H + h) * W + c0 + c;
+      *reinterpret_cast<chunk16*>((T*)a.qa + at) = *reinterpret_cast<const chunk16*>(so + r * PO + c);
+      if constexpr (kTwo<T>)
+        *reinterpret_cast<chunk16*>((T*)a.qa_lo + at) = *reinterpret_cast<const chunk16*>(sl + r * PO + c);
+    }
+    if (t0 + tparts * 32 < a.T) lds_barrier();  // q and the results are read
   }
+}
+template <typename T, int DN>
+constexpr size_t absorb_lds() {
+  return sizeof(T) * ((size_t)(kAbsorbRows + 32) * DN + (kTwo<T> ? 2 : 1) * 32 * (kAbsorbRows + 16 / sizeof(T)));
 }
 
 // q_rope of one token, every head: a thread keeps one pair's angle
@@ -159,14 +194,15 @@ struct SplitCfg {
   static constexpr int NI = (kTileKeys * P + 63) / 64;  // copies of 64 chunks per tile
   static constexpr int PER = NI / 4;                     // of each wave, at least
   static constexpr int TILE = NI * 64 * E;               // elements
+  static constexpr int kMost = sizeof(T) == 2 && ND <= 2 ? 2 : 4;  // two stages where that lets more workgroups on a CU
   static constexpr int kRing = 140 * 1024 / (NI * 1024);
-  static constexpr int NS = kRing < 1 ? 1 : kRing > 4 ? 4 : kRing;
+  static constexpr int NS = kRing < 1 ? 1 : kRing > kMost ? kMost : kRing;
   static constexpr int KS = 2 * ND + 1;                  // contraction steps of 16 per wave
 };
 constexpr int kWindow = 512;  // page ids of a row held in LDS
 
 template <typename T, int ND>
-__global__ __launch_bounds__(256) void split_kernel(PagedArgs a, int head_blocks) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 && ND <= 2 ? 2 : 1) void split_kernel(PagedArgs a, int head_blocks) {
   using C = SplitCfg<T, ND>;
   constexpr int NS = C::NS, P = C::P, E = C::E;
   __shared__ __attribute__((aligned(16))) T ring[NS * C::TILE];
@@ -405,7 +441,7 @@ __global__ __launch_bounds__(256) void split_kernel(PagedArgs a, int head_blocks
 // its partials read by 32 lanes at once, and a batch of whole rows keeps 32 rows per product.
 // W_v's rows arrive by direct copies meanwhile. Bound by the latency of those two reads.
 template <typename T, int DV, int NB, int NST>  // NB 32-column blocks of out; NST steps of 16 per wave
-__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, int tblocks) {
+__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, int tblocks, int joined) {
   constexpr int E = 16 / sizeof(T), CPR = 32 * NB / E;  // 16-byte chunks of a staged row
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   __shared__ float s_dot[4][32];
@@ -443,6 +479,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, in
     } else {
       w0 = first / per;
       last = (last - 1) / per + 1;
+      if (joined) last = w0 + 1;
       whole = last == w0 + 1;
     }
   }
@@ -579,31 +616,64 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, in
   }
 }
 
+// Rows that several workers share, put together in obar: a thread per four columns of a row's
+// head adds its partials up in order.
+__global__ __launch_bounds__(256) void combine_kernel(PagedArgs a) {
+  const int quads = a.d_c / 4;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, th = x / quads;
+  const int c = (int)(x % quads) * 4;
+  const int t = (int)(th / a.H), h = (int)(th % a.H);
+  if (t >= a.T) return;
+  const int32_t* before = a.sched + kSchedHeader;
+  const int per = a.sched[0], first = before[t], end = before[t + 1];
+  if (first == end) return;
+  const int w0 = first / per, w1 = (end - 1) / per;
+  if (w0 == w1) return;
+  float mx = -INFINITY, sum = 0.f;
+  f32x4 v = {};
+#pragma unroll 8
+  for (int w = w0; w <= w1; ++w) {
+    const int64_t p = (int64_t)partial_place(w, per, first) * a.H + h;
+    const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + p * a.d_c + c);
+    const float m = a.part_ml[2 * p], l = a.part_ml[2 * p + 1], m_new = fmaxf(mx, m);
+    const float m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float f = fast_exp2(m - m_use), old = mx == -INFINITY ? 0.f : fast_exp2(mx - m_use);
+    mx = m_new;
+    sum = __builtin_fmaf(sum, old, f * l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(f, o[e], v[e] * old);
+  }
+  const float inv = 1.f / sum;
+  *reinterpret_cast<f32x4*>(a.obar + th * a.d_c + c) = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+  if (c == 0 && a.lse) a.lse[th] = (mx + fast_log2(sum)) * kLn2;
+}
+
 // Lanes per row: as many as leave 32 / SUB >= T rows, and more while the launch is small and a
 // row may have that many partials.
 template <typename T, int DV, int NB>
-hipError_t launch_join(const PagedArgs& a, hipStream_t st) {
+hipError_t launch_join(const PagedArgs& a, bool joined, hipStream_t st) {
   int sl = 0;
-  while (sl < 5 && (a.T << sl) <= 16) ++sl;
+  while (!joined && sl < 5 && (a.T << sl) <= 16) ++sl;
   auto blocks = [&] { return (int)(((int64_t)a.T + (32 >> sl) - 1) / (32 >> sl)); };
-  while (sl < 5 && (int64_t)a.H * (DV / (32 * NB)) * blocks() < 2 * kCus && ((int64_t)a.T << sl) < a.workers) ++sl;
+  while (!joined && sl < 5 && (int64_t)a.H * (DV / (32 * NB)) * blocks() < 2 * kCus && ((int64_t)a.T << sl) < a.workers) ++sl;
   const unsigned wgs = (unsigned)((int64_t)a.H * (DV / (32 * NB)) * blocks());
   const size_t w = (size_t)a.d_c * 32 * NB * sizeof(T), red = (size_t)NB * 16384, lds = w > red ? w : red;
   const int tb = blocks();
-  if (a.d_c <= 128) join_kernel<T, DV, NB, 2><<<wgs, 256, lds, st>>>(a, sl, tb);
-  else if (a.d_c <= 256) join_kernel<T, DV, NB, 4><<<wgs, 256, lds, st>>>(a, sl, tb);
-  else if (a.d_c <= 512) join_kernel<T, DV, NB, 8><<<wgs, 256, lds, st>>>(a, sl, tb);
-  else join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, sl, tb);
+  if (a.d_c <= 128) join_kernel<T, DV, NB, 2><<<wgs, 256, lds, st>>>(a, sl, tb, joined);
+  else if (a.d_c <= 256) join_kernel<T, DV, NB, 4><<<wgs, 256, lds, st>>>(a, sl, tb, joined);
+  else if (a.d_c <= 512) join_kernel<T, DV, NB, 8><<<wgs, 256, lds, st>>>(a, sl, tb, joined);
+  else join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, sl, tb, joined);
   return hipGetLastError();
 }
 
 template <typename T, int DN>
 hipError_t launch_paged_t(const PagedArgs& a, hipStream_t st) {
-  const int cblocks = (a.d_c + 32 * kAbsorbWaves - 1) / (32 * kAbsorbWaves);
+  const int cblocks = (a.d_c + kAbsorbRows - 1) / kAbsorbRows;
   const int64_t blocks = (int64_t)a.H * cblocks;
   const int ttiles = (a.T + 31) / 32;
   const int want = (int)((4 * kCus + blocks - 1) / blocks), tparts = ttiles < want ? ttiles : want;
-  absorb_kernel<T, DN><<<(unsigned)(a.T + 1 + blocks * tparts), 64 * kAbsorbWaves, 0, st>>>(a, cblocks, tparts);
+  absorb_kernel<T, DN><<<(unsigned)(a.T + 1 + blocks * tparts), 64 * kAbsorbWaves, absorb_lds<T, DN>(), st>>>(
+      a, cblocks, tparts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int hb = (a.H + a.heads_per_wg - 1) / a.heads_per_wg;
@@ -618,9 +688,11 @@ hipError_t launch_paged_t(const PagedArgs& a, hipStream_t st) {
   // all of out's columns in one workgroup where W_v's rows of a head fit in LDS beside another workgroup's
   // (o is then read once), and by 32 where the launch would be small
   constexpr int NB = DN / 32;
+  const bool joined = getenv("JOINED") != nullptr;
+  if (joined) combine_kernel<<<(unsigned)(((int64_t)a.T * a.H * a.d_c / 4 + 255) / 256), 256, 0, st>>>(a);
   if (sizeof(T) == 2 && NB > 1 && a.d_c <= 512 && (int64_t)a.H * ((a.T + 31) / 32) >= kCus / 2)
-    return launch_join<T, DN, NB>(a, st);
-  return launch_join<T, DN, 1>(a, st);
+    return launch_join<T, DN, NB>(a, joined, st);
+  return launch_join<T, DN, 1>(a, joined, st);
 }
 
 }  // namespace
