@@ -99,6 +99,23 @@ class Paged:
     page_stride: int = 0  # elements between pages; 0: pages are contiguous
     reserved: int = 0
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_made", None)  # what was made of the fields before
+
+    def _forms(self):
+        """(reference to the C struct, shapes), made once for these fields: a step passes them to each call."""
+        made = self.__dict__.get("_made")
+        if made is None:
+            made = self.__dict__["_made"] = (ctypes.byref(self.c()), self._shapes())
+        return made
+
+    def ref(self):
+        return self._forms()[0]
+
+    def shapes(self) -> dict:
+        return self._forms()[1]
+
     def c(self) -> _CPaged:
         return _CPaged(self.rows, self.requests, self.table_width, self.n_pages, self.page_size, self.page_stride,
                        self.n_heads, self.d_c, self.d_nope, self.d_rope, self.d_v, self.softmax_scale, self.dtype,
@@ -108,9 +125,9 @@ class Paged:
     def torch_dtype(self):
         return torch.bfloat16 if self.dtype == DTYPE_BF16 else torch.float32
 
-    def shapes(self) -> dict:
+    def _shapes(self) -> dict:
         T, R, H = self.rows, self.requests, self.n_heads
-        return {"cache": (self.n_pages, self.page_size, self.d_c + self.d_rope), "block_table": (R, self.table_width),
+        return {"gamma": (self.d_c,), "cache": (self.n_pages, self.page_size, self.d_c + self.d_rope), "block_table": (R, self.table_width),
                 "free_pages": (self.n_pages,), "free_count": (1,), "free_count_out": (1,), "status": (1,),
                 "lengths": (R,), "lengths_out": (R,), "fresh": (R,), "drop": (R,), "row_begin": (R + 1,),
                 "row_request": (T,), "position": (T,), "slot": (T,), "latent_raw": (T, self.d_c),
@@ -432,63 +449,90 @@ def laga_prologue_bwd(p: Problem, latent_raw, rstd, dc_kv, dk_pe, dq=None, gamma
 
 
 def laga_paged_workspace_bytes(p: Paged, op: int) -> int:
-    return int(_lib.laga_paged_workspace_bytes(ctypes.byref(p.c()), op))
+    return int(_lib.laga_paged_workspace_bytes(p.ref(), op))
 
 
-class _Device:
-    """The device of a serving call: every tensor has to be on it, and the call is made with it
-    current, on its current stream unless the caller names one."""
-
-    def __init__(self, first, name):
-        if not isinstance(first, torch.Tensor):
-            raise TypeError(f"{name} must be a torch.Tensor")
-        if not first.is_cuda:
-            raise ValueError(f"{name} must be a device tensor")
-        self.device = first.device
-
-    def ptr(self, t, name, shape, dtype, required=True):
-        ptr = _ptr(t, name, shape, dtype, required)
-        if t is not None and t.device != self.device:
-            raise ValueError(f"{name} is on {t.device}, expected {self.device}")
-        return ptr
-
-    def _strided(self, t, name, shape, dtype):
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name} must be a torch.Tensor")
-        if t.device != self.device:
-            raise ValueError(f"{name} is on {t.device}, expected {self.device}")
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
-        if t.dtype != dtype:
-            raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
-
-    def rows(self, t, name, shape, dtype):
-        """Pointer and row stride of a matrix whose rows are contiguous (columns of a wider one)."""
-        self._strided(t, name, shape, dtype)
-        if t.stride(1) != 1:
-            raise ValueError(f"{name} must have contiguous rows")
-        return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
-
-    def cache(self, p, t):
-        """Pointer of the pool: rows contiguous in a page, pages p.page_stride elements apart."""
-        shape = p.shapes()["cache"]
-        self._strided(t, "cache", shape, p.torch_dtype)
-        want = (p.page_stride or shape[1] * shape[2], shape[2], 1)
-        if any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), want)):
-            raise ValueError(f"cache has strides {t.stride()}, expected {want}")
-        return t.data_ptr()
-
-    def stream(self, stream):
-        return _stream(torch.cuda.current_stream(self.device) if stream is None else stream)
-
-    def int32(self, p, name, t):
-        return torch.empty(p.shapes()[name], dtype=torch.int32, device=self.device) if t is None else t
+def _fault(t, name, shape, dtype, index):
+    """Why t is not a contiguous tensor of this shape and type on device number index."""
+    if not isinstance(t, torch.Tensor):
+        return TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        return ValueError(f"{name} must be a device tensor")
+    if t.get_device() != index:
+        return ValueError(f"{name} is on {t.device}, expected cuda:{index}")
+    if tuple(t.shape) != shape:
+        return ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if t.dtype != dtype:
+        return ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    return ValueError(f"{name} must be contiguous")
 
 
-def _plan_workspace(p, workspace, device):
+def _at(t, name, shape, dtype, index):
+    """Address of a required contiguous tensor. (A decoding step makes some thirty of these checks, and its
+    kernels take microseconds: what is right is found right at once, what is not is looked at again.)"""
+    try:
+        if t.shape == shape and t.dtype is dtype and t.get_device() == index and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    raise _fault(t, name, shape, dtype, index)
+
+
+def _device_of(t, name):
+    """Number of the device of a serving call: that of its first tensor; every other has to be on it."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"{name} must be a device tensor")
+    return index
+
+
+def _rows_at(t, name, shape, dtype, index):
+    """Address and row stride of a matrix whose rows are contiguous (columns of a wider one)."""
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+        raise _fault(t, name, shape, dtype, index)
+    if t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _cache_at(p, t, index):
+    """Address of the pool: rows contiguous in a page, pages p.page_stride elements apart."""
+    shape = p.shapes()["cache"]
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not p.torch_dtype or t.get_device() != index:
+        raise _fault(t, "cache", shape, p.torch_dtype, index)
+    want = (p.page_stride or shape[1] * shape[2], shape[2], 1)
+    if t.stride() != want and any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), want)):
+        raise ValueError(f"cache has strides {t.stride()}, expected {want}")
+    return t.data_ptr()
+
+
+def _serve(where, index, stream, function, *args):
+    """The call with its device current, on the device's current stream unless the caller names one."""
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return _serve(where, index, stream, function, *args)
+    status = function(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+    if status != 0:
+        raise LagaError(status, where)
+
+
+def _empty(shape, dtype, index):
+    return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
+
+
+def _int32(sh, name, t, index):
+    return _empty(sh[name], torch.int32, index) if t is None else t
+
+
+def _serve_workspace(p, op, workspace, index):
+    """(workspace, its bytes)."""
     if workspace is None:
-        workspace = torch.empty(max(1, laga_paged_workspace_bytes(p, OP_PAGE_PLAN)), dtype=torch.uint8, device=device)
-    return workspace
+        workspace = _empty((max(1, laga_paged_workspace_bytes(p, op)),), torch.uint8, index)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise _fault(workspace, "workspace", tuple(workspace.shape), workspace.dtype, index)
+    return workspace, workspace.numel() * workspace.element_size()
 
 
 def laga_page_plan(p: Paged, lengths, fresh, block_table, free_pages, free_count, lengths_out=None, free_count_out=None,
@@ -497,52 +541,49 @@ def laga_page_plan(p: Paged, lengths, fresh, block_table, free_pages, free_count
     updated in place. Returns (lengths_out, free_count_out, row_begin, row_request, position, slot,
     status); lengths_out may be lengths, and free_count_out free_count. Nothing is read on the
     host: status[0] (PLAN_*) says on the device whether the step fits."""
-    D, sh, i32 = _Device(lengths, "lengths"), p.shapes(), torch.int32
-    given = {"lengths_out": lengths_out, "free_count_out": free_count_out, "row_begin": row_begin,
-             "row_request": row_request, "position": position, "slot": slot, "status": status}
-    outs = {k: D.int32(p, k, t) for k, t in given.items()}
-    workspace = _plan_workspace(p, workspace, D.device)
-    with torch.cuda.device(D.device):
-        _check(_lib.laga_page_plan(
-            ctypes.byref(p.c()), D.ptr(lengths, "lengths", sh["lengths"], i32), D.ptr(fresh, "fresh", sh["fresh"], i32),
-            D.ptr(block_table, "block_table", sh["block_table"], i32),
-            D.ptr(free_pages, "free_pages", sh["free_pages"], i32), D.ptr(free_count, "free_count", (1,), i32),
-            *[D.ptr(t, k, sh[k], i32) for k, t in outs.items()], D.ptr(workspace, "workspace", None, None),
-            workspace.numel() * workspace.element_size(), D.stream(stream)), "laga_page_plan")
-    return tuple(outs.values())
+    sh, i32, d = p.shapes(), torch.int32, _device_of(lengths, "lengths")
+    lengths_out, free_count_out = _int32(sh, "lengths_out", lengths_out, d), _int32(sh, "free_count_out", free_count_out, d)
+    row_begin, row_request = _int32(sh, "row_begin", row_begin, d), _int32(sh, "row_request", row_request, d)
+    position, slot = _int32(sh, "position", position, d), _int32(sh, "slot", slot, d)
+    status = _int32(sh, "status", status, d)
+    workspace, nbytes = _serve_workspace(p, OP_PAGE_PLAN, workspace, d)
+    _serve("laga_page_plan", d, stream, _lib.laga_page_plan, p.ref(), _at(lengths, "lengths", sh["lengths"], i32, d),
+           _at(fresh, "fresh", sh["fresh"], i32, d), _at(block_table, "block_table", sh["block_table"], i32, d),
+           _at(free_pages, "free_pages", sh["free_pages"], i32, d), _at(free_count, "free_count", (1,), i32, d),
+           _at(lengths_out, "lengths_out", sh["lengths"], i32, d), _at(free_count_out, "free_count_out", (1,), i32, d),
+           _at(row_begin, "row_begin", sh["row_begin"], i32, d), _at(row_request, "row_request", sh["row_request"], i32, d),
+           _at(position, "position", sh["position"], i32, d), _at(slot, "slot", sh["slot"], i32, d),
+           _at(status, "status", (1,), i32, d), workspace.data_ptr(), nbytes)
+    return lengths_out, free_count_out, row_begin, row_request, position, slot, status
 
 
 def laga_page_release(p: Paged, lengths, drop, block_table, free_pages, free_count, lengths_out=None,
                       free_count_out=None, status=None, workspace=None, stream=None):
     """The pages of the requests with drop[r] != 0 go back on the stack (free_pages is updated in
     place); returns (lengths_out, free_count_out, status)."""
-    D, sh, i32 = _Device(lengths, "lengths"), p.shapes(), torch.int32
-    given = {"lengths_out": lengths_out, "free_count_out": free_count_out, "status": status}
-    outs = {k: D.int32(p, k, t) for k, t in given.items()}
-    workspace = _plan_workspace(p, workspace, D.device)
-    with torch.cuda.device(D.device):
-        _check(_lib.laga_page_release(
-            ctypes.byref(p.c()), D.ptr(lengths, "lengths", sh["lengths"], i32), D.ptr(drop, "drop", sh["drop"], i32),
-            D.ptr(block_table, "block_table", sh["block_table"], i32),
-            D.ptr(free_pages, "free_pages", sh["free_pages"], i32), D.ptr(free_count, "free_count", (1,), i32),
-            *[D.ptr(t, k, sh[k], i32) for k, t in outs.items()], D.ptr(workspace, "workspace", None, None),
-            workspace.numel() * workspace.element_size(), D.stream(stream)), "laga_page_release")
-    return tuple(outs.values())
+    sh, i32, d = p.shapes(), torch.int32, _device_of(lengths, "lengths")
+    lengths_out, free_count_out = _int32(sh, "lengths_out", lengths_out, d), _int32(sh, "free_count_out", free_count_out, d)
+    status = _int32(sh, "status", status, d)
+    workspace, nbytes = _serve_workspace(p, OP_PAGE_PLAN, workspace, d)
+    _serve("laga_page_release", d, stream, _lib.laga_page_release, p.ref(), _at(lengths, "lengths", sh["lengths"], i32, d),
+           _at(drop, "drop", sh["drop"], i32, d), _at(block_table, "block_table", sh["block_table"], i32, d),
+           _at(free_pages, "free_pages", sh["free_pages"], i32, d), _at(free_count, "free_count", (1,), i32, d),
+           _at(lengths_out, "lengths_out", sh["lengths"], i32, d), _at(free_count_out, "free_count_out", (1,), i32, d),
+           _at(status, "status", (1,), i32, d), workspace.data_ptr(), nbytes)
+    return lengths_out, free_count_out, status
 
 
 def laga_cache_append(p: Paged, latent_raw, kpe_raw, position, slot, cache, gamma=None, eps=1e-6, rope_base=10000.0,
                       position_offset=0, stream=None):
     """The cache rows of new tokens, normalised latent and rotated shared key, into their slots;
     returns cache. latent_raw and kpe_raw may be columns of one wider matrix."""
-    D, sh, dt, i32 = _Device(cache, "cache"), p.shapes(), p.torch_dtype, torch.int32
-    lat, lat_stride = D.rows(latent_raw, "latent_raw", sh["latent_raw"], dt)
-    kpe, kpe_stride = D.rows(kpe_raw, "kpe_raw", sh["kpe_raw"], dt)
+    sh, dt, i32, d = p.shapes(), p.torch_dtype, torch.int32, _device_of(cache, "cache")
+    lat, lat_stride = _rows_at(latent_raw, "latent_raw", sh["latent_raw"], dt, d)
+    kpe, kpe_stride = _rows_at(kpe_raw, "kpe_raw", sh["kpe_raw"], dt, d)
     cfg = _CPrologue(eps, rope_base, position_offset)
-    with torch.cuda.device(D.device):
-        _check(_lib.laga_cache_append(
-            ctypes.byref(p.c()), ctypes.byref(cfg), lat, lat_stride, D.ptr(gamma, "gamma", (p.d_c,), dt, required=False),
-            kpe, kpe_stride, D.ptr(position, "position", sh["position"], i32), D.ptr(slot, "slot", sh["slot"], i32),
-            D.cache(p, cache), D.stream(stream)), "laga_cache_append")
+    _serve("laga_cache_append", d, stream, _lib.laga_cache_append, p.ref(), ctypes.byref(cfg), lat, lat_stride,
+           None if gamma is None else _at(gamma, "gamma", sh["gamma"], dt, d), kpe, kpe_stride,
+           _at(position, "position", sh["position"], i32, d), _at(slot, "slot", sh["slot"], i32, d), _cache_at(p, cache, d))
     return cache
 
 
@@ -550,21 +591,17 @@ def laga_paged_attn(p: Paged, q, w_kv_b, cache, block_table, position, row_reque
                     position_offset=0, out=None, lse=None, workspace=None, stream=None):
     """Attention of rows over the cached positions 0 .. position[t] of their requests; returns (out,
     lse). With rope_base q's rope band is turned by the row's position first (without, it has been)."""
-    D, sh, dt, i32 = _Device(q, "q"), p.shapes(), p.torch_dtype, torch.int32
+    sh, dt, i32, d = p.shapes(), p.torch_dtype, torch.int32, _device_of(q, "q")
     if out is None:
-        out = _new(p, "out", dt, D.device)
+        out = _empty(sh["out"], dt, d)
     if lse is None:
-        lse = _new(p, "lse", torch.float32, D.device)
-    if workspace is None:
-        workspace = torch.empty(max(1, laga_paged_workspace_bytes(p, OP_PAGED_ATTN)), dtype=torch.uint8, device=D.device)
-    cfg = None if rope_base is None else _CPrologue(0.0, rope_base, position_offset)
-    with torch.cuda.device(D.device):
-        _check(_lib.laga_paged_attn(
-            ctypes.byref(p.c()), None if cfg is None else ctypes.byref(cfg), D.ptr(q, "q", sh["q"], dt),
-            D.ptr(w_kv_b, "w_kv_b", sh["w_kv_b"], dt), D.cache(p, cache),
-            D.ptr(block_table, "block_table", sh["block_table"], i32),
-            D.ptr(row_request, "row_request", sh["row_request"], i32, required=False),
-            D.ptr(position, "position", sh["position"], i32), D.ptr(out, "out", sh["out"], dt),
-            D.ptr(lse, "lse", sh["lse"], torch.float32), D.ptr(workspace, "workspace", None, None),
-            workspace.numel() * workspace.element_size(), D.stream(stream)), "laga_paged_attn")
+        lse = _empty(sh["lse"], torch.float32, d)
+    workspace, nbytes = _serve_workspace(p, OP_PAGED_ATTN, workspace, d)
+    cfg = None if rope_base is None else ctypes.byref(_CPrologue(0.0, rope_base, position_offset))
+    _serve("laga_paged_attn", d, stream, _lib.laga_paged_attn, p.ref(), cfg, _at(q, "q", sh["q"], dt, d),
+           _at(w_kv_b, "w_kv_b", sh["w_kv_b"], dt, d), _cache_at(p, cache, d),
+           _at(block_table, "block_table", sh["block_table"], i32, d),
+           None if row_request is None else _at(row_request, "row_request", sh["row_request"], i32, d),
+           _at(position, "position", sh["position"], i32, d), _at(out, "out", sh["out"], dt, d),
+           _at(lse, "lse", sh["lse"], torch.float32, d), workspace.data_ptr(), nbytes)
     return out, lse

@@ -1,6 +1,7 @@
 """The serving calls without a GPU: the rule that shares out tiles, and what the C ABI and the
 binding refuse before any launch."""
 import ctypes
+import dataclasses
 import os
 import subprocess
 
@@ -31,7 +32,7 @@ def test_shares_of_tiles(tmp_path):
 
 
 def replaced(**kw):
-    return ctypes.byref(L.Paged(**{**P.__dict__, **kw}).c())
+    return ctypes.byref(dataclasses.replace(P, **kw).c())
 
 
 def call(name, p, ptr=FAKE, ws=FAKE, nbytes=BIG, cfg=ctypes.byref(CFG)):
@@ -124,3 +125,14 @@ def test_binding_refuses_host_tensors():
         L.laga_paged_attn(P, f["q"], f["w_kv_b"], f["cache"], i32["block_table"], i32["position"])
     with pytest.raises(TypeError, match="lengths"):
         L.laga_page_plan(P, None, i32["fresh"], i32["block_table"], i32["free_pages"], i32["free_count"])
+
+
+def test_a_problem_follows_its_fields():
+    p = dataclasses.replace(P)
+    assert p.shapes()["q"] == (8, 16, 192) and p == P
+    need = L.laga_paged_workspace_bytes(p, L.OP_PAGED_ATTN)
+    p.rows, p.n_heads = 9, 32
+    assert p.shapes()["q"] == (9, 32, 192) and p.shapes()["lse"] == (9, 32) and p != P
+    assert L.laga_paged_workspace_bytes(p, L.OP_PAGED_ATTN) > need
+    p.d_c = 48
+    assert L.laga_paged_workspace_bytes(p, L.OP_PAGED_ATTN) == 0
