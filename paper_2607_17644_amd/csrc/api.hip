@@ -206,7 +206,7 @@ PagedWs paged_layout(const laga_paged_t* p, const PagedDims& d, const PagedPlan&
   PagedWs w{};
   const size_t rows = (size_t)d.T * d.H, places = (size_t)2 * plan.workers * d.H;
   size_t off = 0;
-  w.sched = off; off += round_up(sizeof(int32_t) * ((size_t)kSchedHeader + d.T + 1 + plan.workers));
+  w.sched = off; off += round_up(sizeof(int32_t) * sched_ints(d.T, plan.workers));
   w.qa = off; off += round_up(elem_size(p) * rows * (d.d_c + d.dr));
   w.qa_lo = off; off += p->dtype == LAGA_DTYPE_BF16 ? round_up(elem_size(p) * rows * (d.d_c + d.dr)) : 0;
   w.obar = off; off += round_up(sizeof(float) * rows * d.d_c);
@@ -398,7 +398,7 @@ laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg,
   }
   a.sched = (int32_t*)(wsb + ws.sched); a.qa = wsb + ws.qa; a.qa_lo = wsb + ws.qa_lo; a.obar = (float*)(wsb + ws.obar);
   a.part_o = (float*)(wsb + ws.part_o); a.part_ml = (float*)(wsb + ws.part_ml);
-  a.lse_fix = plan.wide; a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.min_per = plan.min_per;
+  a.lse_fix = plan.wide; a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.min_per = plan.min_per; a.groups = plan.groups;
   hipStream_t st = (hipStream_t)stream;
   return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_paged_attn<bf16>(a, st) : launch_paged_attn<float>(a, st));
 }

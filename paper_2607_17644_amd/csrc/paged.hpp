@@ -88,7 +88,7 @@ struct PagedArgs {
   int rotate;        // 1: q_rope is turned by its row's position first
   double log2_base;
   // workspace
-  int32_t* sched;    // [per, total] then tiles_before[T + 1] and first_row[workers]
+  int32_t* sched;    // layout of the tiles (sched_ints)
   void* qa;          // [T][H][d_c + d_rope]: W_k q_nope, then q_rope
   void* qa_lo;       // bf16: what qa's rounding left, rounded
   float* obar;       // [T][H][d_c]: normalised rows that one worker took whole
@@ -98,14 +98,33 @@ struct PagedArgs {
   int heads_per_wg;  // heads of a head block
   int workers;       // of each head block
   int min_per;       // fewest tiles that a worker takes
+  int groups;        // of 32 heads in heads_per_wg (wide kernel), or 0
 };
-constexpr int kSchedHeader = 4;
+// Layout of the tiles: [tiles per worker, tiles, groups, -], tiles before each row [T + 1], and of
+// each worker's first share (kShareInts) the row, its first tile and end, request and visible keys.
+constexpr int kSchedHeader = 4, kShareInts = 8;
+__host__ __device__ inline int64_t sched_shares(int64_t T) { return (kSchedHeader + T + 1 + 7) / 8 * 8; }
+inline size_t sched_ints(long long T, int workers) { return (size_t)sched_shares(T) + (size_t)kShareInts * workers; }
 
 __host__ __device__ inline int tiles_of(int visible) { return (visible + kTileKeys - 1) / kTileKeys; }
 // Tiles per worker: even shares, and no fewer than min_per.
 __host__ __device__ inline int tiles_per_worker(int total, int workers, int min_per) {
   const int even = (int)(((int64_t)total + workers - 1) / workers);
   return even > min_per ? even : min_per;
+}
+// How the wide kernel's workgroups go about their tiles. With few, a workgroup takes 32 of its
+// heads (groups of them: one after the other on the workgroups of an XCD) and its four waves share each
+// tile; a tile is then done in a third of the time, and no parts of waves have to meet at
+// the end. groups 0: the wide way.
+constexpr int kFewTiles = 8;  // tiles of a worker
+struct Shares { int per, workers, groups; };
+__host__ __device__ inline Shares shares_of(int total, int workers, int min_per, int groups) {
+  const int few = groups > 0 ? workers / (8 * groups) * 8 : 0;
+  if (few > 0) {
+    const int per = tiles_per_worker(total, few, 1);
+    if (per <= kFewTiles) return {per, few, groups};
+  }
+  return {tiles_per_worker(total, workers, min_per), workers, 0};
 }
 // The partial place of worker w's share of the row whose tiles begin at row_first: a row that
 // was begun before the worker's range (or with it) is its first, any other its last.
@@ -125,7 +144,7 @@ inline void page_division(int page, uint32_t* magic, uint32_t* shift) {
 
 struct PagedPlan {
   bool wide;  // paged_wide.hip: bf16 with d_c = 512 and d_rope = 64
-  int heads_per_wg, head_blocks, workers, min_per;
+  int heads_per_wg, head_blocks, workers, min_per, groups;
 };
 inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
   PagedPlan p;
@@ -136,7 +155,8 @@ inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
   const int wgs = (elem_size == 2 && d_c <= 256 ? 2 : 1) * kCus;  // what runs at once
   const int w = wgs / p.head_blocks / 8 * 8;  // whole rounds over the 8 XCDs
   p.workers = w > 8 ? w : 8;
-  p.min_per = 4;
+  p.groups = p.wide ? (p.heads_per_wg + 31) / 32 : 0;
+  p.min_per = 1;
   return p;
 }
 

@@ -27,6 +27,31 @@ __device__ __forceinline__ RowState row_state(const PagedArgs& a, int t) {
   return {r, p + 1, false};
 }
 
+// What is the same in every lane, in scalar registers.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const char* uniform(const char* p) {
+  return (const char*)((uintptr_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)p) |
+                       ((uintptr_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uintptr_t)p >> 32)) << 32));
+}
+
+// A row that a worker has a share of: its tiles, its request and what it sees of it.
+struct Share {
+  int t, first, end, request, visible;
+};
+// where worker w's tiles begin
+__device__ __forceinline__ Share first_share(const PagedArgs& a, int w) {
+  const int32_t* s = a.sched + sched_shares(a.T) + (int64_t)w * kShareInts;
+  return {uniform(s[0]), uniform(s[1]), uniform(s[2]), uniform(s[3]), uniform(s[4])};
+}
+// the row after t that has tile at (the end of t's)
+__device__ __forceinline__ Share next_share(const PagedArgs& a, int t, int at) {
+  const int32_t* before = a.sched + kSchedHeader;
+  int end;
+  do ++t; while ((end = uniform(before[t + 1])) <= at);
+  const RowState rs = row_state(a, t);
+  return {t, at, end, uniform(rs.request), uniform(rs.visible)};
+}
+
 // Rows that are not read are copied from here (the widest row and its padding).
 static __device__ const __attribute__((aligned(16))) unsigned char kZeroRow[4608] = {};
 

@@ -2,7 +2,7 @@
 // heads over the whole row, so every byte of a tile that it reads from LDS feeds 32 heads and
 // no partial scores cross waves. (paged_attn.hip has the form for any width.)
 #define LAGA_LDS_DMA_ASM 1
-#include "paged_dev.hpp"
+#include "paged_split.hpp"
 
 namespace laga {
 namespace {
@@ -40,12 +40,6 @@ __device__ __forceinline__ int fresh_lane() {
   asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
   return l;
 }
-// What is the same in every lane, in scalar registers.
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ const char* uniform(const char* p) {
-  return (const char*)((uintptr_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)p) |
-                       ((uintptr_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uintptr_t)p >> 32)) << 32));
-}
 // Direct copies of 1 KB (common.hpp, g2lds16_so and g2lds16). NT: the data are used by this workgroup alone, and
 // pass the caches by (6.9 against 5.9 TB/s for a pool read once, 334 MB).
 template <bool NT>
@@ -75,6 +69,7 @@ template <int HG, bool NT>
 __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_blocks) {
   constexpr int KP = 4 / HG, NS = HG;
   __shared__ __attribute__((aligned(16))) bf16 ring[4 * kTile];
+  static_assert(SplitCfg<bf16, 4>::LDS <= (int)sizeof(ring), "the general form's LDS");
   __shared__ int32_t s_page[4][kPages];
   __shared__ float s_m[4][32], s_l[4][32];
   __shared__ int s_high[4];
@@ -84,24 +79,27 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
   const int hg = wave % HG, kp = wave / HG;
   // the head blocks of a worker follow each other on one XCD: its L2 serves all but the first
   const int id = blockIdx.x, hb = id / 8 % head_blocks, w = id / (8 * head_blocks) * 8 + id % 8;
-  const int h0 = hb * a.heads_per_wg + 32 * hg;
-  const int nh = min(32, min(a.H, (hb + 1) * a.heads_per_wg) - h0);  // <= 0: this wave only copies
-  const int per = uniform(a.sched[0]), total = uniform(a.sched[1]);
+  const int per = uniform(a.sched[0]), total = uniform(a.sched[1]), groups = uniform(a.sched[2]);
+  const int hb0 = hb * a.heads_per_wg, hb1 = min(a.H, hb0 + a.heads_per_wg);
+  if (groups > 0) {  // few tiles
+    const int hf = hb0 + 32 * (w / 8 % groups);
+    if (w / (8 * groups) < a.workers / (8 * groups) && hf < hb1)
+      split_shares<bf16, 4>(a, (unsigned char*)ring, w / (8 * groups) * 8 + w % 8, hf, min(32, hb1 - hf), per, total);
+    return;
+  }
+  const int h0 = hb0 + 32 * hg, nh = min(32, hb1 - h0);  // nh <= 0: this wave only copies
   const int64_t start = (int64_t)w * per;
   if (start >= total) return;
   const int end = (int)min((int64_t)total, start + per);
-  const int32_t* before = a.sched + kSchedHeader;
-  int t = uniform(before[a.T + 1 + w]);
   int32_t* win_ids = s_page[wave];
 
-  for (int at = (int)start; at < end; ++t) {
-    const int row_first = uniform(before[t]), row_end = uniform(before[t + 1]);
-    if (row_end <= at) continue;
+  Share share = first_share(a, w);
+  for (int at = (int)start;;) {
+    const int t = share.t, row_first = share.first, row_end = share.end;
     const int it0 = at - row_first, it1 = min(end, row_end) - row_first;
     at = min(end, row_end);
-    const RowState rs = row_state(a, t);
-    const int visible = min(uniform(rs.visible), it1 * kTileKeys);  // to the end of this share
-    const int32_t* pages = a.table + (int64_t)uniform(rs.request) * a.width;
+    const int visible = min(share.visible, it1 * kTileKeys);  // to the end of this share
+    const int32_t* pages = a.table + (int64_t)share.request * a.width;
 
     bf16x8 qf[kRow / 16], ql[kDr / 16];
     {
@@ -387,6 +385,8 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
         a.lse[(int64_t)t * a.H + h] = (m + fast_log2(ltot)) * kLn2;
       }
     }
+    if (at >= end) return;
+    share = next_share(a, t, at);
   }
 }
 

@@ -25,11 +25,15 @@ int main() {
               const int visible = rnd(4) == 0 ? 0 : longest ? (int)rnd(32 * longest) + 1 : 0;
               before[t + 1] = before[t] + laga::tiles_of(visible);
             }
-            const int total = (int)before[rows], per = laga::tiles_per_worker(total, p.workers, p.min_per);
-            if ((long long)per * p.workers < total) ++bad;
+            const int total = (int)before[rows];
+            const laga::Shares sh = laga::shares_of(total, p.workers, p.min_per, p.groups);
+            const int per = sh.per;
+            if ((long long)per * sh.workers < total || per < 1 || sh.workers > p.workers || sh.workers % 8) ++bad;
+            // with few tiles every group of heads has its workers among the workgroups
+            if (sh.groups && (sh.groups * 32 < p.heads_per_wg || sh.workers * sh.groups > p.workers)) ++bad;
             std::vector<int> place(2 * p.workers, -1), partials(rows, 0);
             long long done = 0;
-            for (int w = 0; w < p.workers; ++w) {
+            for (int w = 0; w < sh.workers; ++w) {
               const long long start = (long long)w * per, end = start + per < total ? start + per : total;
               for (int t = 0; t < rows; ++t) {
                 const long long a = before[t] > start ? before[t] : start, b = before[t + 1] < end ? before[t + 1] : end;
