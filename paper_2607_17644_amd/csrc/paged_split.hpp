@@ -53,6 +53,24 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
   const int end = (int)min((int64_t)total, start + per);
   Share share = first_share(a, w);
 
+  // copy j's lane: chunk c of the tile's row; and its place in a tile whose rows follow each other
+  constexpr int NJ = (C::NI + 3) / 4;
+  constexpr uint32_t kNoPlace = ~0u;
+  auto chunk_of = [&](int j, int& row, int& c) {
+    const int p = j * 64 + l;
+    row = p / P;
+    c = p - row * P;
+    if (C::NI * 64 > kTileKeys * P && row >= kTileKeys) row = 0, c = 0;
+    if constexpr (sizeof(T) == 2) c ^= swz<24>(row);
+  };
+  uint32_t place[NJ];
+#pragma unroll
+  for (int jj = 0; jj < NJ; ++jj) {
+    int row, c;
+    chunk_of(wave + 4 * jj, row, c);
+    place[jj] = c * E < W ? (uint32_t)(row * W * (int)sizeof(T) + c * 16) : kNoPlace;
+  }
+
   for (int at = (int)start;;) {
     const int t = share.t, row_first = share.first, row_end = share.end;
     const int it0 = at - row_first, it1 = min(end, row_end) - row_first;
@@ -84,13 +102,26 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
     auto page_of = [&](int key) { return (int)((uint64_t)(uint32_t)key * a.page_magic >> a.page_shift); };
     // copies of tile `it` into stage st, after a barrier that freed it
     auto fetch = [&](int it, int st) {
-      const int k0 = it * kTileKeys, last = page_of(min(k0 + kTileKeys, rs.visible) - 1);
-      if (win < 0 || last >= win + kWindow) {  // the same for every thread
+      const int k0 = it * kTileKeys, p0 = page_of(k0), o0 = k0 - p0 * a.page;
+      if (win < 0 || page_of(min(k0 + kTileKeys, rs.visible) - 1) >= win + kWindow) {  // the same for every thread
         lds_barrier();
-        win = page_of(k0);
+        win = p0;
         const int have = page_of(rs.visible - 1) + 1;
         for (int i = threadIdx.x; i < kWindow; i += 256) s_page[i] = win + i < have ? pages[win + i] : -1;
         lds_barrier();
+      }
+      // a tile that lies in one page: rows follow each other, places relative to the tile's are known
+      const int pid0 = uniform(s_page[p0 - win]);
+      if (k0 + kTileKeys <= rs.visible && o0 + kTileKeys <= a.page && (unsigned)pid0 < (unsigned)a.n_pages) {
+        const char* base = (const char*)((const T*)a.cache + (int64_t)pid0 * a.page_stride + (int64_t)o0 * W);
+        if (threadIdx.x == 0) s_bad[st] = 0;
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) {
+          const int j = wave + 4 * jj;
+          if (C::NI % 4 == 0 || j < C::NI)
+            g2lds16(place[jj] == kNoPlace ? (const char*)kZeroRow : base + place[jj], ring + st * C::TILE + j * 64 * E);
+        }
+        return;
       }
       const int key = k0 + n;
       const bool live = key < rs.visible;
@@ -102,13 +133,11 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
       if (threadIdx.x == 0) s_bad[st] = bad;
       const uint32_t lo = (uint32_t)(uintptr_t)src, hi = (uint32_t)((uintptr_t)src >> 32);
 #pragma unroll
-      for (int jj = 0; jj < (C::NI + 3) / 4; ++jj) {
+      for (int jj = 0; jj < NJ; ++jj) {
         const int j = wave + 4 * jj;
         if (C::NI % 4 == 0 || j < C::NI) {
-          const int p = j * 64 + l;
-          int row = p / P, c = p - row * P;
-          if (C::NI * 64 > kTileKeys * P && row >= kTileKeys) row = 0, c = 0;
-          if constexpr (sizeof(T) == 2) c ^= swz<24>(row);
+          int row, c;
+          chunk_of(j, row, c);
           const uintptr_t base = (uintptr_t)(uint32_t)__shfl((int)lo, row) |
                                  ((uintptr_t)(uint32_t)__shfl((int)hi, row) << 32);
           const unsigned char* from = c * E < W ? (const unsigned char*)base : kZeroRow;
@@ -142,14 +171,21 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
       const T* tile = ring + st * C::TILE;
 
       f32x16 s = {};
+      constexpr int KB = C::KS < 9 ? C::KS : 9;  // K fragments in flight
+      frag_t<T> k[KB];
+      auto k_frag = [&](int i) {
+        const int ks = wave + 4 * i;
+        if constexpr (sizeof(T) == 2) return *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + (((2 * ks + g) ^ swz<24>(n)) * E));
+        else return *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + 16 * ks + 8 * g);
+      };
+#pragma unroll
+      for (int i = 0; i < KB; ++i) k[i] = k_frag(i);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < C::KS; ++i) {
-        const int ks = wave + 4 * i;
-        frag_t<T> k;
-        if constexpr (sizeof(T) == 2) k = *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + (((2 * ks + g) ^ swz<24>(n)) * E));
-        else k = *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + 16 * ks + 8 * g);
-        mma(s, k, qf[i]);
-        if constexpr (kTwo<T>) mma(s, k, ql[i]);
+        mma(s, k[i % KB], qf[i]);
+        if constexpr (kTwo<T>) mma(s, k[i % KB], ql[i]);
+        if (i + KB < C::KS) k[i % KB] = k_frag(i + KB);
       }
 #pragma unroll
       for (int rr = 0; rr < 4; ++rr)
