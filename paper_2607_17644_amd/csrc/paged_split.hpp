@@ -100,8 +100,21 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
 
     int win = -1;  // first page of the window
     auto page_of = [&](int key) { return (int)((uint64_t)(uint32_t)key * a.page_magic >> a.page_shift); };
-    // copies of tile `it` into stage st, after a barrier that freed it
-    auto fetch = [&](int it, int st) {
+    // copies of tile `it` into stage st, after a barrier that freed it; of a tile in one page the
+    // copies are only made ready, and issued in kSlots parts (at_once: here)
+    const char* flat = nullptr;
+    T* flat_to = nullptr;
+    constexpr int kSlots = 8, kPerSlot = (NJ + kSlots - 1) / kSlots;
+    auto some = [&](int slot) {
+      if (!flat) return;
+#pragma unroll
+      for (int i = 0; i < kPerSlot; ++i) {
+        const int jj = slot * kPerSlot + i, j = wave + 4 * jj;
+        if (jj < NJ && (C::NI % 4 == 0 || j < C::NI))
+          g2lds16(place[jj < NJ ? jj : 0] == kNoPlace ? (const char*)kZeroRow : flat + place[jj < NJ ? jj : 0], flat_to + j * 64 * E);
+      }
+    };
+    auto fetch = [&](int it, int st, bool at_once) {
       const int k0 = it * kTileKeys, p0 = page_of(k0), o0 = k0 - p0 * a.page;
       if (win < 0 || page_of(min(k0 + kTileKeys, rs.visible) - 1) >= win + kWindow) {  // the same for every thread
         lds_barrier();
@@ -113,16 +126,15 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
       // a tile that lies in one page: rows follow each other, places relative to the tile's are known
       const int pid0 = uniform(s_page[p0 - win]);
       if (k0 + kTileKeys <= rs.visible && o0 + kTileKeys <= a.page && (unsigned)pid0 < (unsigned)a.n_pages) {
-        const char* base = (const char*)((const T*)a.cache + (int64_t)pid0 * a.page_stride + (int64_t)o0 * W);
         if (threadIdx.x == 0) s_bad[st] = 0;
+        flat = (const char*)((const T*)a.cache + (int64_t)pid0 * a.page_stride + (int64_t)o0 * W);
+        flat_to = ring + st * C::TILE;
+        if (at_once)
 #pragma unroll
-        for (int jj = 0; jj < NJ; ++jj) {
-          const int j = wave + 4 * jj;
-          if (C::NI % 4 == 0 || j < C::NI)
-            g2lds16(place[jj] == kNoPlace ? (const char*)kZeroRow : base + place[jj], ring + st * C::TILE + j * 64 * E);
-        }
+          for (int i = 0; i < kSlots; ++i) some(i);
         return;
       }
+      flat = nullptr;
       const int key = k0 + n;
       const bool live = key < rs.visible;
       const int pg = live ? page_of(key) : win, off = live ? key - pg * a.page : 0;
@@ -149,12 +161,12 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
     lds_barrier();  // the tiles and pages of the row before are read
 #pragma unroll
     for (int i = 0; i < NS - 1; ++i)
-      if (it0 + i < it1) fetch(it0 + i, i);
+      if (it0 + i < it1) fetch(it0 + i, i, true);
     int st = 0;
     for (int it = it0; it < it1; ++it) {
       if constexpr (NS == 1) {
         lds_barrier();  // the tile before is read
-        fetch(it, 0);
+        fetch(it, 0, true);
         wait_vmem();
       } else {
         // tile `it` has landed: only the tiles issued after it may be in flight
@@ -167,7 +179,10 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
       }
       lds_barrier();  // ... every wave's copies, and the stage before is read
       if constexpr (NS > 1)
-        if (it + NS - 1 < it1) fetch(it + NS - 1, st == 0 ? NS - 1 : st - 1);
+      {
+        flat = nullptr;
+        if (it + NS - 1 < it1) fetch(it + NS - 1, st == 0 ? NS - 1 : st - 1, false);
+      }
       const T* tile = ring + st * C::TILE;
 
       f32x16 s = {};
@@ -186,7 +201,10 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
         mma(s, k[i % KB], qf[i]);
         if constexpr (kTwo<T>) mma(s, k[i % KB], ql[i]);
         if (i + KB < C::KS) k[i % KB] = k_frag(i + KB);
+        if (NS > 1 && i == C::KS / 3) some(0);
+        if (NS > 1 && i == 2 * C::KS / 3) some(1);
       }
+      if (NS > 1) some(2);
 #pragma unroll
       for (int rr = 0; rr < 4; ++rr)
         s_part[(wave * 4 + rr) * 64 + l] = f32x4{s[4 * rr], s[4 * rr + 1], s[4 * rr + 2], s[4 * rr + 3]};
@@ -199,6 +217,7 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[4 * rr + e] = v[e];
       }
+      if (NS > 1) some(3);
       const int lim = rs.visible - it * kTileKeys - 4 * g;
       const uint32_t bad = s_bad[st];
       if (lim + 4 * g < kTileKeys || bad) {
@@ -213,6 +232,7 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
 #pragma unroll
       for (int r = 0; r < 16; ++r) mraw = fmaxf(mraw, s[r]);
       const float m_new = fmaxf(m, wave_xor32_max(mraw) * a.scale_log2);
+      if (NS > 1) some(4);
       const bool bump = m_new > m + kRescaleLog2;
       const float alpha = bump ? fast_exp2(m - m_new) : 1.f;
       m = bump ? m_new : m;
@@ -224,12 +244,14 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
         ps += s[r];
       }
       lsum = lsum * alpha + ps;
+      if (NS > 1) some(5);
       if (__ballot(bump)) {
 #pragma unroll
         for (int i = 0; i < ND; ++i) oacc[i] *= alpha;
       }
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
+        if (NS > 1) some(6 + kk);
         const frag_t<T> pf = acc_to_frag<T>(s, kk);
         frag_t<T> pl;
         if constexpr (kTwo<T>) {
