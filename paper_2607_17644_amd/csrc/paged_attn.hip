@@ -9,7 +9,6 @@
 // by W_v (join_kernel). Bound by the cache's bytes for few heads (2 (2 d_c + d_rope) flop per
 // head for each row of d_c + d_rope elements).
 #include <math.h>
-#include <stdlib.h>
 
 #define LAGA_LDS_DMA_ASM 1
 #include "common.hpp"
@@ -200,24 +199,90 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && ND <= 2 ? 2 : 1) void split_
 }
 
 // ---------------------------------------------------------------- join
-// out^T = W_v^T o^T for some rows of one head. The four waves take a quarter of the contraction
-// each; a lane's column of o^T is one row's partials j, j + SUB, ... (SUB lanes share a row,
-// rows of the 32 columns: 32 / SUB), weighted by exp2(m - max m) / sum and added up in registers; as the
-// product is linear, the SUB columns are added after it. So one row split over all workers has
-// its partials read by 32 lanes at once, and a batch of whole rows keeps 32 rows per product.
-// W_v's rows arrive by direct copies meanwhile. Bound by the latency of those two reads.
+// The running softmax of some partials of a row: this thread's four columns of sum f o, with f
+// = exp2(m - max m), and the sum of f l.
+struct Joined {
+  float m, l;
+  f32x4 o;
+};
+__device__ __forceinline__ void join_in(Joined& x, float m, float l, const f32x4& o) {
+  const float m_new = fmaxf(x.m, m), m_use = m_new == -INFINITY ? 0.f : m_new;
+  const float f = fast_exp2(m - m_use), old = x.m == -INFINITY ? 0.f : fast_exp2(x.m - m_use);
+  x.m = m_new;
+  x.l = __builtin_fmaf(x.l, old, f * l);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x.o[e] = __builtin_fmaf(f, o[e], x.o[e] * old);
+}
+// The workers [w0, w1] that share row t; split false: one worker took the row whole, or none did
+// (seen false), or the row is bad (fill: what its results are then).
+struct RowParts {
+  int first, w0, w1;
+  bool seen, split;
+  float fill;
+};
+__device__ __forceinline__ RowParts parts_of(const PagedArgs& a, int t) {
+  const int32_t* before = a.sched + kSchedHeader;
+  const int per = a.sched[0], first = before[t], end = before[t + 1];
+  if (first == end) return {0, 0, -1, false, false, row_state(a, t).bad ? NAN : 0.f};
+  const int w0 = first / per, w1 = (end - 1) / per;
+  return {first, w0, w1, true, w0 != w1, 0.f};
+}
+// Partials of a row's head, dealt to `groups` threads of the same four columns (c), then joined in order
+// through LDS (room: 24 bytes per thread). The result is complete in the threads of group 0.
+__device__ __forceinline__ Joined join_parts(const PagedArgs& a, const RowParts& r, int h, int c, int group, int groups,
+                                             int quads, bool mine, unsigned char* lds) {
+  Joined x = {-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+  const int per = a.sched[0];
+  if (mine)
+#pragma unroll 8
+    for (int w = r.w0 + group; w <= r.w1; w += groups) {
+      const int64_t p = (int64_t)partial_place(w, per, r.first) * a.H + h;
+      join_in(x, a.part_ml[2 * p], a.part_ml[2 * p + 1], *reinterpret_cast<const f32x4*>(a.part_o + p * a.d_c + c));
+    }
+  if (groups == 1) return x;
+  f32x4* so = (f32x4*)lds;
+  float2* sm = (float2*)(so + blockDim.x);
+  so[threadIdx.x] = x.o;
+  sm[threadIdx.x] = float2{x.m, x.l};
+  __syncthreads();
+  if (group == 0 && mine)
+    for (int u = 1; u < groups; ++u) join_in(x, sm[u * quads + threadIdx.x].x, sm[u * quads + threadIdx.x].y, so[u * quads + threadIdx.x]);
+  return x;
+}
+
+// Rows that several workers share, put together in obar: a workgroup per row and head. Bound by
+// reading the partials (128 heads x 61 rows, 83 MB, 19 us; within the product's own kernel, where a
+// lane had several loads of 16 bytes under way at most, 47 with it against 19 + 17).
+constexpr int kCombineThreads = 256;
+__global__ __launch_bounds__(kCombineThreads) void combine_kernel(PagedArgs a) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[24 * kCombineThreads];
+  const int t = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  const RowParts r = parts_of(a, t);
+  if (!r.split) return;
+  const int quads = a.d_c / 4, groups = kCombineThreads / quads, group = threadIdx.x / quads;
+  const int c = threadIdx.x % quads * 4;
+  const Joined x = join_parts(a, r, h, c, group, groups, quads, group < groups, lds);
+  if (group != 0) return;
+  const int64_t th = (int64_t)t * a.H + h;
+  const float inv = 1.f / x.l;
+  *reinterpret_cast<f32x4*>(a.obar + th * a.d_c + c) = f32x4{x.o[0] * inv, x.o[1] * inv, x.o[2] * inv, x.o[3] * inv};
+  if (c == 0 && a.lse) a.lse[th] = (x.m + fast_log2(x.l)) * kLn2;
+}
+
+// out^T = W_v^T o^T for 32 rows of one head, o normalised in obar. The four waves take a quarter of
+// the contraction each, o straight from global memory as operands, W_v's rows by direct copies
+// meanwhile. Bound by the latency of those two reads, or by reading o.
 template <typename T, int DV, int NB, int NST>  // NB 32-column blocks of out; NST steps of 16 per wave
-__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, int tblocks, int joined) {
+__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
   constexpr int E = 16 / sizeof(T), CPR = 32 * NB / E;  // 16-byte chunks of a staged row
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   __shared__ float s_dot[4][32];
   T* sw = (T*)smem;
   const int l = threadIdx.x & 63, n = l & 31, g = l >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int sub = 1 << sub_log2, j = n & (sub - 1);
   constexpr int VB = DV / (32 * NB);
   const int vb = blockIdx.x % VB, h = blockIdx.x / VB / tblocks;
-  const int t0 = blockIdx.x / VB % tblocks * (32 >> sub_log2), t = t0 + (n >> sub_log2);
+  const int t = blockIdx.x / VB % tblocks * 32 + n;
   const int dc = a.d_c, nch = dc * CPR;
   const int64_t ldw = (int64_t)a.H * (a.d_nope + DV);
   const T* wv = (const T*)a.w + (int64_t)h * (a.d_nope + DV) + a.d_nope + 32 * NB * vb;
@@ -228,99 +293,43 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, in
     g2lds16(wv + r * ldw + c * E, sw + p0 * E);
   }
 
-  // this lane's share of its row's partials
-  const int32_t* before = a.sched + kSchedHeader;
-  const int per = a.sched[0];
-  int first = 0, last = 0, w0 = 0;  // its partials: workers first, first + sub, .. < last
-  bool whole = false;
-  float fill = 0.f;
-  float lse = -INFINITY;
+  const bool fix = a.lse && vb == 0 && a.lse_fix && a.sched[2] == 0;
+  const int64_t th = (int64_t)t * a.H + h;
+  bool seen = false;
+  float fill = 0.f, lse = 0.f;
   if (t < a.T) {
-    first = before[t];
-    last = before[t + 1];
-    if (first == last) {
-      if (row_state(a, t).bad) fill = lse = NAN;
-      last = 0;
-      w0 = 0;
-    } else {
-      w0 = first / per;
-      last = (last - 1) / per + 1;
-      if (joined) last = w0 + 1;
-      whole = last == w0 + 1;
-    }
+    const int32_t* before = a.sched + kSchedHeader;
+    seen = before[t] != before[t + 1];
+    if (!seen && row_state(a, t).bad) fill = NAN;
+    if (seen && fix) lse = a.lse[th];
+    if (!seen) lse = fill == 0.f ? -INFINITY : NAN;
   }
-  const int row_first = first;
-  if (whole && a.lse) lse = a.lse[(int64_t)t * a.H + h];
-
   // step i of this wave: columns 16 (NST wave + i) + {4 g .. + 3, 8 + 4 g .. + 3}
-  float v[NST][8];
-#pragma unroll
-  for (int i = 0; i < NST; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = j == 0 ? fill : 0.f;
   const int c0 = 16 * NST * wave + 4 * g;
-  // this lane's partials under their own running maximum: nothing waits for another lane's
-  float mx = -INFINITY, sum = 0.f;
-  for (int w = w0 + j; w < last; w += sub) {
-    const int64_t p = (int64_t)partial_place(w, per, row_first) * a.H + h;
-    const float* o = whole ? a.obar + ((int64_t)t * a.H + h) * dc : a.part_o + p * dc;
-    f32x4 x[NST], y[NST];
+  f32x4 x[NST][2];
 #pragma unroll
-    for (int i = 0; i < NST; ++i) {
-      if (16 * (NST * wave + i) >= dc) continue;  // wave-uniform
-      x[i] = *reinterpret_cast<const f32x4*>(o + c0 + 16 * i);
-      y[i] = *reinterpret_cast<const f32x4*>(o + c0 + 16 * i + 8);
-    }
-    float f = 1.f, old = 1.f;
-    if (!whole) {
-      const float m = a.part_ml[2 * p], l = a.part_ml[2 * p + 1], m_new = fmaxf(mx, m);
-      const float m_use = m_new == -INFINITY ? 0.f : m_new;
-      f = fast_exp2(m - m_use);
-      old = mx == -INFINITY ? 0.f : fast_exp2(mx - m_use);
-      mx = m_new;
-      sum = __builtin_fmaf(sum, old, f * l);
-    }
-#pragma unroll
-    for (int i = 0; i < NST; ++i) {
-      if (16 * (NST * wave + i) >= dc) continue;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[i][e] = __builtin_fmaf(f, x[i][e], v[i][e] * old);
-        v[i][4 + e] = __builtin_fmaf(f, y[i][e], v[i][4 + e] * old);
-      }
+  for (int i = 0; i < NST; ++i) {
+    x[i][0] = x[i][1] = f32x4{fill, fill, fill, fill};
+    if (seen && 16 * (NST * wave + i) < dc) {
+      x[i][0] = *reinterpret_cast<const f32x4*>(a.obar + th * dc + c0 + 16 * i);
+      x[i][1] = *reinterpret_cast<const f32x4*>(a.obar + th * dc + c0 + 16 * i + 8);
     }
   }
-  // and brought to the row's
-  if (last > 0 && !whole) {  // (the same for the lanes of a row)
-    float all = mx;
-    for (int o = sub >> 1; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o));
-    const float m_use = all == -INFINITY ? 0.f : all;
-    float f = mx == -INFINITY ? 0.f : fast_exp2(mx - m_use);
-    sum *= f;
-    for (int o = sub >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    lse = (all + fast_log2(sum)) * kLn2;
-    f /= sum;
-#pragma unroll
-    for (int i = 0; i < NST; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] *= f;
-  }
-  const bool fix = a.lse_fix && a.sched[2] == 0;
-  if (a.lse && fix && vb == 0) {
+  if (fix) {
     float dot = 0.f;
-    if (t < a.T) {
-      const T* q = (const T*)a.qa_lo + ((int64_t)t * a.H + h) * (dc + a.d_rope) + c0;
+    if (seen) {
+      const T* q = (const T*)a.qa_lo + th * (dc + a.d_rope) + c0;
 #pragma unroll
-      for (int i = 0; i < NST; ++i) {
-        if (16 * (NST * wave + i) >= dc) continue;
-        typedef typename FragOf<T>::half half4;
-        const half4 x = *reinterpret_cast<const half4*>(q + 16 * i), y = *reinterpret_cast<const half4*>(q + 16 * i + 8);
+      for (int i = 0; i < NST; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) dot += v[i][e] * to_f32(x[e]) + v[i][4 + e] * to_f32(y[e]);
-      }
+        for (int u = 0; u < 2; ++u) {
+          if (16 * (NST * wave + i) >= dc) continue;
+          const typename FragOf<T>::half y = *reinterpret_cast<const typename FragOf<T>::half*>(q + 16 * i + 8 * u);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dot = __builtin_fmaf(x[i][u][e], to_f32(y[e]), dot);
+        }
     }
     dot = wave_xor32_sum(dot);
-    for (int o = sub >> 1; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
     if (g == 0) s_dot[wave][n] = dot;
   }
 
@@ -332,12 +341,12 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, in
 #pragma unroll
   for (int i = 0; i < NST; ++i) {
     const int ks = NST * wave + i;
-    if (16 * ks >= dc) continue;
+    if (16 * ks >= dc) continue;  // wave-uniform
     frag_t<T> hi, lo;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      hi[e] = to_elem<T>(v[i][e]);
-      lo[e] = to_elem<T>(v[i][e] - to_f32(hi[e]));
+      hi[e] = to_elem<T>(x[i][e / 4][e % 4]);
+      lo[e] = to_elem<T>(x[i][e / 4][e % 4] - to_f32(hi[e]));
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -349,11 +358,6 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, in
       if constexpr (kTwo<T>) mma(acc[b], wf, lo);
     }
   }
-  for (int o = sub >> 1; o > 0; o >>= 1)
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[b][r] += __shfl_xor(acc[b][r], o);
   lds_barrier();  // W_v is read
   f32x4* red = (f32x4*)smem;
 #pragma unroll
@@ -362,20 +366,19 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, in
     for (int rr = 0; rr < 4; ++rr)
       red[((wave * NB + b) * 4 + rr) * 64 + l] = f32x4{acc[b][4 * rr], acc[b][4 * rr + 1], acc[b][4 * rr + 2], acc[b][4 * rr + 3]};
   lds_barrier();
-  if (a.lse && vb == 0 && wave == 0 && g == 0 && j == 0 && t < a.T) {
-    if (fix)
-      lse += (((s_dot[0][n] + s_dot[1][n]) + s_dot[2][n]) + s_dot[3][n]) * a.scale_log2 * kLn2;
-    if (fix || !whole) a.lse[(int64_t)t * a.H + h] = lse;
+  if (t >= a.T) return;
+  if (a.lse && vb == 0 && wave == 0 && g == 0 && (fix || !seen)) {
+    if (fix && seen) lse += (((s_dot[0][n] + s_dot[1][n]) + s_dot[2][n]) + s_dot[3][n]) * a.scale_log2 * kLn2;
+    a.lse[th] = lse;
   }
   // 4 NB groups of four columns per lane, dealt to the waves
-  if (t >= a.T || j != 0) return;
-  T* o = (T*)a.out + ((int64_t)t * a.H + h) * DV + 32 * NB * vb + 4 * g;
+  T* o = (T*)a.out + th * DV + 32 * NB * vb + 4 * g;
 #pragma unroll
-  for (int x = 0; x < NB; ++x) {
-    const int i = wave + 4 * x, b = i / 4, rr = i % 4;
+  for (int u = 0; u < NB; ++u) {
+    const int i = wave + 4 * u, b = i / 4, rr = i % 4;
     f32x4 y = red[(b * 4 + rr) * 64 + l];
 #pragma unroll
-    for (int u = 1; u < 4; ++u) y += red[((u * NB + b) * 4 + rr) * 64 + l];
+    for (int w = 1; w < 4; ++w) y += red[((w * NB + b) * 4 + rr) * 64 + l];
     typename FragOf<T>::half z;
 #pragma unroll
     for (int e = 0; e < 4; ++e) z[e] = to_elem<T>(y[e]);
@@ -383,54 +386,103 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int sub_log2, in
   }
 }
 
-// Rows that several workers share, put together in obar: a thread per four columns of a row's
-// head adds its partials up in order.
-__global__ __launch_bounds__(256) void combine_kernel(PagedArgs a) {
-  const int quads = a.d_c / 4;
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, th = x / quads;
-  const int c = (int)(x % quads) * 4;
-  const int t = (int)(th / a.H), h = (int)(th % a.H);
-  if (t >= a.T) return;
-  const int32_t* before = a.sched + kSchedHeader;
-  const int per = a.sched[0], first = before[t], end = before[t + 1];
-  if (first == end) return;
-  const int w0 = first / per, w1 = (end - 1) / per;
-  if (w0 == w1) return;
-  float mx = -INFINITY, sum = 0.f;
-  f32x4 v = {};
-#pragma unroll 8
-  for (int w = w0; w <= w1; ++w) {
-    const int64_t p = (int64_t)partial_place(w, per, first) * a.H + h;
-    const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + p * a.d_c + c);
-    const float m = a.part_ml[2 * p], l = a.part_ml[2 * p + 1], m_new = fmaxf(mx, m);
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float f = fast_exp2(m - m_use), old = mx == -INFINITY ? 0.f : fast_exp2(mx - m_use);
-    mx = m_new;
-    sum = __builtin_fmaf(sum, old, f * l);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(f, o[e], v[e] * old);
-  }
-  const float inv = 1.f / sum;
-  *reinterpret_cast<f32x4*>(a.obar + th * a.d_c + c) = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-  if (c == 0 && a.lse) a.lse[th] = (mx + fast_log2(sum)) * kLn2;
+template <typename T, int DV, int NB>
+void launch_join_product(const PagedArgs& a, hipStream_t st) {
+  const int tb = (a.T + 31) / 32;
+  const unsigned wgs = (unsigned)((int64_t)a.H * (DV / (32 * NB)) * tb);
+  const size_t w = (size_t)a.d_c * 32 * NB * sizeof(T), red = (size_t)NB * 16384, lds = w > red ? w : red;
+  if (a.d_c <= 128) join_kernel<T, DV, NB, 2><<<wgs, 256, lds, st>>>(a, tb);
+  else if (a.d_c <= 256) join_kernel<T, DV, NB, 4><<<wgs, 256, lds, st>>>(a, tb);
+  else if (a.d_c <= 512) join_kernel<T, DV, NB, 8><<<wgs, 256, lds, st>>>(a, tb);
+  else join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, tb);
 }
 
-// Lanes per row: as many as leave 32 / SUB >= T rows, and more while the launch is small and a
-// row may have that many partials.
-template <typename T, int DV, int NB>
-hipError_t launch_join(const PagedArgs& a, bool joined, hipStream_t st) {
-  int sl = 0;
-  while (!joined && sl < 5 && (a.T << sl) <= 16) ++sl;
-  auto blocks = [&] { return (int)(((int64_t)a.T + (32 >> sl) - 1) / (32 >> sl)); };
-  while (!joined && sl < 5 && (int64_t)a.H * (DV / (32 * NB)) * blocks() < 2 * kCus && ((int64_t)a.T << sl) < a.workers) ++sl;
-  const unsigned wgs = (unsigned)((int64_t)a.H * (DV / (32 * NB)) * blocks());
-  const size_t w = (size_t)a.d_c * 32 * NB * sizeof(T), red = (size_t)NB * 16384, lds = w > red ? w : red;
-  const int tb = blocks();
-  if (a.d_c <= 128) join_kernel<T, DV, NB, 2><<<wgs, 256, lds, st>>>(a, sl, tb, joined);
-  else if (a.d_c <= 256) join_kernel<T, DV, NB, 4><<<wgs, 256, lds, st>>>(a, sl, tb, joined);
-  else if (a.d_c <= 512) join_kernel<T, DV, NB, 8><<<wgs, 256, lds, st>>>(a, sl, tb, joined);
-  else join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, sl, tb, joined);
-  return hipGetLastError();
+// The same for one row and head per workgroup of 1024 threads, partials and all, in fp32: where
+// there are no more of them than CUs. W_v's rows are on their way to registers (one 32-bit or
+// 64-bit pair of columns and up to kVecRows rows per thread) before the partials are known.
+constexpr int kVecThreads = 1024, kVecRows = 32;
+template <typename T, int DV>
+__global__ __launch_bounds__(kVecThreads) void join_vec_kernel(PagedArgs a) {
+  constexpr int PAIRS = DV / 2, SLICES = kVecThreads / PAIRS;
+  typedef __attribute__((__vector_size__(2 * sizeof(T)))) T pair_t;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[24 * kVecThreads];
+  __shared__ float s_o[1024], s_out[SLICES][DV];
+  const int tid = threadIdx.x, t = blockIdx.x / a.H, h = blockIdx.x % a.H, dc = a.d_c;
+  const int64_t th = (int64_t)t * a.H + h, ldw = (int64_t)a.H * (a.d_nope + DV);
+  const int v = tid % PAIRS, slice = tid / PAIRS, rows = (dc + SLICES - 1) / SLICES, r0 = slice * rows;
+  const T* w = (const T*)a.w + (int64_t)h * (a.d_nope + DV) + a.d_nope + 2 * v;
+  pair_t wr[kVecRows];
+#pragma unroll
+  for (int i = 0; i < kVecRows; ++i)
+    if (i < rows && r0 + i < dc) wr[i] = *reinterpret_cast<const pair_t*>(w + (r0 + i) * ldw);
+  const RowParts r = parts_of(a, t);
+  const bool fix = a.lse && a.lse_fix && a.sched[2] == 0;
+  const int quads = dc / 4, groups = kVecThreads / quads, group = tid / quads, c = tid % quads * 4;
+  float lse = -INFINITY;
+  if (r.split) {
+    const Joined x = join_parts(a, r, h, c, group, groups, quads, group < groups, lds);
+    if (group == 0) {
+      const float inv = 1.f / x.l;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s_o[c + e] = x.o[e] * inv;
+      lse = (x.m + fast_log2(x.l)) * kLn2;
+    }
+  } else if (group == 0) {
+    f32x4 x = {r.fill, r.fill, r.fill, r.fill};
+    if (r.seen) {
+      x = *reinterpret_cast<const f32x4*>(a.obar + th * dc + c);
+      if (a.lse) lse = a.lse[th];
+    } else if (r.fill != 0.f) {
+      lse = NAN;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s_o[c + e] = x[e];
+  }
+  __syncthreads();
+  if (a.lse && tid < 64) {
+    float dot = 0.f;
+    if (fix && r.seen) {
+      const T* q = (const T*)a.qa_lo + th * (dc + a.d_rope);
+      for (int i = tid; i < dc; i += 64) dot = __builtin_fmaf(s_o[i], to_f32(q[i]), dot);
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) dot += __shfl_xor(dot, o);
+    }
+    if (tid == 0) a.lse[th] = lse + dot * a.scale_log2 * kLn2;
+  }
+  float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+  for (int i = 0; i < kVecRows; ++i)
+    if (i < rows && r0 + i < dc) {
+      y0 = __builtin_fmaf(s_o[r0 + i], to_f32(wr[i][0]), y0);
+      y1 = __builtin_fmaf(s_o[r0 + i], to_f32(wr[i][1]), y1);
+    }
+  for (int i = kVecRows; i < rows && r0 + i < dc; ++i) {
+    const pair_t x = *reinterpret_cast<const pair_t*>(w + (r0 + i) * ldw);
+    y0 = __builtin_fmaf(s_o[r0 + i], to_f32(x[0]), y0);
+    y1 = __builtin_fmaf(s_o[r0 + i], to_f32(x[1]), y1);
+  }
+  s_out[slice][2 * v] = y0;
+  s_out[slice][2 * v + 1] = y1;
+  __syncthreads();
+  if (tid < DV) {
+    float y = 0.f;
+#pragma unroll
+    for (int i = 0; i < SLICES; ++i) y += s_out[i][tid];
+    ((T*)a.out)[th * DV + tid] = to_elem<T>(y);
+  }
+}
+
+template <typename T, int DV>
+void launch_join(const PagedArgs& a, hipStream_t st) {
+  const int64_t pairs = (int64_t)a.T * a.H;
+  if (pairs <= kCus) return join_vec_kernel<T, DV><<<(unsigned)pairs, kVecThreads, 0, st>>>(a);
+  combine_kernel<<<(unsigned)pairs, kCombineThreads, 0, st>>>(a);
+  // all of out's columns in one workgroup (o is then read once) where W_v's rows of a head fit in
+  // LDS and heads and rows alone fill half of the GPU
+  constexpr int NB = DV / 32;
+  if (sizeof(T) == 2 && NB > 1 && a.d_c <= 512 && (int64_t)a.H * ((a.T + 31) / 32) >= kCus / 2)
+    return launch_join_product<T, DV, NB>(a, st);
+  launch_join_product<T, DV, 1>(a, st);
 }
 
 template <typename T, int DN>
@@ -452,14 +504,8 @@ hipError_t launch_paged_t(const PagedArgs& a, hipStream_t st) {
   else split_kernel<T, 8><<<wgs, 256, 0, st>>>(a, hb);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // all of out's columns in one workgroup where W_v's rows of a head fit in LDS beside another workgroup's
-  // (o is then read once), and by 32 where the launch would be small
-  constexpr int NB = DN / 32;
-  const bool joined = getenv("JOINED") != nullptr;
-  if (joined) combine_kernel<<<(unsigned)(((int64_t)a.T * a.H * a.d_c / 4 + 255) / 256), 256, 0, st>>>(a);
-  if (sizeof(T) == 2 && NB > 1 && a.d_c <= 512 && (int64_t)a.H * ((a.T + 31) / 32) >= kCus / 2)
-    return launch_join<T, DN, NB>(a, joined, st);
-  return launch_join<T, DN, 1>(a, joined, st);
+  launch_join<T, DN>(a, st);
+  return hipGetLastError();
 }
 
 }  // namespace
