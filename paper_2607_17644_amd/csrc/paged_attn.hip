@@ -397,27 +397,27 @@ void launch_join_product(const PagedArgs& a, hipStream_t st) {
   else join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, tb);
 }
 
-// The same for one row and head per workgroup of 1024 threads, partials and all, in fp32: where
-// there are no more of them than CUs. W_v's rows are on their way to registers (one 32-bit or
-// 64-bit pair of columns and up to kVecRows rows per thread) before the partials are known.
-constexpr int kVecThreads = 1024, kVecRows = 32;
-template <typename T, int DV>
-__global__ __launch_bounds__(kVecThreads) void join_vec_kernel(PagedArgs a) {
-  constexpr int PAIRS = DV / 2, SLICES = kVecThreads / PAIRS;
-  typedef __attribute__((__vector_size__(2 * sizeof(T)))) T pair_t;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[24 * kVecThreads];
-  __shared__ float s_o[1024], s_out[SLICES][DV];
+// The same for one row and head per workgroup, partials and all, in fp32: where there are no more of
+// them than CUs. W_v's rows are on their way to registers (16 bytes of a row per thread, up to
+// kVecRows rows) before the partials are known. 256 threads for small heads, else 1024.
+constexpr int kVecRows = 16;
+template <typename T, int DV, int NT>
+__global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
+  constexpr int E = 16 / sizeof(T), CPR = DV / E, SLICES = NT / CPR;  // columns of a thread; threads of a row
+  typedef __attribute__((__vector_size__(16))) T chunk_t;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[24 * NT];
+  __shared__ float s_o[1024], s_out[NT / 64][DV];
   const int tid = threadIdx.x, t = blockIdx.x / a.H, h = blockIdx.x % a.H, dc = a.d_c;
   const int64_t th = (int64_t)t * a.H + h, ldw = (int64_t)a.H * (a.d_nope + DV);
-  const int v = tid % PAIRS, slice = tid / PAIRS, rows = (dc + SLICES - 1) / SLICES, r0 = slice * rows;
-  const T* w = (const T*)a.w + (int64_t)h * (a.d_nope + DV) + a.d_nope + 2 * v;
-  pair_t wr[kVecRows];
+  const int v = tid % CPR * E, slice = tid / CPR;  // rows slice, slice + SLICES, ...
+  const T* w = (const T*)a.w + (int64_t)h * (a.d_nope + DV) + a.d_nope + v;
+  chunk_t wr[kVecRows];
 #pragma unroll
   for (int i = 0; i < kVecRows; ++i)
-    if (i < rows && r0 + i < dc) wr[i] = *reinterpret_cast<const pair_t*>(w + (r0 + i) * ldw);
+    if (slice + i * SLICES < dc) wr[i] = *reinterpret_cast<const chunk_t*>(w + (slice + i * SLICES) * ldw);
   const RowParts r = parts_of(a, t);
   const bool fix = a.lse && a.lse_fix && a.sched[2] == 0;
-  const int quads = dc / 4, groups = kVecThreads / quads, group = tid / quads, c = tid % quads * 4;
+  const int quads = dc / 4, groups = NT / quads, group = tid / quads, c = tid % quads * 4;
   float lse = -INFINITY;
   if (r.split) {
     const Joined x = join_parts(a, r, h, c, group, groups, quads, group < groups, lds);
@@ -443,39 +443,55 @@ __global__ __launch_bounds__(kVecThreads) void join_vec_kernel(PagedArgs a) {
     float dot = 0.f;
     if (fix && r.seen) {
       const T* q = (const T*)a.qa_lo + th * (dc + a.d_rope);
-      for (int i = tid; i < dc; i += 64) dot = __builtin_fmaf(s_o[i], to_f32(q[i]), dot);
+      for (int i = 8 * tid; i < dc; i += 512) {
+        float x[8];
+        load8(q + i, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(s_o[i + e], x[e], dot);
+      }
 #pragma unroll
       for (int o = 32; o >= 1; o >>= 1) dot += __shfl_xor(dot, o);
     }
     if (tid == 0) a.lse[th] = lse + dot * a.scale_log2 * kLn2;
   }
-  float y0 = 0.f, y1 = 0.f;
+  float y[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = 0.f;
 #pragma unroll
   for (int i = 0; i < kVecRows; ++i)
-    if (i < rows && r0 + i < dc) {
-      y0 = __builtin_fmaf(s_o[r0 + i], to_f32(wr[i][0]), y0);
-      y1 = __builtin_fmaf(s_o[r0 + i], to_f32(wr[i][1]), y1);
-    }
-  for (int i = kVecRows; i < rows && r0 + i < dc; ++i) {
-    const pair_t x = *reinterpret_cast<const pair_t*>(w + (r0 + i) * ldw);
-    y0 = __builtin_fmaf(s_o[r0 + i], to_f32(x[0]), y0);
-    y1 = __builtin_fmaf(s_o[r0 + i], to_f32(x[1]), y1);
+    if (slice + i * SLICES < dc)
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = __builtin_fmaf(s_o[slice + i * SLICES], to_f32(wr[i][e]), y[e]);
+  for (int i = slice + kVecRows * SLICES; i < dc; i += SLICES) {
+    const chunk_t x = *reinterpret_cast<const chunk_t*>(w + i * ldw);
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = __builtin_fmaf(s_o[i], to_f32(x[e]), y[e]);
   }
-  s_out[slice][2 * v] = y0;
-  s_out[slice][2 * v + 1] = y1;
+  // the slices of a wave, then the waves, in order
+#pragma unroll
+  for (int o = CPR; o < 64; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] += __shfl_xor(y[e], o);
+  if ((tid & 63) < CPR)
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_out[tid / 64][v + e] = y[e];
   __syncthreads();
   if (tid < DV) {
-    float y = 0.f;
+    float out = 0.f;
 #pragma unroll
-    for (int i = 0; i < SLICES; ++i) y += s_out[i][tid];
-    ((T*)a.out)[th * DV + tid] = to_elem<T>(y);
+    for (int i = 0; i < NT / 64; ++i) out += s_out[i][tid];
+    ((T*)a.out)[th * DV + tid] = to_elem<T>(out);
   }
 }
 
 template <typename T, int DV>
 void launch_join(const PagedArgs& a, hipStream_t st) {
   const int64_t pairs = (int64_t)a.T * a.H;
-  if (pairs <= kCus) return join_vec_kernel<T, DV><<<(unsigned)pairs, kVecThreads, 0, st>>>(a);
+  if (pairs <= kCus) {
+    if (a.d_c * DV <= 128 * 64) join_vec_kernel<T, DV, 256><<<(unsigned)pairs, 256, 0, st>>>(a);
+    else join_vec_kernel<T, DV, 1024><<<(unsigned)pairs, 1024, 0, st>>>(a);
+    return;
+  }
   combine_kernel<<<(unsigned)pairs, kCombineThreads, 0, st>>>(a);
   // all of out's columns in one workgroup (o is then read once) where W_v's rows of a head fit in
   // LDS and heads and rows alone fill half of the GPU
