@@ -398,7 +398,7 @@ laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg,
   }
   a.sched = (int32_t*)(wsb + ws.sched); a.qa = wsb + ws.qa; a.qa_lo = wsb + ws.qa_lo; a.obar = (float*)(wsb + ws.obar);
   a.part_o = (float*)(wsb + ws.part_o); a.part_ml = (float*)(wsb + ws.part_ml);
-  a.lse_fix = plan.wide; a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.min_per = plan.min_per; a.groups = plan.groups;
+  a.lse_fix = plan.wide; a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.groups = plan.groups;
   hipStream_t st = (hipStream_t)stream;
   return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_paged_attn<bf16>(a, st) : launch_paged_attn<float>(a, st));
 }

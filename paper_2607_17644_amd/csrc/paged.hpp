@@ -97,37 +97,43 @@ struct PagedArgs {
   int lse_fix;       // the wide kernel's: lse lacks the low halves of q W_k^T (it is added in the join)
   int heads_per_wg;  // heads of a head block
   int workers;       // of each head block
-  int min_per;       // fewest tiles that a worker takes
   int groups;        // of 32 heads in heads_per_wg (wide kernel), or 0
 };
-// Layout of the tiles: [tiles per worker, tiles, groups, -], tiles before each row [T + 1], and of
+// Layout of the tiles: [units per worker, units, groups, units of a row's cost], units before each row [T + 1], and of
 // each worker's first share (kShareInts) the row, its first tile and end, request and visible keys.
 constexpr int kSchedHeader = 4, kShareInts = 8;
 __host__ __device__ inline int64_t sched_shares(int64_t T) { return (kSchedHeader + T + 1 + 7) / 8 * 8; }
 inline size_t sched_ints(long long T, int workers) { return (size_t)sched_shares(T) + (size_t)kShareInts * workers; }
 
 __host__ __device__ inline int tiles_of(int visible) { return (visible + kTileKeys - 1) / kTileKeys; }
-// Tiles per worker: even shares, and no fewer than min_per.
-__host__ __device__ inline int tiles_per_worker(int total, int workers, int min_per) {
-  const int even = (int)(((int64_t)total + workers - 1) / workers);
-  return even > min_per ? even : min_per;
+// A row's length in the layout: its tiles and, before them, some units of no tile, which stand for what a
+// share costs besides its tiles (q in, the first tiles' way from memory, its result out). Us without
+// them and with: wide kernel, 2 x 100000 keys, 128 heads 98 and 84 (6 units 88, 24 units 86); 20 x up to
+// 3000 keys, 128 heads 61 and 42; 200 x up to 1500 keys, 32 heads 96 and 72 (24 units 80); the others, 64
+// x up to 4000 keys, d_c = 256, 33 and 32, with 9 units 34.
+constexpr int kRowCost = 2, kWideRowCost = 9;
+__host__ __device__ inline int units_of(int visible, int cost) { return visible > 0 ? cost + tiles_of(visible) : 0; }
+// Units per worker: even shares.
+__host__ __device__ inline int units_per_worker(int total, int workers) {
+  return total > workers ? (int)(((int64_t)total + workers - 1) / workers) : 1;
 }
 // How the wide kernel's workgroups go about their tiles. With few, a workgroup takes 32 of its
 // heads (groups of them: one after the other on the workgroups of an XCD) and its four waves share each
 // tile; a tile is then done in a third of the time, and no parts of waves have to meet at
 // the end. groups 0: the wide way.
-constexpr int kFewTiles = 8;  // tiles of a worker
-struct Shares { int per, workers, groups; };
-__host__ __device__ inline Shares shares_of(int total, int workers, int min_per, int groups) {
+constexpr int kFewTiles = 8;  // units of a worker
+struct Shares { int per, workers, groups, cost, total; };
+__host__ __device__ inline Shares shares_of(int tiles, int rows, int workers, int groups) {
   const int few = groups > 0 ? workers / (8 * groups) * 8 : 0;
   if (few > 0) {
-    const int per = tiles_per_worker(total, few, 1);
-    if (per <= kFewTiles) return {per, few, groups};
+    const int total = tiles + rows * kRowCost, per = units_per_worker(total, few);
+    if (per <= kFewTiles) return {per, few, groups, kRowCost, total};
   }
-  return {tiles_per_worker(total, workers, min_per), workers, 0};
+  const int cost = groups > 0 ? kWideRowCost : kRowCost, total = tiles + rows * cost;
+  return {units_per_worker(total, workers), workers, 0, cost, total};
 }
-// The partial place of worker w's share of the row whose tiles begin at row_first: a row that
-// was begun before the worker's range (or with it) is its first, any other its last.
+// The partial place of worker w's share of the row whose tiles begin at unit row_first: a row whose tiles
+// begin before the worker's range (or with it) is its first, any other its last.
 __host__ __device__ inline int partial_place(int w, int per, int row_first) {
   return 2 * w + (row_first > (int64_t)w * per ? 1 : 0);
 }
@@ -144,7 +150,7 @@ inline void page_division(int page, uint32_t* magic, uint32_t* shift) {
 
 struct PagedPlan {
   bool wide;  // paged_wide.hip: bf16 with d_c = 512 and d_rope = 64
-  int heads_per_wg, head_blocks, workers, min_per, groups;
+  int heads_per_wg, head_blocks, workers, groups;
 };
 inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
   PagedPlan p;
@@ -156,7 +162,6 @@ inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
   const int w = wgs / p.head_blocks / 8 * 8;  // whole rounds over the 8 XCDs
   p.workers = w > 8 ? w : 8;
   p.groups = p.wide ? (p.heads_per_wg + 31) / 32 : 0;
-  p.min_per = 1;
   return p;
 }
 

@@ -113,7 +113,7 @@ __device__ void absorb_band(const PagedArgs& a, int t) {
   }
 }
 
-// Tiles before each row, tiles per worker, and each worker's first share.
+// Units before each row, units per worker, and each worker's first share.
 constexpr int kLayoutLds = 2048;  // rows whose sums and states are kept in LDS
 __device__ void lay_out_tiles(const PagedArgs& a) {
   constexpr int NT = 64 * kAbsorbWaves;
@@ -123,12 +123,32 @@ __device__ void lay_out_tiles(const PagedArgs& a) {
   const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
   const bool lds = a.T <= kLayoutLds;
   int32_t* before = a.sched + kSchedHeader;
+  // all tiles, and the rows that have any
+  RowState mine = {0, 0, false};
+  int tiles = 0, rows = 0;
+  for (int t = tid; t < a.T; t += NT) {
+    const RowState rs = row_state(a, t);
+    if (t < NT) mine = rs;
+    tiles += tiles_of(rs.visible);
+    rows += rs.visible > 0;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    tiles += __shfl_xor(tiles, o);
+    rows += __shfl_xor(rows, o);
+  }
+  if (l == 0) sm[wave] = tiles, sm[kAbsorbWaves + wave] = rows;
+  __syncthreads();
+  tiles = rows = 0;
+  for (int w = 0; w < kAbsorbWaves; ++w) tiles += sm[w], rows += sm[kAbsorbWaves + w];
+  const Shares sh = shares_of(tiles, rows, a.workers, a.groups);
+  __syncthreads();
   int sum = 0;
   for (int base = 0; base < a.T; base += NT) {
     const int t = base + tid;
     RowState rs = {0, 0, false};
-    if (t < a.T) rs = row_state(a, t);
-    const int n = tiles_of(rs.visible);
+    if (t < a.T) rs = base == 0 ? mine : row_state(a, t);
+    const int n = units_of(rs.visible, sh.cost);
     int inc = n;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -152,19 +172,19 @@ __device__ void lay_out_tiles(const PagedArgs& a) {
       }
     }
   }
-  const Shares sh = shares_of(sum, a.workers, a.min_per, a.groups);
   if (tid == 0) {
     before[a.T] = sum;
     a.sched[0] = sh.per;
     a.sched[1] = sum;
     a.sched[2] = sh.groups;
+    a.sched[3] = sh.cost;
   }
   __syncthreads();
   const int32_t* sums = lds ? s_before : before;
   for (int w = tid; w < sh.workers; w += NT) {
     const int64_t start = (int64_t)w * sh.per;
     if (start >= sum) break;
-    int lo = 0, hi = a.T;  // last row whose tiles begin at or before start
+    int lo = 0, hi = a.T;  // last row whose units begin at or before start
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (sums[mid] <= start) lo = mid; else hi = mid;
@@ -173,11 +193,11 @@ __device__ void lay_out_tiles(const PagedArgs& a) {
     const RowState rs = lds ? RowState{s_request[lo], s_visible[lo], false} : row_state(a, lo);
     int32_t* out = a.sched + sched_shares(a.T) + (int64_t)w * kShareInts;
     typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
-    *reinterpret_cast<i32x4*>(out) = i32x4{lo, sums[lo], end, rs.request};
+    *reinterpret_cast<i32x4*>(out) = i32x4{lo, sums[lo] + sh.cost, end, rs.request};
     out[4] = rs.visible;
   }
 }
-constexpr size_t layout_lds() { return sizeof(int32_t) * (3 * kLayoutLds + kAbsorbWaves); }
+constexpr size_t layout_lds() { return sizeof(int32_t) * (3 * kLayoutLds + 2 * kAbsorbWaves); }
 
 template <typename T, int DN>
 __global__ __launch_bounds__(64 * kAbsorbWaves) void absorb_kernel(PagedArgs a, int cblocks, int tparts) {
@@ -222,8 +242,8 @@ struct RowParts {
 };
 __device__ __forceinline__ RowParts parts_of(const PagedArgs& a, int t) {
   const int32_t* before = a.sched + kSchedHeader;
-  const int per = a.sched[0], first = before[t], end = before[t + 1];
-  if (first == end) return {0, 0, -1, false, false, row_state(a, t).bad ? NAN : 0.f};
+  const int per = a.sched[0], first = before[t] + a.sched[3], end = before[t + 1];
+  if (before[t] == end) return {0, 0, -1, false, false, row_state(a, t).bad ? NAN : 0.f};
   const int w0 = first / per, w1 = (end - 1) / per;
   return {first, w0, w1, true, w0 != w1, 0.f};
 }

@@ -43,13 +43,13 @@ __device__ __forceinline__ Share first_share(const PagedArgs& a, int w) {
   const int32_t* s = a.sched + sched_shares(a.T) + (int64_t)w * kShareInts;
   return {uniform(s[0]), uniform(s[1]), uniform(s[2]), uniform(s[3]), uniform(s[4])};
 }
-// the row after t that has tile at (the end of t's)
+// the next row that has tiles after t, whose units end at `at`
 __device__ __forceinline__ Share next_share(const PagedArgs& a, int t, int at) {
   const int32_t* before = a.sched + kSchedHeader;
   int end;
   do ++t; while ((end = uniform(before[t + 1])) <= at);
   const RowState rs = row_state(a, t);
-  return {t, at, end, uniform(rs.request), uniform(rs.visible)};
+  return {t, at + uniform(a.sched[3]), end, uniform(rs.request), uniform(rs.visible)};
 }
 
 // Rows that are not read are copied from here (the widest row and its padding).

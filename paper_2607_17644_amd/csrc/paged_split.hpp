@@ -52,6 +52,7 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
   if (start >= total) return;
   const int end = (int)min((int64_t)total, start + per);
   Share share = first_share(a, w);
+  if (share.first >= end) return;  // (units of no tile)
 
   // copy j's lane: chunk c of the tile's row; and its place in a tile whose rows follow each other
   constexpr int NJ = (C::NI + 3) / 4;
@@ -71,7 +72,7 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
     place[jj] = c * E < W ? (uint32_t)(row * W * (int)sizeof(T) + c * 16) : kNoPlace;
   }
 
-  for (int at = (int)start;;) {
+  for (int at = max((int)start, share.first);;) {
     const int t = share.t, row_first = share.first, row_end = share.end;
     const int it0 = at - row_first, it1 = min(end, row_end) - row_first;
     at = min(end, row_end);
@@ -319,6 +320,8 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
     }
     if (at >= end) return;
     share = next_share(a, t, at);
+    at = share.first;
+    if (at >= end) return;
   }
 }
 

@@ -7,11 +7,11 @@
 namespace laga {
 namespace {
 
-// A workgroup's four waves are HG groups of 32 heads x KP = 4 / HG parts of the keys: the waves
-// of one part share a tile (HG = 4: more than 64 heads), the parts take every KP-th tile and
-// meet at the row's end. A part's ring has HG stages, so that four tiles fit in LDS; with HG = 1
-// a wave fills and reads its one stage by itself, and the other three waves' copies and
-// products overlap with its wait.
+// A workgroup's four waves are HG groups of 32 heads x KP = 4 / HG parts of the keys. HG = 4, more than
+// 32 heads: the waves share a tile, and a ring of four of them in LDS (with two groups x two parts for 33
+// to 64 heads, a tile for each part and one stage ahead, 64 requests x 4000 keys took 180 us, so 80).
+// HG = 1: each wave takes every fourth tile, fills and reads its one stage by itself, the other
+// three waves' copies and products overlap with its wait, and the parts meet at the row's end.
 //   S^T = K Q^T, O^T += C^T P^T, a lane per head, as in the general kernel
 // Registers: Q (36 fragments of a row's 576 elements), the low halves of its band, and O (512 columns
 // x 32 heads) in the accumulation registers. The low halves of q W_k^T have no room: their effect on
@@ -67,10 +67,12 @@ __device__ __forceinline__ V lds_at(uint32_t address) {
 
 template <int HG, bool NT>
 __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_blocks) {
-  constexpr int KP = 4 / HG, NS = HG;
+  static_assert(HG == 1 || HG == 4);
+  constexpr int KP = 4 / HG;
   __shared__ __attribute__((aligned(16))) bf16 ring[4 * kTile];
   static_assert(SplitCfg<bf16, 4>::LDS <= (int)sizeof(ring), "the general form's LDS");
   __shared__ int32_t s_page[4][kPages];
+  __shared__ bf16x8 s_low[4][kDr / 32][64];
   __shared__ float s_m[4][32], s_l[4][32];
   __shared__ int s_high[4];
 
@@ -94,21 +96,27 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
   int32_t* win_ids = s_page[wave];
 
   Share share = first_share(a, w);
-  for (int at = (int)start;;) {
+  if (share.first >= end) return;  // (units of no tile)
+  for (int at = max((int)start, share.first);;) {
     const int t = share.t, row_first = share.first, row_end = share.end;
     const int it0 = at - row_first, it1 = min(end, row_end) - row_first;
     at = min(end, row_end);
     const int visible = min(share.visible, it1 * kTileKeys);  // to the end of this share
     const int32_t* pages = a.table + (int64_t)share.request * a.width;
 
-    bf16x8 qf[kRow / 16], ql[kDr / 16];
+    // (half of the band's low halves in LDS: with all in registers one of Q's would spill)
+    bf16x8 qf[kRow / 16], ql[kDr / 32];
     {
       const int64_t q = ((int64_t)t * a.H + (nh > 0 ? h0 + min(n, nh - 1) : 0)) * kRow + 8 * g;
 #pragma unroll
       for (int i = 0; i < kRow / 16; ++i) qf[i] = *reinterpret_cast<const bf16x8*>((const bf16*)a.qa + q + 16 * i);
 #pragma unroll
-      for (int i = 0; i < kDr / 16; ++i)
-        ql[i] = *reinterpret_cast<const bf16x8*>((const bf16*)a.qa_lo + q + kDc + 16 * i);
+      for (int i = 0; i < kDr / 16; ++i) {
+        const bf16x8 x = *reinterpret_cast<const bf16x8*>((const bf16*)a.qa_lo + q + kDc + 16 * i);
+        if (i < kDr / 32) ql[i] = x;
+        else s_low[wave][i - kDr / 32][l] = x;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     }
     f32x16 oacc[kDc / 32];
     float m = -INFINITY, lsum;
@@ -120,7 +128,18 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
     // HG = 1, whose copies wait for memory and not for their addresses), each row's place comes
     // from the lane of its key.
     constexpr int NMAIN = kTileKeys / HG, NCOPY = NMAIN + 4 / HG;
-    auto fetch = [&](int it, bf16* buf) -> uint32_t {
+    auto copy = [&](const char* flat, bf16* buf, int j, int l) {  // the j-th, of a tile that lies in one page
+      if (j < NMAIN) {
+        const int r = hg + HG * j;
+        copy_row<NT>(flat + r * 2 * kRow, (uint32_t)((l ^ swz<16>(r)) * 16), buf + r * kDc);
+      } else {
+        const int i = hg + HG * (j - NMAIN), r = l >> 3;  // (rows 8 apart are swizzled by the flip of one bit)
+        copy_row<NT>(flat + 8 * i * 2 * kRow + 2 * kDc, r * 2 * kRow + ((l & 7) ^ swz<8>(r) ^ (i & 1)) * 16,
+                     buf + kMain + i * 512);
+      }
+    };
+    const char* flat = nullptr;  // the tile's first row, where the copies are left to the caller
+    auto fetch = [&](int it, bf16* buf, bool at_once) -> uint32_t {
       const int l = fresh_lane(), n = l & 31;
       const int k0 = it * kTileKeys, p0 = page_of(k0), o0 = k0 - p0 * a.page;
       if (k0 < visible && (win < 0 || page_of(min(k0 + kTileKeys, visible) - 1) >= win + kPages)) {
@@ -132,23 +151,19 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
       }
+      flat = nullptr;
       if (HG > 1 && k0 + kTileKeys <= visible && o0 + kTileKeys <= a.page) {
-        const int pid = __builtin_amdgcn_readfirstlane(win_ids[p0 - win]);
-        const bool ok = (unsigned)pid < (unsigned)a.n_pages;
-        const char* base = uniform(ok ? (const char*)((const bf16*)a.cache + (int64_t)pid * a.page_stride + (int64_t)o0 * kRow)
-                                      : (const char*)kZeroRow);
-        const int step = __builtin_amdgcn_readfirstlane(ok ? 2 * kRow : 0);
+        const int pid = uniform(win_ids[p0 - win]);
+        if ((unsigned)pid < (unsigned)a.n_pages) {
+          const char* base = uniform((const char*)((const bf16*)a.cache + (int64_t)pid * a.page_stride + (int64_t)o0 * kRow));
+          if (at_once) {
 #pragma unroll
-        for (int j = 0; j < NMAIN; ++j) {
-          const int r = hg + HG * j;
-          copy_row<NT>(base + r * step, (uint32_t)((l ^ swz<16>(r)) * 16), buf + r * kDc);
+            for (int j = 0; j < NCOPY; ++j) copy(base, buf, j, l);
+          } else {
+            flat = base;
+          }
+          return 0;
         }
-#pragma unroll
-        for (int j = 0; j < 4 / HG; ++j) {
-          const int i = hg + HG * j, r = l >> 3;  // (rows 8 apart are swizzled by the flip of one bit)
-          copy_row<NT>(base + 8 * i * step + 2 * kDc, r * step + ((l & 7) ^ swz<8>(r) ^ (i & 1)) * 16, buf + kMain + i * 512);
-        }
-        return ok ? 0u : ~0u;
       }
       const int key = k0 + n;
       const bool live = key < visible;
@@ -174,7 +189,7 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
       return (uint32_t)__ballot(live && !ok);
     };
     // fragments are read PF (PV) products ahead, in a pinned order
-    constexpr int PF = 5, NQ = kRow / 16, PV = 4, NV = 2 * (kDc / 32);
+    constexpr int PF = HG == 4 ? 3 : 5, NQ = kRow / 16, PV = 4, NV = 2 * (kDc / 32);
     // Chunk c of a tile's row r is at c ^ swz<16>(r) (c part; c ^ swz<8>(r) in the band). This lane
     // reads the fragment of contraction step i in row n at (k ^ 32 (i % 8)) + 256 (i / 8), of
     // the band's step i at b ^ 32 i, and for the transposing reads of column block i, rows vr
@@ -197,20 +212,25 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
       const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)((x.v8 ^ flip) + add));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    // S^T of a tile, and its largest score over the lane's head
-    auto scores = [&](int it, const Reads& x, uint32_t bad, f32x16& s) {
-      bf16x8 k[PF + 1];
+    // S^T of a tile; `beside(i)` runs beside product i
+    auto products = [&](const Reads& x, f32x16& s, auto&& beside) {
+      constexpr int B0 = kDc / 16, B1 = B0 + kDr / 32;  // the band's steps; those with low halves in LDS
+      bf16x8 k[PF + 1], low[kDr / 32];
+      const uint32_t low_at = lds_address(s_low[wave]) + 16 * fresh_lane();
 #pragma unroll
       for (int i = 0; i < PF; ++i) k[i] = k_frag(x, i);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
         if (i + PF < NQ) k[(i + PF) % (PF + 1)] = k_frag(x, i + PF);
+        if (i + PF >= NQ && i + PF - NQ < kDr / 32) low[i + PF - NQ] = lds_at<bf16x8>(low_at + 1024 * (i + PF - NQ));
         score_step(s, k[i % (PF + 1)], qf[i], i == 0);
-        if (i >= kDc / 16) score_step(s, k[i % (PF + 1)], ql[i - kDc / 16], false);
+        if (i >= B0) score_step(s, k[i % (PF + 1)], i < B1 ? ql[i < B1 ? i - B0 : 0] : low[i < B1 ? 0 : i - B1], false);
+        beside(i);
         __builtin_amdgcn_sched_barrier(0);
       }
-      scores_done(s);
+    };
+    auto mask = [&](int it, uint32_t bad, f32x16& s) {
       const int lim = visible - it * kTileKeys;
       if (lim < kTileKeys || bad) {
         const int g = fresh_lane() >> 5;  // (and keeps the branch)
@@ -220,10 +240,41 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
           s[r] = k < lim ? (bad >> k & 1 ? NAN : s[r]) : -INFINITY;
         }
       }
+    };
+    // a tile's scores, and its largest over the lane's head
+    auto scores = [&](int it, const Reads& x, uint32_t bad, f32x16& s) {
+      products(x, s, [](int) {});
+      scores_done(s);
+      mask(it, bad, s);
       float mx = -INFINITY;
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
       return wave_xor32_max(mx) * a.scale_log2;
+    };
+    // O with a tile's probabilities hi + lo, two column blocks at a time, so that no product waits for the
+    // one before it; `beside(i)` runs beside product i
+    auto accumulate = [&](const Reads& x, const bf16x8 (&pf)[2], const bf16x8 (&pl)[2], auto&& beside) {
+      bf16x8 v[PV + 2];
+#pragma unroll
+      for (int i = 0; i < PV; ++i) v[i] = v_frag(x, i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < NV; i += 2) {
+        if (i + PV < NV) {
+          v[(i + PV) % (PV + 2)] = v_frag(x, i + PV);
+          v[(i + PV + 1) % (PV + 2)] = v_frag(x, i + PV + 1);
+        }
+        const bf16x8 &v0 = v[i % (PV + 2)], &v1 = v[(i + 1) % (PV + 2)];
+        mma(oacc[i % 16], v0, pf[i / 16]);
+        beside(2 * i);
+        mma(oacc[i % 16 + 1], v1, pf[i / 16]);
+        beside(2 * i + 1);
+        mma(oacc[i % 16], v0, pl[i / 16]);
+        beside(2 * i + 2);
+        mma(oacc[i % 16 + 1], v1, pl[i / 16]);
+        beside(2 * i + 3);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     };
     // O and the sums with a tile's probabilities
     auto update = [&](int it, const bf16* buf, uint32_t bad) {
@@ -248,24 +299,7 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
         for (int e = 0; e < 8; ++e) s[8 * kk + e] -= to_f32(pf[kk][e]);
         pl[kk] = acc_to_frag<bf16>(s, kk);
       }
-      // two column blocks at a time, so that no product waits for the one before it
-      bf16x8 v[PV + 2];
-#pragma unroll
-      for (int i = 0; i < PV; ++i) v[i] = v_frag(x, i);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < NV; i += 2) {
-        if (i + PV < NV) {
-          v[(i + PV) % (PV + 2)] = v_frag(x, i + PV);
-          v[(i + PV + 1) % (PV + 2)] = v_frag(x, i + PV + 1);
-        }
-        const bf16x8 &v0 = v[i % (PV + 2)], &v1 = v[(i + 1) % (PV + 2)];
-        mma(oacc[i % 16], v0, pf[i / 16]);
-        mma(oacc[i % 16 + 1], v1, pf[i / 16]);
-        mma(oacc[i % 16], v0, pl[i / 16]);
-        mma(oacc[i % 16 + 1], v1, pl[i / 16]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      accumulate(x, pf, pl, [](int) {});
     };
     // the tiles of this wave's part, in order; a tile past the share's end (a part's last step) is
     // copied from zeros and all masked
@@ -273,40 +307,77 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
     auto sweep = [&](auto&& body) {
       win = -1;
       lds_barrier();  // the tiles of the sweep before, and its parts, are read
-      if constexpr (HG == 1) {
-        bf16* buf = ring + kp * kTile;
-        for (int it = it0 + kp, i = 0; i < steps; ++i, it += KP) {
-          const uint32_t bad = fetch(it, buf);
-          wait_vmem();
-          body(it, buf, bad);
-        }
-      } else {
-        uint32_t bads[NS];
-#pragma unroll
-        for (int i = 0; i < NS; ++i) bads[i] = 0;
-#pragma unroll
-        for (int i = 0; i < NS - 1; ++i) bads[i] = fetch(it0 + i * KP + kp, ring + (i * KP + kp) * kTile);
-        int st = 0;
-        for (int step = 0; step < steps; ++step) {
-          const int it = it0 + step * KP + kp;
-          wait_vmem_le<(NS - 2) * NCOPY>();
-          lds_barrier();  // every wave's copies of the step's tiles; the stage before is read
-          // (past the end the copies are of zeros, into a stage that is not read)
-          bads[NS - 1] = fetch(it + (NS - 1) * KP, ring + ((st == 0 ? NS - 1 : st - 1) * KP + kp) * kTile);
-          body(it, ring + (st * KP + kp) * kTile, bads[0]);
-#pragma unroll
-          for (int i = 0; i < NS - 1; ++i) bads[i] = bads[i + 1];
-          st = st + 1 == NS ? 0 : st + 1;
-        }
+      bf16* buf = ring + kp * kTile;
+      for (int it = it0 + kp, i = 0; i < steps; ++i, it += KP) {
+        if (HG > 1 && i > 0) lds_barrier();  // the tile before is read
+        const uint32_t bad = fetch(it, buf, true);
         wait_vmem();
+        if (HG > 1) lds_barrier();
+        body(it, buf, bad);
       }
+    };
+    // The same for HG = 4, a tile ahead: the products of tile i + 1's scores run beside tile i's softmax,
+    // the copies of tile i + 3 beside tile i's products with P (2 x 100000 keys, 128 heads: 98 us, a tile
+    // after the other 103).
+    auto sweep_ahead = [&](auto) {
+      win = -1;
+      lds_barrier();  // the tiles of the sweep before are read
+      uint32_t bad0 = fetch(it0, ring, true), bad1 = fetch(it0 + 1, ring + kTile, true),
+               bad2 = fetch(it0 + 2, ring + 2 * kTile, true);
+      wait_vmem_le<2 * NCOPY>();
+      lds_barrier();
+      f32x16 s;
+      products(reads_of(ring), s, [](int) {});
+      scores_done(s);
+      mask(it0, bad0, s);
+      for (int step = 0; step < steps; ++step) {
+        const int it = it0 + step;
+        wait_vmem_le<NCOPY>();
+        lds_barrier();  // every wave's copies of tile it + 1; tile it - 1 is read
+        const uint32_t bad3 = fetch(it + 3, ring + (step + 3 & 3) * kTile, false);
+        f32x16 next;
+        bf16x8 pf[2], pl[2];
+        float mx = -INFINITY, ps = 0.f, m_use = 0.f;
+        products(reads_of(ring + (step + 1 & 3) * kTile), next, [&](int i) {
+          if (i < 8) {
+            mx = fmaxf(mx, fmaxf(s[2 * i], s[2 * i + 1]));
+          } else if (i == 8) {
+            mx = wave_xor32_max(mx) * a.scale_log2;
+          } else if (i == 9) {
+            m = m == -INFINITY ? mx : m;  // (nothing but zeros or NaN is summed up so far)
+            high |= __ballot(mx > m + kHead) != 0;
+            m_use = m == -INFINITY ? 0.f : m;
+          } else if (i < 26) {
+            s[i - 10] = fast_exp2(__builtin_fmaf(s[i - 10], a.scale_log2, -m_use));
+            ps += s[i - 10];
+          } else if (i < 34) {
+            const int kk = (i - 26) / 4, j = (i - 26) % 4;
+            if (j == 0) pf[kk] = acc_to_frag<bf16>(s, kk);
+            else if (j < 3)
+#pragma unroll
+              for (int e = 4 * (j - 1); e < 4 * j; ++e) s[8 * kk + e] -= to_f32(pf[kk][e]);
+            else pl[kk] = acc_to_frag<bf16>(s, kk);
+          }
+        });
+        lsum += ps;
+        accumulate(reads_of(ring + (step & 3) * kTile), pf, pl, [&](int i) {
+          if (i % 4 == 1 && i / 4 < NCOPY && flat) copy(flat, ring + (step + 3 & 3) * kTile, i / 4, fresh_lane());
+        });
+        scores_done(next);
+        mask(it + 1, bad1, next);
+        s = next;
+        bad1 = bad2;
+        bad2 = bad3;
+      }
+      wait_vmem();
     };
     for (bool again = false;; again = true) {
 #pragma unroll
       for (int i = 0; i < kDc / 32; ++i) oacc[i] = f32x16{};
       lsum = 0.f;
       high = false;
-      sweep(update);
+      if constexpr (HG == 4) sweep_ahead(0);
+      else sweep(update);
       if (again) break;
       if (l == 0) s_high[wave] = high;
       lds_barrier();
@@ -387,6 +458,8 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
     }
     if (at >= end) return;
     share = next_share(a, t, at);
+    at = share.first;
+    if (at >= end) return;
   }
 }
 
@@ -395,8 +468,7 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
 void launch_paged_wide(const PagedArgs& a, int head_blocks, hipStream_t st) {
   const unsigned wgs = (unsigned)(head_blocks * a.workers);
   if (head_blocks > 1) wide_kernel<4, false><<<wgs, 256, 0, st>>>(a, head_blocks);
-  else if (a.heads_per_wg > 64) wide_kernel<4, true><<<wgs, 256, 0, st>>>(a, head_blocks);
-  else if (a.heads_per_wg > 32) wide_kernel<2, true><<<wgs, 256, 0, st>>>(a, head_blocks);
+  else if (a.heads_per_wg > 32) wide_kernel<4, true><<<wgs, 256, 0, st>>>(a, head_blocks);
   else wide_kernel<1, true><<<wgs, 256, 0, st>>>(a, head_blocks);
 }
 

@@ -16,18 +16,24 @@ int main() {
       for (int es : {2, 4}) {
         const laga::PagedPlan p = laga::paged_plan(heads, d_c, 64, es);
         if (p.workers < 8 || p.workers % 8 || p.head_blocks * p.heads_per_wg < heads ||
-            (p.head_blocks - 1) * p.heads_per_wg >= heads || p.min_per < 1)
+            (p.head_blocks - 1) * p.heads_per_wg >= heads || p.groups < 0)
           ++bad;
         for (int rows : {1, 2, 7, 64, 300, 5000})
           for (int longest : {0, 1, 2, 40, 700, 9000}) {
             std::vector<long long> before(rows + 1, 0);
+            std::vector<int> seen(rows);
+            long long tiles = 0;
+            int live = 0;
             for (int t = 0; t < rows; ++t) {
               const int visible = rnd(4) == 0 ? 0 : longest ? (int)rnd(32 * longest) + 1 : 0;
-              before[t + 1] = before[t] + laga::tiles_of(visible);
+              seen[t] = visible;
+              tiles += laga::tiles_of(visible);
+              live += visible > 0;
             }
-            const int total = (int)before[rows];
-            const laga::Shares sh = laga::shares_of(total, p.workers, p.min_per, p.groups);
-            const int per = sh.per;
+            const laga::Shares sh = laga::shares_of((int)tiles, live, p.workers, p.groups);
+            for (int t = 0; t < rows; ++t) before[t + 1] = before[t] + laga::units_of(seen[t], sh.cost);
+            const int total = (int)before[rows], per = sh.per;
+            if (total != sh.total) ++bad;
             if ((long long)per * sh.workers < total || per < 1 || sh.workers > p.workers || sh.workers % 8) ++bad;
             // with few tiles every group of heads has its workers among the workgroups
             if (sh.groups && (sh.groups * 32 < p.heads_per_wg || sh.workers * sh.groups > p.workers)) ++bad;
@@ -36,24 +42,24 @@ int main() {
             for (int w = 0; w < sh.workers; ++w) {
               const long long start = (long long)w * per, end = start + per < total ? start + per : total;
               for (int t = 0; t < rows; ++t) {
-                const long long a = before[t] > start ? before[t] : start, b = before[t + 1] < end ? before[t + 1] : end;
+                const long long first = before[t] + sh.cost, a = first > start ? first : start, b = before[t + 1] < end ? before[t + 1] : end;
                 if (a >= b) continue;
                 ++shares;
                 done += b - a;
-                if (a == before[t] && b == before[t + 1]) continue;  // whole
-                const int at = laga::partial_place(w, per, (int)before[t]);
+                if (a == first && b == before[t + 1]) continue;  // whole
+                const int at = laga::partial_place(w, per, (int)first);
                 if (at < 0 || at >= 2 * p.workers || place[at] >= 0) ++bad;
                 else place[at] = t;
                 ++partials[t];
               }
             }
-            if (done != total) ++bad;
+            if (done != tiles) ++bad;
             for (int t = 0; t < rows; ++t) {
               if (before[t] == before[t + 1]) continue;
-              const int w0 = (int)(before[t] / per), w1 = (int)((before[t + 1] - 1) / per);
+              const int first = (int)before[t] + sh.cost, w0 = first / per, w1 = (int)((before[t + 1] - 1) / per);
               if (partials[t] != (w0 == w1 ? 0 : w1 - w0 + 1)) ++bad;
               for (int w = w0; w <= w1 && w1 > w0; ++w)
-                if (place[laga::partial_place(w, per, (int)before[t])] != t) ++bad;
+                if (place[laga::partial_place(w, per, first)] != t) ++bad;
             }
           }
       }
