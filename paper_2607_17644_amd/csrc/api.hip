@@ -198,9 +198,9 @@ laga_status_t validate_paged(const laga_paged_t* p, PagedDims* d) {
 }
 size_t elem_size(const laga_paged_t* p) { return p->dtype == LAGA_DTYPE_BF16 ? 2 : 4; }
 
-// [schedule | absorbed queries | their low halves (bf16) | whole rows | partials: outputs, statistics]
+// [schedule | absorbed queries | their second and third parts (bf16) | whole rows | partials: outputs, statistics]
 struct PagedWs {
-  size_t sched, qa, qa_lo, obar, part_o, part_ml, total;
+  size_t sched, qa, qa_lo, qa_low2, obar, part_o, part_ml, total;
 };
 PagedWs paged_layout(const laga_paged_t* p, const PagedDims& d, const PagedPlan& plan) {
   PagedWs w{};
@@ -208,7 +208,9 @@ PagedWs paged_layout(const laga_paged_t* p, const PagedDims& d, const PagedPlan&
   size_t off = 0;
   w.sched = off; off += round_up(sizeof(int32_t) * sched_ints(d.T, plan.workers));
   w.qa = off; off += round_up(elem_size(p) * rows * (d.d_c + d.dr));
-  w.qa_lo = off; off += p->dtype == LAGA_DTYPE_BF16 ? round_up(elem_size(p) * rows * (d.d_c + d.dr)) : 0;
+  const size_t low = p->dtype == LAGA_DTYPE_BF16 ? round_up(elem_size(p) * rows * (d.d_c + d.dr)) : 0;
+  w.qa_lo = off; off += low;
+  w.qa_low2 = off; off += low;
   w.obar = off; off += round_up(sizeof(float) * rows * d.d_c);
   w.part_o = off; off += round_up(sizeof(float) * places * d.d_c);
   w.part_ml = off; off += round_up(sizeof(float) * places * 2);
@@ -396,9 +398,9 @@ laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg,
     a.position_offset = cfg->position_offset;
     a.log2_base = log2((double)cfg->rope_base);
   }
-  a.sched = (int32_t*)(wsb + ws.sched); a.qa = wsb + ws.qa; a.qa_lo = wsb + ws.qa_lo; a.obar = (float*)(wsb + ws.obar);
-  a.part_o = (float*)(wsb + ws.part_o); a.part_ml = (float*)(wsb + ws.part_ml);
-  a.lse_fix = plan.wide; a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.groups = plan.groups;
+  a.sched = (int32_t*)(wsb + ws.sched); a.qa = wsb + ws.qa; a.qa_lo = wsb + ws.qa_lo; a.qa_low2 = wsb + ws.qa_low2;
+  a.obar = (float*)(wsb + ws.obar); a.part_o = (float*)(wsb + ws.part_o); a.part_ml = (float*)(wsb + ws.part_ml);
+  a.wide = plan.wide; a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.groups = plan.groups;
   hipStream_t st = (hipStream_t)stream;
   return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_paged_attn<bf16>(a, st) : launch_paged_attn<float>(a, st));
 }

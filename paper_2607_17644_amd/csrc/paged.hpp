@@ -91,10 +91,11 @@ struct PagedArgs {
   int32_t* sched;    // layout of the tiles (sched_ints)
   void* qa;          // [T][H][d_c + d_rope]: W_k q_nope, then q_rope
   void* qa_lo;       // bf16: what qa's rounding left, rounded
+  void* qa_low2;     // and what that left
   float* obar;       // [T][H][d_c]: normalised rows that one worker took whole
   float* part_o;     // [2 * workers][H][d_c]
   float* part_ml;    // [2 * workers][H][2]
-  int lse_fix;       // the wide kernel's: lse lacks the low halves of q W_k^T (it is added in the join)
+  int wide;          // paged_wide.hip's
   int heads_per_wg;  // heads of a head block
   int workers;       // of each head block
   int groups;        // of 32 heads in heads_per_wg (wide kernel), or 0
@@ -117,17 +118,21 @@ __host__ __device__ inline int units_of(int visible, int cost) { return visible 
 __host__ __device__ inline int units_per_worker(int total, int workers) {
   return total > workers ? (int)(((int64_t)total + workers - 1) / workers) : 1;
 }
-// How the wide kernel's workgroups go about their tiles. With few, a workgroup takes 32 of its
-// heads (groups of them: one after the other on the workgroups of an XCD) and its four waves share each
-// tile; a tile is then done in a third of the time, and no parts of waves have to meet at
-// the end. groups 0: the wide way.
-constexpr int kFewTiles = 8;  // units of a worker
+// How the wide kernel's workgroups go about their tiles. With few, or short rows, a workgroup takes 32 of
+// its heads (groups of them: one after the other on the workgroups of an XCD) and its four waves share
+// each tile; a tile is then done in a third of the time, no parts of waves have to meet at the end, and
+// the scores have the second part of q W_k^T (the lse of short rows averages no roundings). groups 0:
+// the wide way. Us this way and wide: 1000 rows of up to 32 keys, 16 heads 36 and 70, up to 150 62 and 89, up to
+// 500 122 and 126; 300 rows, 128 heads, up to 32 keys 60 and 53, up to 150 85 and 70; 600 rows of up to 150
+// keys, 64 heads 86 and 83.
+constexpr int kFewTiles = 8;   // units of a worker
+constexpr int kShortRows = 8;  // groups of heads x tiles, in the mean
 struct Shares { int per, workers, groups, cost, total; };
 __host__ __device__ inline Shares shares_of(int tiles, int rows, int workers, int groups) {
   const int few = groups > 0 ? workers / (8 * groups) * 8 : 0;
   if (few > 0) {
     const int total = tiles + rows * kRowCost, per = units_per_worker(total, few);
-    if (per <= kFewTiles) return {per, few, groups, kRowCost, total};
+    if (per <= kFewTiles || (int64_t)tiles * groups < kShortRows * rows) return {per, few, groups, kRowCost, total};
   }
   const int cost = groups > 0 ? kWideRowCost : kRowCost, total = tiles + rows * cost;
   return {units_per_worker(total, workers), workers, 0, cost, total};

@@ -27,14 +27,33 @@ namespace {
 // q_rope, and one lays out the tiles.
 constexpr int kAbsorbWaves = 4, kAbsorbRows = 32 * kAbsorbWaves;
 
+// N elements of qa; bf16 in three parts, each the rounding of what the ones before leave (the sum is
+// within 2^-25 of the value: the scores of a row with one key are its lse, and two parts left 2.5e-6 there).
+template <typename T, int N>
+__device__ __forceinline__ void store_parts(const PagedArgs& a, int64_t at, const float (&y)[N]) {
+  typedef __attribute__((__vector_size__(N * sizeof(T)))) T vec;
+  vec v, low, low2;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    v[e] = to_elem<T>(y[e]);
+    const float rest = y[e] - to_f32(v[e]);
+    low[e] = to_elem<T>(rest);
+    low2[e] = to_elem<T>(rest - to_f32(low[e]));
+  }
+  *reinterpret_cast<vec*>((T*)a.qa + at) = v;
+  if constexpr (kTwo<T>) {
+    *reinterpret_cast<vec*>((T*)a.qa_lo + at) = low;
+    *reinterpret_cast<vec*>((T*)a.qa_low2 + at) = low2;
+  }
+}
+
 template <typename T, int DN>
 __device__ void absorb_product(const PagedArgs& a, int blk, int cblocks, int tpart, int tparts) {
-  constexpr int E = 16 / sizeof(T), CPR = DN / E, PO = kAbsorbRows + E;  // chunks of a row; pitch of the results
+  constexpr int E = 16 / sizeof(T), CPR = DN / E, PO = kAbsorbRows + 4;  // chunks of a row; pitch of the results
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   T* sw = (T*)smem;
   T* sq = sw + kAbsorbRows * DN;
-  T* so = sq + 32 * DN;
-  T* sl = so + 32 * PO;  // bf16: low halves
+  float* so = (float*)(sq + 32 * DN);
   const int l = threadIdx.x & 63, n = l & 31, g = l >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blk / cblocks, c0 = blk % cblocks * kAbsorbRows, nc = min(kAbsorbRows, a.d_c - c0);
@@ -64,32 +83,24 @@ __device__ void absorb_product(const PagedArgs& a, int blk, int cblocks, int tpa
 #pragma unroll
     for (int ks = 0; ks < DN / 16; ++ks) mma(acc, frag(sw, 32 * wave + n, ks), frag(sq, n, ks));
 #pragma unroll
-    for (int rr = 0; rr < 4; ++rr) {
-      typename FragOf<T>::half v, low;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = to_elem<T>(acc[4 * rr + e]);
-        low[e] = to_elem<T>(acc[4 * rr + e] - to_f32(v[e]));
-      }
-      const int at = n * PO + 32 * wave + 8 * rr + 4 * g;
-      *reinterpret_cast<typename FragOf<T>::half*>(so + at) = v;
-      if constexpr (kTwo<T>) *reinterpret_cast<typename FragOf<T>::half*>(sl + at) = low;
-    }
+    for (int rr = 0; rr < 4; ++rr)
+      *reinterpret_cast<f32x4*>(so + n * PO + 32 * wave + 8 * rr + 4 * g) =
+          f32x4{acc[4 * rr], acc[4 * rr + 1], acc[4 * rr + 2], acc[4 * rr + 3]};
     lds_barrier();
     for (int x = threadIdx.x; x < nt * (kAbsorbRows / E); x += 64 * kAbsorbWaves) {
       const int r = x / (kAbsorbRows / E), c = x % (kAbsorbRows / E) * E;
       if (c >= nc) continue;
-      const int64_t at = ((int64_t)(t0 + r) * a.H + h) * W + c0 + c;
-      *reinterpret_cast<chunk16*>((T*)a.qa + at) = *reinterpret_cast<const chunk16*>(so + r * PO + c);
-      if constexpr (kTwo<T>)
-        *reinterpret_cast<chunk16*>((T*)a.qa_lo + at) = *reinterpret_cast<const chunk16*>(sl + r * PO + c);
+      float y[E];
+#pragma unroll
+      for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>(y + i) = *reinterpret_cast<const f32x4*>(so + r * PO + c + i);
+      store_parts<T, E>(a, ((int64_t)(t0 + r) * a.H + h) * W + c0 + c, y);
     }
     if (t0 + tparts * 32 < a.T) lds_barrier();  // q and the results are read
   }
 }
 template <typename T, int DN>
 constexpr size_t absorb_lds() {
-  return sizeof(T) * ((size_t)(kAbsorbRows + 32) * DN + (kTwo<T> ? 2 : 1) * 32 * (kAbsorbRows + 16 / sizeof(T)));
+  return sizeof(T) * (size_t)(kAbsorbRows + 32) * DN + sizeof(float) * 32 * (kAbsorbRows + 4);
 }
 
 // q_rope of one token, every head: a thread keeps one pair's angle
@@ -104,12 +115,7 @@ __device__ void absorb_band(const PagedArgs& a, int t) {
     const int64_t at = ((int64_t)t * a.H + h) * W + a.d_c + 2 * i;
     const float x0 = to_f32(x[0]), x1 = to_f32(x[1]);
     const float y[2] = {x0 * cs - x1 * sn, x0 * sn + x1 * cs};
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const T v = to_elem<T>(y[e]);
-      ((T*)a.qa)[at + e] = v;
-      if constexpr (kTwo<T>) ((T*)a.qa_lo)[at + e] = to_elem<T>(y[e] - to_f32(v));
-    }
+    store_parts<T, 2>(a, at, y);
   }
 }
 
@@ -247,6 +253,10 @@ __device__ __forceinline__ RowParts parts_of(const PagedArgs& a, int t) {
   const int w0 = first / per, w1 = (end - 1) / per;
   return {first, w0, w1, true, w0 != w1, 0.f};
 }
+// bf16: the scores lack the third part of q W_k^T, or on the wide kernel's way (not with few tiles) the second and
+// what is behind it: lse's share of this part to first order is scale sum_c dqa_c o_c with the row's
+// normalised sum o (the second order is below 1e-6 for the second part).
+__device__ __forceinline__ const void* lse_lacks(const PagedArgs& a) { return a.wide && a.sched[2] == 0 ? a.qa_lo : a.qa_low2; }
 // Partials of a row's head, dealt to `groups` threads of the same four columns (c), then joined in order
 // through LDS (room: 24 bytes per thread). The result is complete in the threads of group 0.
 __device__ __forceinline__ Joined join_parts(const PagedArgs& a, const RowParts& r, int h, int c, int group, int groups,
@@ -313,7 +323,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
     g2lds16(wv + r * ldw + c * E, sw + p0 * E);
   }
 
-  const bool fix = a.lse && vb == 0 && a.lse_fix && a.sched[2] == 0;
+  const bool fix = kTwo<T> && a.lse && vb == 0;
   const int64_t th = (int64_t)t * a.H + h;
   bool seen = false;
   float fill = 0.f, lse = 0.f;
@@ -338,13 +348,14 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
   if (fix) {
     float dot = 0.f;
     if (seen) {
-      const T* q = (const T*)a.qa_lo + th * (dc + a.d_rope) + c0;
+      const T* q = (const T*)lse_lacks(a) + th * (dc + a.d_rope) + c0;
 #pragma unroll
       for (int i = 0; i < NST; ++i)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           if (16 * (NST * wave + i) >= dc) continue;
-          const typename FragOf<T>::half y = *reinterpret_cast<const typename FragOf<T>::half*>(q + 16 * i + 8 * u);
+          typedef typename FragOf<T>::half quad;
+          const quad y = *reinterpret_cast<const quad*>(q + 16 * i + 8 * u);
 #pragma unroll
           for (int e = 0; e < 4; ++e) dot = __builtin_fmaf(x[i][u][e], to_f32(y[e]), dot);
         }
@@ -436,7 +447,7 @@ __global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
   for (int i = 0; i < kVecRows; ++i)
     if (slice + i * SLICES < dc) wr[i] = *reinterpret_cast<const chunk_t*>(w + (slice + i * SLICES) * ldw);
   const RowParts r = parts_of(a, t);
-  const bool fix = a.lse && a.lse_fix && a.sched[2] == 0;
+  const bool fix = kTwo<T> && a.lse;
   const int quads = dc / 4, groups = NT / quads, group = tid / quads, c = tid % quads * 4;
   float lse = -INFINITY;
   if (r.split) {
@@ -462,7 +473,7 @@ __global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
   if (a.lse && tid < 64) {
     float dot = 0.f;
     if (fix && r.seen) {
-      const T* q = (const T*)a.qa_lo + th * (dc + a.d_rope);
+      const T* q = (const T*)lse_lacks(a) + th * (dc + a.d_rope);
       for (int i = 8 * tid; i < dc; i += 512) {
         float x[8];
         load8(q + i, x);
@@ -533,7 +544,7 @@ hipError_t launch_paged_t(const PagedArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   const int hb = (a.H + a.heads_per_wg - 1) / a.heads_per_wg;
   const unsigned wgs = (unsigned)(hb * a.workers);
-  if (a.lse_fix) launch_paged_wide(a, hb, st);
+  if (a.wide) launch_paged_wide(a, hb, st);
   else if (a.d_c <= 128) split_kernel<T, 1><<<wgs, 256, 0, st>>>(a, hb);
   else if (a.d_c <= 256) split_kernel<T, 2><<<wgs, 256, 0, st>>>(a, hb);
   else if (a.d_c <= 512) split_kernel<T, 4><<<wgs, 256, 0, st>>>(a, hb);

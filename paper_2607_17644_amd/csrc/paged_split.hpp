@@ -80,7 +80,9 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
     const int32_t* pages = a.table + (int64_t)rs.request * a.width;
 
     // this wave's part of the queries: step i covers elements 16 (wave + 4 i) ..
-    frag_t<T> qf[C::KS], ql[kTwo<T> ? C::KS : 1];
+    // (bf16: and the second parts, and the third of the band's one step)
+    frag_t<T> qf[C::KS], ql[kTwo<T> ? C::KS : 1], q3 = frag_t<T>{};
+    const int band = (wave - a.d_c / 16 & 3) + a.d_c / 16;
     {
       const int64_t q = ((int64_t)t * a.H + h0 + min(n, nh - 1)) * W + 8 * g;
 #pragma unroll
@@ -93,6 +95,7 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
           if (c < W) ql[i] = *reinterpret_cast<const frag_t<T>*>((const T*)a.qa_lo + q + c);
         }
       }
+      if (kTwo<T> && 16 * band < W) q3 = *reinterpret_cast<const frag_t<T>*>((const T*)a.qa_low2 + q + 16 * band);
     }
     f32x16 oacc[ND];
 #pragma unroll
@@ -187,24 +190,26 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
       const T* tile = ring + st * C::TILE;
 
       f32x16 s = {};
-      constexpr int KB = C::KS < 9 ? C::KS : 9;  // K fragments in flight
+      constexpr int KB = C::KS < 9 ? C::KS : C::KS > 9 ? 4 : 9;  // K fragments in flight
       frag_t<T> k[KB];
-      auto k_frag = [&](int i) {
-        const int ks = wave + 4 * i;
+      auto k_frag = [&](int ks) {
         if constexpr (sizeof(T) == 2) return *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + (((2 * ks + g) ^ swz<24>(n)) * E));
         else return *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + 16 * ks + 8 * g);
       };
 #pragma unroll
-      for (int i = 0; i < KB; ++i) k[i] = k_frag(i);
+      for (int i = 0; i < KB; ++i) k[i] = k_frag(wave + 4 * i);
+      frag_t<T> kb;
+      if constexpr (kTwo<T>) kb = k_frag(band);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < C::KS; ++i) {
         mma(s, k[i % KB], qf[i]);
         if constexpr (kTwo<T>) mma(s, k[i % KB], ql[i]);
-        if (i + KB < C::KS) k[i % KB] = k_frag(i + KB);
+        if (i + KB < C::KS) k[i % KB] = k_frag(wave + 4 * (i + KB));
         if (NS > 1 && i == C::KS / 3) some(0);
         if (NS > 1 && i == 2 * C::KS / 3) some(1);
       }
+      if constexpr (kTwo<T>) mma(s, kb, q3);
       if (NS > 1) some(2);
 #pragma unroll
       for (int rr = 0; rr < 4; ++rr)

@@ -403,3 +403,20 @@ def test_served_rows_are_the_trained_block_s(heads):
     torch.cuda.synchronize()
     assert (so.float() - out[0].float()).abs().max() < 4e-2
     assert (sl - lse[0].t()).abs().max() < 4e-2
+
+
+@pytest.mark.parametrize("widths,d_c,heads", [("v3", 512, 24), ("v3", 1024, 5), ("half", 128, 64), ("small", 32, 40)])
+@pytest.mark.parametrize("count,longest", [(24, 1), (24, 4), (1500, 3)])
+def test_lse_of_short_rows_is_held_in_fp32(widths, d_c, heads, count, longest):
+    """The lse of a row with one key is its score, sum_c qa_c row_c over d_nope, then d_c + d_rope terms: fp32 sums of
+    N terms are within sqrt(N) 2^-24 of their value in the mean, for any roundings that do not lean one way."""
+    rng = np.random.default_rng(5)
+    lengths = [int(v) for v in rng.integers(1, longest + 1, count)]
+    x = make(lengths, 16, widths, d_c, heads, seed=9)
+    p = x["p"]
+    lse = f64(call(x, base=10000.0, offset=2)[1])
+    _, want = O.attend(f64(x["q"]), f64(x["w"]), f64(x["cache"]), x["table"], x["position"], x["request"], d_c=d_c,
+                       d_nope=p.d_nope, d_v=p.d_v, scale=p.softmax_scale, base=10000.0, offset=2)
+    off = np.linalg.norm(lse - want) / np.linalg.norm(want)
+    print(f"{off:.2e}")
+    assert off <= np.sqrt(p.d_nope + d_c + p.d_rope) * 2.0 ** -24
