@@ -280,152 +280,179 @@ __device__ __forceinline__ Joined join_parts(const PagedArgs& a, const RowParts&
   return x;
 }
 
-// Rows that several workers share, put together in obar: a workgroup per row and head. Bound by
+// Rows that several workers share, put together in obar: a workgroup per row and some heads. Bound by
 // reading the partials (128 heads x 61 rows, 83 MB, 19 us; within the product's own kernel, where a
 // lane had several loads of 16 bytes under way at most, 47 with it against 19 + 17).
 constexpr int kCombineThreads = 256;
+template <int HEADS>
 __global__ __launch_bounds__(kCombineThreads) void combine_kernel(PagedArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char lds[24 * kCombineThreads];
-  const int t = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  const int hblocks = (a.H + HEADS - 1) / HEADS, t = blockIdx.x / hblocks, h0 = blockIdx.x % hblocks * HEADS;
   const RowParts r = parts_of(a, t);
   if (!r.split) return;
   const int quads = a.d_c / 4, groups = kCombineThreads / quads, group = threadIdx.x / quads;
   const int c = threadIdx.x % quads * 4;
-  const Joined x = join_parts(a, r, h, c, group, groups, quads, group < groups, lds);
-  if (group != 0) return;
-  const int64_t th = (int64_t)t * a.H + h;
-  const float inv = 1.f / x.l;
-  *reinterpret_cast<f32x4*>(a.obar + th * a.d_c + c) = f32x4{x.o[0] * inv, x.o[1] * inv, x.o[2] * inv, x.o[3] * inv};
-  if (c == 0 && a.lse) a.lse[th] = (x.m + fast_log2(x.l)) * kLn2;
+  for (int h = h0; h < min(a.H, h0 + HEADS); ++h) {
+    const Joined x = join_parts(a, r, h, c, group, groups, quads, group < groups, lds);
+    if (group == 0) {
+      const int64_t th = (int64_t)t * a.H + h;
+      const float inv = 1.f / x.l;
+      *reinterpret_cast<f32x4*>(a.obar + th * a.d_c + c) = f32x4{x.o[0] * inv, x.o[1] * inv, x.o[2] * inv, x.o[3] * inv};
+      if (c == 0 && a.lse) a.lse[th] = (x.m + fast_log2(x.l)) * kLn2;
+    }
+    if (HEADS > 1) __syncthreads();  // lds is read
+  }
 }
 
-// out^T = W_v^T o^T for 32 rows of one head, o normalised in obar. The four waves take a quarter of
-// the contraction each, o straight from global memory as operands, W_v's rows by direct copies
-// meanwhile. Bound by the latency of those two reads, or by reading o.
+constexpr int kJoinRed = 16384;  // LDS in which the waves' sums meet
+// out^T = W_v^T o^T, 32 rows of one head at a time, o normalised in obar. The four waves take a quarter
+// of the contraction each, o straight from global memory as operands, W_v's rows by direct copies
+// once. A workgroup takes every tparts-th block of rows, and reads the next one's o beside this one's
+// products: with one block per workgroup, each waited for W_v and o (300 rows, 128 heads: 72 us, so 46). Bound by
+// the latency of those two reads with few rows, by reading o with many.
 template <typename T, int DV, int NB, int NST>  // NB 32-column blocks of out; NST steps of 16 per wave
-__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tblocks) {
+__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tparts) {
   constexpr int E = 16 / sizeof(T), CPR = 32 * NB / E;  // 16-byte chunks of a staged row
+  typedef typename FragOf<T>::half quad;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  __shared__ float s_dot[4][32];
-  T* sw = (T*)smem;
+  __shared__ float s_dot[2][4][32];
+  f32x4* red = (f32x4*)smem;
+  T* sw = (T*)(smem + kJoinRed);
   const int l = threadIdx.x & 63, n = l & 31, g = l >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   constexpr int VB = DV / (32 * NB);
-  const int vb = blockIdx.x % VB, h = blockIdx.x / VB / tblocks;
-  const int t = blockIdx.x / VB % tblocks * 32 + n;
-  const int dc = a.d_c, nch = dc * CPR;
+  const int vb = blockIdx.x % VB, h = blockIdx.x / VB / tparts;
+  const int dc = a.d_c, nch = dc * CPR, step = 32 * tparts;
   const int64_t ldw = (int64_t)a.H * (a.d_nope + DV);
   const T* wv = (const T*)a.w + (int64_t)h * (a.d_nope + DV) + a.d_nope + 32 * NB * vb;
+  const bool fix = kTwo<T> && a.lse && vb == 0;
+  const int32_t* before = a.sched + kSchedHeader;
+  // step i of this wave: columns 16 (NST wave + i) + {4 g .. + 3, 8 + 4 g .. + 3}
+  const int c0 = 16 * NST * wave + 4 * g;
+  struct Row {
+    bool seen;
+    float fill;
+  };
+  auto row = [&](int t) {
+    Row r = {false, 0.f};
+    if (t < a.T) {
+      r.seen = before[t] != before[t + 1];
+      if (!r.seen && row_state(a, t).bad) r.fill = NAN;
+    }
+    return r;
+  };
+  f32x4 x[NST][2];
+  quad y[kTwo<T> ? NST : 1][2];
+  const T* lacks = (const T*)lse_lacks(a);
+  auto load = [&](int i, int t, const Row& r) {
+    x[i][0] = x[i][1] = f32x4{r.fill, r.fill, r.fill, r.fill};
+    if (r.seen && 16 * (NST * wave + i) < dc) {
+      const int64_t th = (int64_t)t * a.H + h;
+      const float* o = a.obar + th * dc + c0 + 16 * i;
+      x[i][0] = *reinterpret_cast<const f32x4*>(o);
+      x[i][1] = *reinterpret_cast<const f32x4*>(o + 8);
+      if constexpr (kTwo<T>)
+        if (fix) {
+          const T* q = lacks + th * (dc + a.d_rope) + c0 + 16 * i;
+          y[i][0] = *reinterpret_cast<const quad*>(q);
+          y[i][1] = *reinterpret_cast<const quad*>(q + 8);
+        }
+    }
+  };
+  int t = blockIdx.x / VB % tparts * 32 + n;
+  Row now = row(t), next = row(t + step);
+#pragma unroll
+  for (int i = 0; i < NST; ++i) load(i, t, now);
   for (int p0 = wave * 64; p0 < nch; p0 += 256) {
     const int r = (p0 + l) / CPR;
     int c = (p0 + l) % CPR;
     if constexpr (sizeof(T) == 2) c ^= swz<CPR>(r);
     g2lds16(wv + r * ldw + c * E, sw + p0 * E);
   }
-
-  const bool fix = kTwo<T> && a.lse && vb == 0;
-  const int64_t th = (int64_t)t * a.H + h;
-  bool seen = false;
-  float fill = 0.f, lse = 0.f;
-  if (t < a.T) {
-    const int32_t* before = a.sched + kSchedHeader;
-    seen = before[t] != before[t + 1];
-    if (!seen && row_state(a, t).bad) fill = NAN;
-    if (seen && fix) lse = a.lse[th];
-    if (!seen) lse = fill == 0.f ? -INFINITY : NAN;
-  }
-  // step i of this wave: columns 16 (NST wave + i) + {4 g .. + 3, 8 + 4 g .. + 3}
-  const int c0 = 16 * NST * wave + 4 * g;
-  f32x4 x[NST][2];
-#pragma unroll
-  for (int i = 0; i < NST; ++i) {
-    x[i][0] = x[i][1] = f32x4{fill, fill, fill, fill};
-    if (seen && 16 * (NST * wave + i) < dc) {
-      x[i][0] = *reinterpret_cast<const f32x4*>(a.obar + th * dc + c0 + 16 * i);
-      x[i][1] = *reinterpret_cast<const f32x4*>(a.obar + th * dc + c0 + 16 * i + 8);
-    }
-  }
-  if (fix) {
-    float dot = 0.f;
-    if (seen) {
-      const T* q = (const T*)lse_lacks(a) + th * (dc + a.d_rope) + c0;
-#pragma unroll
-      for (int i = 0; i < NST; ++i)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          if (16 * (NST * wave + i) >= dc) continue;
-          typedef typename FragOf<T>::half quad;
-          const quad y = *reinterpret_cast<const quad*>(q + 16 * i + 8 * u);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) dot = __builtin_fmaf(x[i][u][e], to_f32(y[e]), dot);
-        }
-    }
-    dot = wave_xor32_sum(dot);
-    if (g == 0) s_dot[wave][n] = dot;
-  }
-
   wait_vmem();
   lds_barrier();
-  f32x16 acc[NB];
+  for (int turn = 0;; turn ^= 1) {
+    const int64_t th = (int64_t)t * a.H + h;
+    const bool more = t - n + step < a.T;
+    const Row third = row(t + 2 * step);
+    float lse = now.fill == 0.f ? -INFINITY : NAN;
+    if (fix) {
+      if (now.seen) lse = a.lse[th];
+      float dot = 0.f;
+      if constexpr (kTwo<T>)
+        if (now.seen)
 #pragma unroll
-  for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
+          for (int i = 0; i < NST; ++i)
 #pragma unroll
-  for (int i = 0; i < NST; ++i) {
-    const int ks = NST * wave + i;
-    if (16 * ks >= dc) continue;  // wave-uniform
-    frag_t<T> hi, lo;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      hi[e] = to_elem<T>(x[i][e / 4][e % 4]);
-      lo[e] = to_elem<T>(x[i][e / 4][e % 4] - to_f32(hi[e]));
+            for (int e = 0; e < 8; ++e)
+              if (16 * (NST * wave + i) < dc) dot = __builtin_fmaf(x[i][e / 4][e % 4], to_f32(y[i][e / 4][e % 4]), dot);
+      dot = wave_xor32_sum(dot);
+      if (g == 0) s_dot[turn][wave][n] = dot;
     }
+    f32x16 acc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
+#pragma unroll
+    for (int i = 0; i < NST; ++i) {
+      const int ks = NST * wave + i;
+      if (16 * ks >= dc) continue;  // wave-uniform
+      frag_t<T> hi, lo;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        hi[e] = to_elem<T>(x[i][e / 4][e % 4]);
+        lo[e] = to_elem<T>(x[i][e / 4][e % 4] - to_f32(hi[e]));
+      }
+      if (more) load(i, t + step, next);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int ra = 16 * ks + 4 * g;
+        frag_t<T> wf;
+        if constexpr (sizeof(T) == 2) wf = swz_tr_frag<CPR>((const bf16*)sw, ra, ra + 8, 32 * b);
+        else wf = TrRead<float>::get((const float*)sw, 32 * NB, ra, ra + 8, 32 * b);
+        mma(acc[b], wf, hi);
+        if constexpr (kTwo<T>) mma(acc[b], wf, lo);
+      }
+    }
+    // the waves' sums, a block of columns at a time; each wave adds up a quarter
+    T* o = (T*)a.out + th * DV + 32 * NB * vb + 4 * g;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const int ra = 16 * ks + 4 * g;
-      frag_t<T> wf;
-      if constexpr (sizeof(T) == 2) wf = swz_tr_frag<CPR>((const bf16*)sw, ra, ra + 8, 32 * b);
-      else wf = TrRead<float>::get((const float*)sw, 32 * NB, ra, ra + 8, 32 * b);
-      mma(acc[b], wf, hi);
-      if constexpr (kTwo<T>) mma(acc[b], wf, lo);
+      lds_barrier();  // the block before is read
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+        red[(wave * 4 + rr) * 64 + l] = f32x4{acc[b][4 * rr], acc[b][4 * rr + 1], acc[b][4 * rr + 2], acc[b][4 * rr + 3]};
+      lds_barrier();
+      f32x4 y = red[wave * 64 + l];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) y += red[(w * 4 + wave) * 64 + l];
+      quad z;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[e] = to_elem<T>(y[e]);
+      if (t < a.T) *reinterpret_cast<quad*>(o + 32 * b + 8 * wave) = z;
     }
-  }
-  lds_barrier();  // W_v is read
-  f32x4* red = (f32x4*)smem;
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int rr = 0; rr < 4; ++rr)
-      red[((wave * NB + b) * 4 + rr) * 64 + l] = f32x4{acc[b][4 * rr], acc[b][4 * rr + 1], acc[b][4 * rr + 2], acc[b][4 * rr + 3]};
-  lds_barrier();
-  if (t >= a.T) return;
-  if (a.lse && vb == 0 && wave == 0 && g == 0 && (fix || !seen)) {
-    if (fix && seen) lse += (((s_dot[0][n] + s_dot[1][n]) + s_dot[2][n]) + s_dot[3][n]) * a.scale_log2 * kLn2;
-    a.lse[th] = lse;
-  }
-  // 4 NB groups of four columns per lane, dealt to the waves
-  T* o = (T*)a.out + th * DV + 32 * NB * vb + 4 * g;
-#pragma unroll
-  for (int u = 0; u < NB; ++u) {
-    const int i = wave + 4 * u, b = i / 4, rr = i % 4;
-    f32x4 y = red[(b * 4 + rr) * 64 + l];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) y += red[((w * NB + b) * 4 + rr) * 64 + l];
-    typename FragOf<T>::half z;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = to_elem<T>(y[e]);
-    *reinterpret_cast<typename FragOf<T>::half*>(o + 32 * b + 8 * rr) = z;
+    if (t < a.T && a.lse && vb == 0 && wave == 0 && g == 0 && (fix || !now.seen)) {
+      const float(*d)[32] = s_dot[turn];
+      if (fix && now.seen) lse += (((d[0][n] + d[1][n]) + d[2][n]) + d[3][n]) * a.scale_log2 * kLn2;
+      a.lse[th] = lse;
+    }
+    if (!more) return;
+    t += step;
+    now = next;
+    next = third;
   }
 }
 
 template <typename T, int DV, int NB>
 void launch_join_product(const PagedArgs& a, hipStream_t st) {
-  const int tb = (a.T + 31) / 32;
-  const unsigned wgs = (unsigned)((int64_t)a.H * (DV / (32 * NB)) * tb);
-  const size_t w = (size_t)a.d_c * 32 * NB * sizeof(T), red = (size_t)NB * 16384, lds = w > red ? w : red;
-  if (a.d_c <= 128) join_kernel<T, DV, NB, 2><<<wgs, 256, lds, st>>>(a, tb);
-  else if (a.d_c <= 256) join_kernel<T, DV, NB, 4><<<wgs, 256, lds, st>>>(a, tb);
-  else if (a.d_c <= 512) join_kernel<T, DV, NB, 8><<<wgs, 256, lds, st>>>(a, tb);
-  else join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, tb);
+  const size_t lds = kJoinRed + (size_t)a.d_c * 32 * NB * sizeof(T);
+  const int64_t blocks = (int64_t)a.H * (DV / (32 * NB));
+  const int tb = (a.T + 31) / 32, want = (int)((kCus * (160 * 1024 / lds) + blocks - 1) / blocks);  // what runs at once
+  const int tparts = tb < want ? tb : want;
+  const unsigned wgs = (unsigned)(blocks * tparts);
+  if (a.d_c <= 128) join_kernel<T, DV, NB, 2><<<wgs, 256, lds, st>>>(a, tparts);
+  else if (a.d_c <= 256) join_kernel<T, DV, NB, 4><<<wgs, 256, lds, st>>>(a, tparts);
+  else if (NB > 1 || a.d_c <= 512) join_kernel<T, DV, NB, 8><<<wgs, 256, lds, st>>>(a, tparts);
+  else if constexpr (NB == 1) join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, tparts);
 }
 
 // The same for one row and head per workgroup, partials and all, in fp32: where there are no more of
@@ -523,12 +550,15 @@ void launch_join(const PagedArgs& a, hipStream_t st) {
     else join_vec_kernel<T, DV, 1024><<<(unsigned)pairs, 1024, 0, st>>>(a);
     return;
   }
-  combine_kernel<<<(unsigned)pairs, kCombineThreads, 0, st>>>(a);
+  // one head per workgroup; eight where most rows cannot be shared, being more than the workers (300 rows, 128
+  // heads: 24 us and 15; 61 rows 20 and 23)
+  if (a.T > a.workers) combine_kernel<8><<<(unsigned)((int64_t)a.T * ((a.H + 7) / 8)), kCombineThreads, 0, st>>>(a);
+  else combine_kernel<1><<<(unsigned)pairs, kCombineThreads, 0, st>>>(a);
   // all of out's columns in one workgroup (o is then read once) where W_v's rows of a head fit in
   // LDS and heads and rows alone fill half of the GPU
   constexpr int NB = DV / 32;
-  if (sizeof(T) == 2 && NB > 1 && a.d_c <= 512 && (int64_t)a.H * ((a.T + 31) / 32) >= kCus / 2)
-    return launch_join_product<T, DV, NB>(a, st);
+  if constexpr (sizeof(T) == 2 && NB > 1)
+    if (a.d_c <= 512 && (int64_t)a.H * ((a.T + 31) / 32) >= kCus / 2) return launch_join_product<T, DV, NB>(a, st);
   launch_join_product<T, DV, 1>(a, st);
 }
 
