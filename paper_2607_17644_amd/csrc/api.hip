@@ -244,6 +244,7 @@ laga_status_t page_plan(const laga_paged_t* p, bool release, const int32_t* leng
   a.lengths_out = lengths_out; a.free_count_out = free_count_out; a.row_begin = row_begin;
   a.row_request = row_request; a.position = position; a.slot = slot; a.status = status; a.ws = (int32_t*)workspace;
   a.rows = d.T; a.R = d.R; a.width = d.width; a.n_pages = d.n_pages; a.page = d.page; a.release = release;
+  page_division(d.page, &a.page_magic, &a.page_shift);
   return from_hip(launch_plan(a, (hipStream_t)stream));
 }
 

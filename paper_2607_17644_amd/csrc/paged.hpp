@@ -27,8 +27,9 @@ struct PlanArgs {
   int32_t* ws;                // plan_ws_ints(R)
   int rows, R, width, n_pages, page;
   int release;
+  uint32_t page_magic, page_shift;  // key / page = key page_magic >> page_shift
 };
-// workspace: [count, pages, rows, ok] then pages_before[R + 1] and the lengths as they were [R]
+// workspace of a plan or release in two launches: [count, pages, rows, -] then pages_before[R + 1] and the lengths as they were [R]
 constexpr int kPlanHeader = 4;
 inline size_t plan_ws_ints(long long R) { return kPlanHeader + (size_t)(R + 1) + (size_t)R; }
 hipError_t launch_plan(const PlanArgs& a, hipStream_t st);

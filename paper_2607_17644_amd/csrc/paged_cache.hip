@@ -19,20 +19,27 @@ constexpr int kScanChunk = kScanThreads * kScanPer;
 constexpr int kFillThreads = 256;
 constexpr int kSearchLds = 4096;  // sums of this many requests are searched in LDS
 
-__device__ __forceinline__ int pages_of(int64_t n, int page) { return (int)((n + page - 1) / page); }
+__device__ __forceinline__ int page_of(const PlanArgs& a, int key) {
+  return (int)((uint64_t)(uint32_t)key * a.page_magic >> a.page_shift);
+}
+__device__ __forceinline__ int pages_of(const PlanArgs& a, int n) { return page_of(a, n + a.page - 1); }
 
-// Exclusive sums over the workgroup of (rows, pages) per thread; total[] gets the workgroup's.
-__device__ void block_scan(int64_t& rows, int64_t& pages, int64_t (&total)[2], int64_t (*sm)[2]) {
+// Exclusive sums over the workgroup of (rows, pages) per thread; total[] gets the workgroup's. (Pages are at
+// most requests x table width, below 2^31.)
+__device__ void block_scan(int64_t& rows, int& pages, int64_t (&total)[2], int64_t (*sm)[2]) {
   const int l = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t r = rows, p = pages;
+  int64_t r = rows;
+  int p = pages;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t r1 = __shfl_up(r, o), p1 = __shfl_up(p, o);
+    const int64_t r1 = __shfl_up(r, o);
+    const int p1 = __shfl_up(p, o);
     if (l >= o) { r += r1; p += p1; }
   }
   if (l == 63) { sm[wave][0] = r; sm[wave][1] = p; }
   __syncthreads();
   int64_t rb = 0, pb = 0, rt = 0, pt = 0;
+#pragma unroll
   for (int w = 0; w < kScanThreads / 64; ++w) {
     if (w == wave) { rb = rt; pb = pt; }
     rt += sm[w][0];
@@ -41,7 +48,7 @@ __device__ void block_scan(int64_t& rows, int64_t& pages, int64_t (&total)[2], i
   __syncthreads();
   total[0] = rt; total[1] = pt;
   rows = rb + r - rows;
-  pages = pb + p - pages;
+  pages = (int)pb + p - pages;
 }
 
 // last r in [0, n) with sums[r] <= k (sums[0] = 0 <= k < the whole sum: the request of item k)
@@ -54,29 +61,32 @@ __device__ __forceinline__ int find_request(const int32_t* sums, int n, int k) {
   return lo;
 }
 
-// Rows and pages first, first + step, ... of the plan or release that the sums describe.
-__device__ void expand(const PlanArgs& a, const int32_t* pages_before, const int32_t* row_begin, int first, int step) {
-  const int32_t* head = a.ws;
-  const int32_t* lengths = a.ws + kPlanHeader + a.R + 1;
-  const int count = head[0], n_pages = head[1], n_rows = head[2];
-  for (int k = first; k < n_pages; k += step) {
-    const int r = find_request(pages_before, a.R, k), j = k - pages_before[r];
+// What a plan or release hands out, and where to find it: sums and the lengths before the step, by request.
+struct Handout {
+  const int32_t *pages_before, *row_begin, *lengths;
+  int count, pages, rows;
+};
+// Rows and pages first, first + step, ... of it.
+__device__ __forceinline__ void expand(const PlanArgs& a, const Handout& x, int first, int step) {
+  for (int k = first; k < x.pages; k += step) {
+    const int r = find_request(x.pages_before, a.R, k), j = k - x.pages_before[r];
     int32_t* entry = a.table + (int64_t)r * a.width + j;
-    if (a.release) a.free_pages[count + k] = *entry;
-    else entry[pages_of(lengths[r], a.page)] = a.free_pages[count - 1 - k];
+    if (a.release) a.free_pages[x.count + k] = *entry;
+    else entry[pages_of(a, x.lengths[r])] = a.free_pages[x.count - 1 - k];
   }
   if (a.release) return;
   for (int t = first; t < a.rows; t += step) {
     int request = -1, position = -1, slot = -1;
-    if (t < n_rows) {
-      request = find_request(row_begin, a.R, t);
-      const int len = lengths[request];
-      position = len + t - row_begin[request];
+    if (t < x.rows) {
+      request = find_request(x.row_begin, a.R, t);
+      const int len = x.lengths[request];
+      position = len + t - x.row_begin[request];
       // the entry in the table, or the page that this step puts there
-      const int j = position / a.page, have = pages_of(len, a.page);
-      const int id = j < have ? a.table[(int64_t)request * a.width + j]
-                              : a.free_pages[count - 1 - (pages_before[request] + j - have)];
-      if ((unsigned)id < (unsigned)a.n_pages) slot = id * a.page + position % a.page;
+      const int j = page_of(a, position), have = pages_of(a, len);
+      const int32_t* from = j < have ? a.table + (int64_t)request * a.width + j
+                                     : a.free_pages + (x.count - 1 - (x.pages_before[request] + j - have));
+      const int id = *from;
+      if ((unsigned)id < (unsigned)a.n_pages) slot = id * a.page + (position - j * a.page);
     }
     a.row_request[t] = request;
     a.position[t] = position;
@@ -84,53 +94,60 @@ __device__ void expand(const PlanArgs& a, const int32_t* pages_before, const int
   }
 }
 
-// FILL: this workgroup also expands the sums (small steps: one launch).
+// FILL: this workgroup also expands the sums (small steps: one launch), from LDS up to kSearchLds requests.
 template <bool FILL>
 __global__ __launch_bounds__(kScanThreads) void plan_scan_kernel(PlanArgs a) {
   __shared__ int64_t sm[kScanThreads / 64][2];
   __shared__ int bad;
-  __shared__ int32_t s_pages[FILL ? kSearchLds : 1], s_rows[FILL ? kSearchLds : 1];
+  __shared__ int32_t s_pages[FILL ? kSearchLds : 1], s_rows[FILL ? kSearchLds : 1], s_lengths[FILL ? kSearchLds : 1];
   int32_t* pages_before = a.ws + kPlanHeader;
   int32_t* lengths = pages_before + a.R + 1;
+  const bool lds = FILL && a.R <= kSearchLds;
   const int tid = threadIdx.x, count = a.free_count[0];
   const int64_t room = (int64_t)a.width * a.page;
   if (tid == 0) bad = 0;
-  __syncthreads();
 
   int64_t rows0 = 0, pages0 = 0;
+  int len[kScanPer], arg[kScanPer];
   for (int64_t base = 0; base < a.R; base += kScanChunk) {
-    int64_t rows = 0, pages = 0;
-    int f[kScanPer], n[kScanPer], err = 0;
+    int64_t rows = 0;
+    int f[kScanPer], n[kScanPer], pages = 0, err = 0;
 #pragma unroll
     for (int i = 0; i < kScanPer; ++i) {
       const int64_t r = base + tid * kScanPer + i;
+      len[i] = arg[i] = 0;
+      if (r < a.R) len[i] = a.lengths[r], arg[i] = a.arg[r];
+    }
+#pragma unroll
+    for (int i = 0; i < kScanPer; ++i) {
       f[i] = n[i] = 0;
-      if (r < a.R) {
-        const int len = a.lengths[r], arg = a.arg[r];
-        lengths[r] = len;
-        if (len < 0 || (!a.release && arg < 0)) err |= LAGA_PLAN_INVALID;
-        else if (len + (a.release ? 0 : (int64_t)arg) > room) err |= LAGA_PLAN_TABLE;
-        else if (a.release) n[i] = arg ? pages_of(len, a.page) : 0;
-        else {
-          f[i] = arg;
-          n[i] = pages_of((int64_t)len + arg, a.page) - pages_of(len, a.page);
-        }
+      if (len[i] < 0 || (!a.release && arg[i] < 0)) err |= LAGA_PLAN_INVALID;
+      else if (len[i] + (a.release ? 0 : (int64_t)arg[i]) > room) err |= LAGA_PLAN_TABLE;
+      else if (a.release) n[i] = arg[i] ? pages_of(a, len[i]) : 0;
+      else {
+        f[i] = arg[i];
+        n[i] = pages_of(a, len[i] + arg[i]) - pages_of(a, len[i]);
       }
       rows += f[i];
       pages += n[i];
     }
-    if (err) atomicOr(&bad, err);  // (bits of a set: no order)
+    if (base == 0) __syncthreads();  // bad is cleared
+    if (err) atomicOr(&bad, err);    // (bits of a set: no order)
     int64_t total[2];
     block_scan(rows, pages, total, sm);
     rows += rows0;
-    pages += pages0;
+    pages += (int)pages0;
 #pragma unroll
     for (int i = 0; i < kScanPer; ++i) {
       const int64_t r = base + tid * kScanPer + i;
       if (r < a.R) {  // (sums past 2^31 end in an error below: nothing reads them)
-        pages_before[r] = (int32_t)pages;
         if (!a.release) a.row_begin[r] = (int32_t)rows;
-        if (FILL && r < kSearchLds) { s_pages[r] = (int32_t)pages; s_rows[r] = (int32_t)rows; }
+        if (lds) {
+          s_pages[r] = pages, s_rows[r] = (int32_t)rows, s_lengths[r] = len[i];
+        } else {
+          pages_before[r] = pages;
+          lengths[r] = len[i];
+        }
       }
       rows += f[i];
       pages += n[i];
@@ -144,25 +161,29 @@ __global__ __launch_bounds__(kScanThreads) void plan_scan_kernel(PlanArgs a) {
   else if (a.release ? count + pages0 > a.n_pages : pages0 > count) status |= LAGA_PLAN_PAGES;
   if (!a.release && rows0 > a.rows) status |= LAGA_PLAN_ROWS;
   const bool ok = status == 0;
+  const int n_pages = ok ? (int)pages0 : 0, n_rows = ok ? (int)rows0 : 0;
+  if constexpr (FILL) {  // (apart, so that LDS is read as LDS)
+    if (lds) expand(a, Handout{s_pages, s_rows, s_lengths, count, n_pages, n_rows}, tid, kScanThreads);
+    else expand(a, Handout{pages_before, a.row_begin, lengths, count, n_pages, n_rows}, tid, kScanThreads);
+  }
 
   // the state after the step (every input has been read)
-  for (int64_t r = tid; r < a.R; r += kScanThreads) {
-    const int len = lengths[r];
-    a.lengths_out[r] = !ok ? len : a.release ? (a.arg[r] ? 0 : len) : len + a.arg[r];
+  auto state = [&](int64_t r, int len, int arg) {
+    a.lengths_out[r] = !ok ? len : a.release ? (arg ? 0 : len) : len + arg;
     if (!a.release && !ok) a.row_begin[r] = 0;
+  };
+  if (a.R <= kScanChunk) {
+#pragma unroll
+    for (int i = 0; i < kScanPer; ++i)
+      if (tid * kScanPer + i < a.R) state(tid * kScanPer + i, len[i], arg[i]);
+  } else {
+    for (int64_t r = tid; r < a.R; r += kScanThreads) state(r, lengths[r], a.arg[r]);
   }
   if (tid == 0) {
-    a.ws[0] = count;
-    a.ws[1] = ok ? (int32_t)pages0 : 0;
-    a.ws[2] = ok ? (int32_t)rows0 : 0;
+    if (!FILL) a.ws[0] = count, a.ws[1] = n_pages, a.ws[2] = n_rows;
     a.status[0] = status;
     a.free_count_out[0] = !ok ? count : a.release ? count + (int32_t)pages0 : count - (int32_t)pages0;
-    if (!a.release) a.row_begin[a.R] = ok ? (int32_t)rows0 : 0;
-  }
-  if constexpr (FILL) {
-    __syncthreads();
-    const bool lds = a.R <= kSearchLds;
-    expand(a, lds ? s_pages : pages_before, lds ? s_rows : a.row_begin, tid, kScanThreads);
+    if (!a.release) a.row_begin[a.R] = n_rows;
   }
 }
 
@@ -177,8 +198,10 @@ __global__ __launch_bounds__(kFillThreads) void plan_fill_kernel(PlanArgs a) {
     }
     __syncthreads();
   }
-  expand(a, lds ? s_pages : pages_before, lds ? s_rows : a.row_begin, blockIdx.x * kFillThreads + threadIdx.x,
-         gridDim.x * kFillThreads);
+  const int32_t* lengths = pages_before + a.R + 1;
+  const int first = blockIdx.x * kFillThreads + threadIdx.x, step = gridDim.x * kFillThreads;
+  if (lds) expand(a, Handout{s_pages, s_rows, lengths, a.ws[0], a.ws[1], a.ws[2]}, first, step);
+  else expand(a, Handout{pages_before, a.row_begin, lengths, a.ws[0], a.ws[1], a.ws[2]}, first, step);
 }
 
 // ---------------------------------------------------------------- rows of new tokens
