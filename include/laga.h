@@ -403,10 +403,11 @@ LAGA_API laga_status_t laga_cache_append(const laga_paged_t* p, const laga_prolo
  * has been. row_request NULL: row t is request t. A row at a negative position sees nothing:
  * out 0, lse -infinity. Any number of rows may belong to one request.
  * The product with W_kv_b's K columns is taken on the query's side and the one with its V
- * columns after the softmax. Statistics, sums and joins of a row's parts are fp32; of the
- * values in between nothing is rounded to fewer than 16 bits of mantissa in bf16, so out is
- * the exact result rounded once, to little more than that. Workspace:
- * laga_paged_workspace_bytes(p, LAGA_OP_PAGED_ATTN). */
+ * columns after the softmax. Statistics, sums and joins of a row's parts are fp32. In bf16 the
+ * values in between keep 16 bits of mantissa or more, so out is the exact result rounded once, to
+ * little more than that; but with d_c = 512, d_rope = 64 and rows of many keys the query's product
+ * with the K columns enters the scores with 8 (its rest enters lse, to first order): out is then off
+ * by about 1.4 roundings. Workspace: laga_paged_workspace_bytes(p, LAGA_OP_PAGED_ATTN). */
 LAGA_API laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg,
                                        const void* q, const void* w_kv_b, const void* cache,
                                        const int32_t* block_table, const int32_t* row_request,
