@@ -327,8 +327,9 @@ LAGA_API size_t laga_out_proj_workspace_bytes(const laga_out_proj_t* p);
  *     rows' lengths and on n_heads.
  * Limits: head dims and d_c as for the attention calls; page_size >= 1; page_stride 0 (read
  * as page_size * (d_c + d_rope)) or at least that and a multiple of 8; n_pages * page_size,
- * requests * table_width, rows * n_heads, rows * table_width * page_size / 32 and
- * 16 * d_c * n_heads * (d_nope + d_v) below 2^31; table_width * page_size at most 2^30;
+ * requests * table_width, rows * n_heads, rows * (table_width * page_size / 32 + 10) and
+ * 16 * d_c * n_heads * (d_nope + d_v) below 2^31;
+ * table_width * page_size at most 2^30; rows below 2^22, rows * ceil(n_heads / 8) below 2^24;
  * else LAGA_ERR_UNSUPPORTED. A size <= 0 is LAGA_ERR_SHAPE. */
 typedef struct {
   int64_t rows;        /* T: new tokens of the step, rows of padding included */

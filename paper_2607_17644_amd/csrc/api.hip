@@ -186,8 +186,10 @@ laga_status_t validate_paged(const laga_paged_t* p, PagedDims* d) {
     if (x >= kMaxElems) return LAGA_ERR_UNSUPPORTED;
   const int64_t cap = p->table_width * p->page_size, row = p->d_c + p->d_rope;
   if (cap > kMaxElems / 2 || p->n_pages * p->page_size >= kMaxElems || p->requests * p->table_width >= kMaxElems ||
-      p->rows * p->n_heads >= kMaxElems || p->rows * ((cap + kTileKeys - 1) / kTileKeys) >= kMaxElems)
+      p->rows * p->n_heads >= kMaxElems || p->rows * ((cap + kTileKeys - 1) / kTileKeys + kWideRowCost) >= kMaxElems)
     return LAGA_ERR_UNSUPPORTED;
+  // what a launch's 2^32 threads hold at a workgroup of 512 per row, or 256 per row and eight heads
+  if (p->rows >= (1 << 22) || p->rows * ((p->n_heads + 7) / 8) >= (1 << 24)) return LAGA_ERR_UNSUPPORTED;
   if (p->page_stride != 0 && (p->page_stride < p->page_size * row || p->page_stride % 8 != 0 ||
                               p->page_stride >= (int64_t)1 << 40))
     return p->page_stride < p->page_size * row ? LAGA_ERR_SHAPE : LAGA_ERR_UNSUPPORTED;

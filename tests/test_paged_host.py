@@ -56,7 +56,8 @@ BAD = [(2, kw) for kw in (dict(rows=0), dict(requests=-1), dict(table_width=0), 
                           dict(rows=1 << 31), dict(rows=BIG), dict(requests=BIG), dict(table_width=BIG),
                           dict(n_pages=BIG), dict(page_size=BIG), dict(n_heads=BIG), dict(n_heads=1024),
                           dict(n_pages=1 << 25), dict(table_width=(1 << 24) + 1), dict(requests=1 << 27),
-                          dict(rows=1 << 27), dict(rows=1 << 26, table_width=17), dict(page_stride=64 * 576 + 4),
+                          dict(rows=1 << 27), dict(rows=1 << 26, table_width=17), dict(rows=1 << 22, table_width=1),
+                          dict(rows=1 << 20, table_width=1, n_heads=128), dict(page_stride=64 * 576 + 4),
                           dict(page_stride=1 << 41))]
 
 
