@@ -103,19 +103,30 @@ constexpr size_t absorb_lds() {
   return sizeof(T) * (size_t)(kAbsorbRows + 32) * DN + sizeof(float) * 32 * (kAbsorbRows + 4);
 }
 
-// q_rope of one token, every head: a thread keeps one pair's angle
+// q_rope of one token, every head: a thread keeps one pair's angle and has eight heads' pairs under way (one
+// after the other, the launch took 11 us for 2 rows of 128 heads, so 7)
+constexpr int kBandHeads = 8;
 template <typename T>
 __device__ void absorb_band(const PagedArgs& a, int t) {
   const int pairs = a.d_rope / 2, i = threadIdx.x % pairs;
   const int W = a.d_c + a.d_rope, dqk = a.d_nope + a.d_rope;
   float cs = 1.f, sn = 0.f;
   if (a.rotate) rope_sincos(a.position_offset + a.position[t], rope_freq(i, a.d_rope, a.log2_base), cs, sn);
-  for (int h = threadIdx.x / pairs; h < a.H; h += 64 * kAbsorbWaves / pairs) {
-    const T* x = (const T*)a.q + ((int64_t)t * a.H + h) * dqk + a.d_nope + 2 * i;
-    const int64_t at = ((int64_t)t * a.H + h) * W + a.d_c + 2 * i;
-    const float x0 = to_f32(x[0]), x1 = to_f32(x[1]);
-    const float y[2] = {x0 * cs - x1 * sn, x0 * sn + x1 * cs};
-    store_parts<T, 2>(a, at, y);
+  typedef __attribute__((__vector_size__(2 * sizeof(T)))) T pair;
+  const int step = 64 * kAbsorbWaves / pairs;
+  for (int h0 = threadIdx.x / pairs; h0 < a.H; h0 += kBandHeads * step) {
+    pair x[kBandHeads];
+#pragma unroll
+    for (int u = 0; u < kBandHeads; ++u)
+      if (h0 + u * step < a.H)
+        x[u] = *reinterpret_cast<const pair*>((const T*)a.q + ((int64_t)t * a.H + h0 + u * step) * dqk + a.d_nope + 2 * i);
+#pragma unroll
+    for (int u = 0; u < kBandHeads; ++u) {
+      if (h0 + u * step >= a.H) break;
+      const float x0 = to_f32(x[u][0]), x1 = to_f32(x[u][1]);
+      const float y[2] = {x0 * cs - x1 * sn, x0 * sn + x1 * cs};
+      store_parts<T, 2>(a, ((int64_t)t * a.H + h0 + u * step) * W + a.d_c + 2 * i, y);
+    }
   }
 }
 
