@@ -139,6 +139,8 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
       }
     };
     const char* flat = nullptr;  // the tile's first row, where the copies are left to the caller
+    int ahead = 0;               // and the id of its first page, read from the window beforehand
+    auto look = [&](int it) { ahead = win_ids[min((uint32_t)(page_of(it * kTileKeys) - win), kPages - 1u)]; };
     auto fetch = [&](int it, bf16* buf, bool at_once) -> uint32_t {
       const int l = fresh_lane(), n = l & 31;
       const int k0 = it * kTileKeys, p0 = page_of(k0), o0 = k0 - p0 * a.page;
@@ -150,10 +152,11 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
         for (int i = l; i < kPages; i += 64) win_ids[i] = win + i < have ? pages[win + i] : -1;
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
+        if (!at_once) look(it);
       }
       flat = nullptr;
       if (HG > 1 && k0 + kTileKeys <= visible && o0 + kTileKeys <= a.page) {
-        const int pid = uniform(win_ids[p0 - win]);
+        const int pid = uniform(at_once ? win_ids[p0 - win] : ahead);
         if ((unsigned)pid < (unsigned)a.n_pages) {
           const char* base = uniform((const char*)((const bf16*)a.cache + (int64_t)pid * a.page_stride + (int64_t)o0 * kRow));
           if (at_once) {
@@ -330,6 +333,7 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
       products(reads_of(ring), s, [](int) {});
       scores_done(s);
       mask(it0, bad0, s);
+      look(it0 + 3);
       for (int step = 0; step < steps; ++step) {
         const int it = it0 + step;
         wait_vmem_le<NCOPY>();
@@ -361,9 +365,10 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
         });
         lsum += ps;
         accumulate(reads_of(ring + (step & 3) * kTile), pf, pl, [&](int i) {
+          if (i == 48) look(it + 4);
           if (i % 4 == 1 && i / 4 < NCOPY && flat) copy(flat, ring + (step + 3 & 3) * kTile, i / 4, fresh_lane());
         });
-        scores_done(next);
+        asm volatile("" : "+v"(next));  // (its products are done long ago)
         mask(it + 1, bad1, next);
         s = next;
         bad1 = bad2;
