@@ -485,7 +485,14 @@ __global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
   for (int i = 0; i < kVecRows; ++i)
     if (slice + i * SLICES < dc) wr[i] = *reinterpret_cast<const chunk_t*>(w + (slice + i * SLICES) * ldw);
   const RowParts r = parts_of(a, t);
-  const bool fix = kTwo<T> && a.lse;
+  // what lse lacks, in the first wave
+  float lack[2][8] = {};
+  if (kTwo<T> && a.lse && tid < 64 && r.seen) {
+    const T* q = (const T*)lse_lacks(a) + th * (dc + a.d_rope);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (8 * tid + 512 * k < dc) load8(q + 8 * tid + 512 * k, lack[k]);
+  }
   const int quads = dc / 4, groups = NT / quads, group = tid / quads, c = tid % quads * 4;
   float lse = -INFINITY;
   if (r.split) {
@@ -510,14 +517,12 @@ __global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
   __syncthreads();
   if (a.lse && tid < 64) {
     float dot = 0.f;
-    if (fix && r.seen) {
-      const T* q = (const T*)lse_lacks(a) + th * (dc + a.d_rope);
-      for (int i = 8 * tid; i < dc; i += 512) {
-        float x[8];
-        load8(q + i, x);
+    if (kTwo<T> && r.seen) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(s_o[i + e], x[e], dot);
-      }
+      for (int k = 0; k < 2; ++k)
+        if (8 * tid + 512 * k < dc)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(s_o[8 * tid + 512 * k + e], lack[k][e], dot);
 #pragma unroll
       for (int o = 32; o >= 1; o >>= 1) dot += __shfl_xor(dot, o);
     }
