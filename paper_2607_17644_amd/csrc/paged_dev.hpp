@@ -27,6 +27,13 @@ __device__ __forceinline__ RowState row_state(const PagedArgs& a, int t) {
   return {r, p + 1, false};
 }
 
+// The lane, formed anew wherever it is asked for: values derived from one kept all the way would fill
+// the registers, and a spilled one's reload waits for the copies in flight.
+__device__ __forceinline__ int fresh_lane() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
 // What is the same in every lane, in scalar registers.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ const char* uniform(const char* p) {

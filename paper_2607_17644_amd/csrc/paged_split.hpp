@@ -57,20 +57,23 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
   // copy j's lane: chunk c of the tile's row; and its place in a tile whose rows follow each other
   constexpr int NJ = (C::NI + 3) / 4;
   constexpr uint32_t kNoPlace = ~0u;
-  auto chunk_of = [&](int j, int& row, int& c) {
-    const int p = j * 64 + l;
+  auto chunk_of = [&](int j, int lane, int& row, int& c) {
+    const int p = j * 64 + lane;
     row = p / P;
     c = p - row * P;
     if (C::NI * 64 > kTileKeys * P && row >= kTileKeys) row = 0, c = 0;
     if constexpr (sizeof(T) == 2) c ^= swz<24>(row);
   };
-  uint32_t place[NJ];
-#pragma unroll
-  for (int jj = 0; jj < NJ; ++jj) {
+  auto place_of = [&](int jj, int lane) {
     int row, c;
-    chunk_of(wave + 4 * jj, row, c);
-    place[jj] = c * E < W ? (uint32_t)(row * W * (int)sizeof(T) + c * 16) : kNoPlace;
-  }
+    chunk_of(wave + 4 * jj, lane, row, c);
+    return c * E < W ? (uint32_t)(row * W * (int)sizeof(T) + c * 16) : kNoPlace;
+  };
+  // (d_c above 512: formed anew for each copy, for want of registers to keep them in)
+  uint32_t place[ND > 4 ? 1 : NJ];
+  if constexpr (ND <= 4)
+#pragma unroll
+    for (int jj = 0; jj < NJ; ++jj) place[jj] = place_of(jj, l);
 
   for (int at = max((int)start, share.first);;) {
     const int t = share.t, row_first = share.first, row_end = share.end;
@@ -114,8 +117,10 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
 #pragma unroll
       for (int i = 0; i < kPerSlot; ++i) {
         const int jj = slot * kPerSlot + i, j = wave + 4 * jj;
-        if (jj < NJ && (C::NI % 4 == 0 || j < C::NI))
-          g2lds16(place[jj < NJ ? jj : 0] == kNoPlace ? (const char*)kZeroRow : flat + place[jj < NJ ? jj : 0], flat_to + j * 64 * E);
+        if (jj < NJ && (C::NI % 4 == 0 || j < C::NI)) {
+          const uint32_t at = ND > 4 ? place_of(jj, fresh_lane()) : place[jj < NJ && ND <= 4 ? jj : 0];
+          g2lds16(at == kNoPlace ? (const char*)kZeroRow : flat + at, flat_to + j * 64 * E);
+        }
       }
     };
     auto fetch = [&](int it, int st, bool at_once) {
@@ -147,13 +152,14 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
       const T* src = ok ? (const T*)a.cache + (int64_t)pid * a.page_stride + (int64_t)off * W : (const T*)kZeroRow;
       const uint32_t bad = (uint32_t)__ballot(live && !ok);
       if (threadIdx.x == 0) s_bad[st] = bad;
+      const int lane = ND > 4 ? fresh_lane() : l;
       const uint32_t lo = (uint32_t)(uintptr_t)src, hi = (uint32_t)((uintptr_t)src >> 32);
 #pragma unroll
       for (int jj = 0; jj < NJ; ++jj) {
         const int j = wave + 4 * jj;
         if (C::NI % 4 == 0 || j < C::NI) {
           int row, c;
-          chunk_of(j, row, c);
+          chunk_of(j, lane, row, c);
           const uintptr_t base = (uintptr_t)(uint32_t)__shfl((int)lo, row) |
                                  ((uintptr_t)(uint32_t)__shfl((int)hi, row) << 32);
           const unsigned char* from = c * E < W ? (const unsigned char*)base : kZeroRow;
@@ -188,13 +194,16 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
         if (it + NS - 1 < it1) fetch(it + NS - 1, st == 0 ? NS - 1 : st - 1, false);
       }
       const T* tile = ring + st * C::TILE;
+      // d_c above 512: addresses are formed anew in each tile, for want of registers to keep them in (64 requests
+      // x 4000 keys, 16 heads, d_c = 1024: 94 us, 235 with them and what they spilled)
+      const int tl = ND > 4 ? fresh_lane() : l, tn = tl & 31, tg = tl >> 5;
 
       f32x16 s = {};
       constexpr int KB = C::KS < 9 ? C::KS : C::KS > 9 ? 4 : 9;  // K fragments in flight
       frag_t<T> k[KB];
       auto k_frag = [&](int ks) {
-        if constexpr (sizeof(T) == 2) return *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + (((2 * ks + g) ^ swz<24>(n)) * E));
-        else return *reinterpret_cast<const frag_t<T>*>(tile + n * P * E + 16 * ks + 8 * g);
+        if constexpr (sizeof(T) == 2) return *reinterpret_cast<const frag_t<T>*>(tile + tn * P * E + (((2 * ks + tg) ^ swz<24>(tn)) * E));
+        else return *reinterpret_cast<const frag_t<T>*>(tile + tn * P * E + 16 * ks + 8 * tg);
       };
 #pragma unroll
       for (int i = 0; i < KB; ++i) k[i] = k_frag(wave + 4 * i);
@@ -266,13 +275,13 @@ __device__ __forceinline__ void split_shares(const PagedArgs& a, unsigned char* 
           for (int e = 0; e < 8; ++e) low[8 * kk + e] = s[8 * kk + e] - to_f32(pf[e]);
           pl = acc_to_frag<T>(low, kk);
         }
-        const int ra = 16 * kk + 4 * g;
+        const int ra = 16 * kk + 4 * tg;
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
           const int c0 = 32 * (wave + 4 * i);
           frag_t<T> cf;
           if constexpr (sizeof(T) == 2) {
-            const int sl = l & 15, col = c0 + 16 * ((l >> 4) & 1) + 4 * (sl & 3);
+            const int sl = tl & 15, col = c0 + 16 * ((tl >> 4) & 1) + 4 * (sl & 3);
             const int r0 = ra + (sl >> 2), r1 = r0 + 8;
             typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
             const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(

@@ -33,13 +33,6 @@ __device__ __forceinline__ void score_step(f32x16& s, const bf16x8& k, const bf1
 }
 __device__ __forceinline__ void scores_done(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 15" : "+v"(s)); }
 
-// The lane, formed anew wherever it is asked for: values derived from one kept all the way would fill
-// the registers, and a spilled one's reload waits for the copies in flight.
-__device__ __forceinline__ int fresh_lane() {
-  int l;
-  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
-  return l;
-}
 // Direct copies of 1 KB (common.hpp, g2lds16_so and g2lds16). NT: the data are used by this workgroup alone, and
 // pass the caches by (6.9 against 5.9 TB/s for a pool read once, 334 MB).
 template <bool NT>
