@@ -462,8 +462,8 @@ void launch_join_product(const PagedArgs& a, hipStream_t st) {
   const unsigned wgs = (unsigned)(blocks * tparts);
   if (a.d_c <= 128) join_kernel<T, DV, NB, 2><<<wgs, 256, lds, st>>>(a, tparts);
   else if (a.d_c <= 256) join_kernel<T, DV, NB, 4><<<wgs, 256, lds, st>>>(a, tparts);
-  else if (NB > 1 || a.d_c <= 512) join_kernel<T, DV, NB, 8><<<wgs, 256, lds, st>>>(a, tparts);
-  else if constexpr (NB == 1) join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, tparts);
+  else if (a.d_c <= 512) join_kernel<T, DV, NB, 8><<<wgs, 256, lds, st>>>(a, tparts);
+  else if constexpr (NB == 1 || 64 * NB == DV) join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, tparts);
 }
 
 // The same for one row and head per workgroup, partials and all, in fp32: where there are no more of
@@ -570,11 +570,15 @@ void launch_join(const PagedArgs& a, hipStream_t st) {
   // heads: 24 us and 15; 61 rows 20 and 23)
   if (a.T > a.workers) combine_kernel<8><<<(unsigned)((int64_t)a.T * ((a.H + 7) / 8)), kCombineThreads, 0, st>>>(a);
   else combine_kernel<1><<<(unsigned)pairs, kCombineThreads, 0, st>>>(a);
-  // all of out's columns in one workgroup (o is then read once) where W_v's rows of a head fit in
-  // LDS and heads and rows alone fill half of the GPU
+  // all of out's columns in one workgroup, or half of them with d_c above 512 (o is then read once or twice: W_v's
+  // rows of a head have to fit in LDS), where heads and rows alone fill half of the GPU (416 rows, 128
+  // heads, d_c = 1024: 284 us with a quarter, so 163)
   constexpr int NB = DV / 32;
   if constexpr (sizeof(T) == 2 && NB > 1)
-    if (a.d_c <= 512 && (int64_t)a.H * ((a.T + 31) / 32) >= kCus / 2) return launch_join_product<T, DV, NB>(a, st);
+    if ((int64_t)a.H * ((a.T + 31) / 32) >= kCus / 2) {
+      if (a.d_c <= 512) return launch_join_product<T, DV, NB>(a, st);
+      return launch_join_product<T, DV, NB / 2>(a, st);
+    }
   launch_join_product<T, DV, 1>(a, st);
 }
 

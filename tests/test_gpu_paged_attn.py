@@ -420,3 +420,11 @@ def test_lse_of_short_rows_is_held_in_fp32(widths, d_c, heads, count, longest):
     off = np.linalg.norm(lse - want) / np.linalg.norm(want)
     print(f"{off:.2e}")
     assert off <= np.sqrt(p.d_nope + d_c + p.d_rope) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("d_c,heads,count,dtype", [(512, 16, 521, "bf16"), (1024, 128, 6, "bf16"), (256, 2, 700, "fp32")])
+def test_products_of_many_rows(d_c, heads, count, dtype):
+    """More blocks of rows than workgroups take at once, and the widest latent with many heads; rows of padding
+    between."""
+    rng = np.random.default_rng(2)
+    check(make([int(v) for v in rng.integers(1, 5, count)], 16, d_c=d_c, heads=heads, dtype=dtype, pad=9), dtype, base=10000.0)
