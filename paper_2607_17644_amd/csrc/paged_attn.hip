@@ -4,10 +4,11 @@
 //   qa = W_k q_nope,  z_j = scale (qa . c_j + q_rope . k_j),  o = sum_j softmax(z)_j c_j,  out = W_v^T o
 //
 // so that a cached position is one row [c_j || k_j] that every head reads, and no per-head key
-// or value exists. Three launches: the products qa and the turned q_rope (absorb_kernel), the
-// attention split over the cache (split_kernel), and the join of split rows with the product
-// by W_v (join_kernel). Bound by the cache's bytes for few heads (2 (2 d_c + d_rope) flop per
-// head for each row of d_c + d_rope elements).
+// or value exists. Launches: the products qa, the turned q_rope and the layout of the tiles
+// (absorb_kernel), the attention split over the cache (split_kernel, or paged_wide.hip's), and the
+// join of split rows with the product by W_v (join_vec_kernel, or combine_kernel and join_kernel).
+// Bound by the cache's bytes for few heads (2 (2 d_c + d_rope) flop per head for each row of d_c
+// + d_rope elements), by the products too for 128.
 #include <math.h>
 
 #define LAGA_LDS_DMA_ASM 1
@@ -561,6 +562,9 @@ __global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
 template <typename T, int DV>
 void launch_join(const PagedArgs& a, hipStream_t st) {
   const int64_t pairs = (int64_t)a.T * a.H;
+  // both in one launch where no workgroup would wait for another: 16 heads of one row 7.6 us (4.7 + 6.7 in two), 2
+  // rows of 128 heads 23.6 (18.4 + 10.4). Small heads with 256 threads: 5.1 us, 8.9 with 1024 (8 rows, 4
+  // heads, d_c = 64, fp32).
   if (pairs <= kCus) {
     if (a.d_c * DV <= 128 * 64) join_vec_kernel<T, DV, 256><<<(unsigned)pairs, 256, 0, st>>>(a);
     else join_vec_kernel<T, DV, 1024><<<(unsigned)pairs, 1024, 0, st>>>(a);
@@ -571,8 +575,8 @@ void launch_join(const PagedArgs& a, hipStream_t st) {
   if (a.T > a.workers) combine_kernel<8><<<(unsigned)((int64_t)a.T * ((a.H + 7) / 8)), kCombineThreads, 0, st>>>(a);
   else combine_kernel<1><<<(unsigned)pairs, kCombineThreads, 0, st>>>(a);
   // all of out's columns in one workgroup, or half of them with d_c above 512 (o is then read once or twice: W_v's
-  // rows of a head have to fit in LDS), where heads and rows alone fill half of the GPU (416 rows, 128
-  // heads, d_c = 1024: 284 us with a quarter, so 163)
+  // rows of a head have to fit in LDS), where heads and rows alone fill half of the GPU (61 rows,
+  // 128 heads: 16 us, 32 with a quarter per workgroup; 416 rows, d_c = 1024: 284 us with a quarter, so 163)
   constexpr int NB = DV / 32;
   if constexpr (sizeof(T) == 2 && NB > 1)
     if ((int64_t)a.H * ((a.T + 31) / 32) >= kCus / 2) {

@@ -284,7 +284,9 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(AppendArgs a) {
 }  // namespace
 
 // One launch, the scanning workgroup expanding its own sums, where it has few rows and pages
-// to do; else a second launch over the GPU.
+// to do; else a second launch over the GPU. Bound by a chain of loads (lengths, sums, stack or table):
+// 64 requests 6.2 us in one, 4.3 + 2.9 in two; 500 requests with 15 new tokens each in the mean, 7500 rows,
+// 7.5 and 4.5 + 4.3, and a launch's gap in between.
 hipError_t launch_plan(const PlanArgs& a, hipStream_t st) {
   const int64_t items = a.release ? (int64_t)a.R * a.width : a.rows;
   if (items <= 8 * kScanThreads) {
@@ -307,6 +309,8 @@ static void launch_append_t(const AppendArgs& a, hipStream_t st) {
 
 template <typename T>
 hipError_t launch_append(const AppendArgs& a, hipStream_t st) {
+  // a wave per token while that is what the GPU holds at once, else four tokens one after the other: 64 tokens
+  // 3.8 us and 5.8, 1024 tokens 4.3 and 6.3, 16384 tokens 15.1 and 13.7 (5.5 TB/s at its best, 11.8 us)
   if (a.T <= 4 * kCus) launch_append_t<T, 1>(a, st);
   else launch_append_t<T, 4>(a, st);
   return hipGetLastError();
