@@ -323,8 +323,8 @@ LAGA_API size_t laga_out_proj_workspace_bytes(const laga_out_proj_t* p);
  *   - cached rows past a row's position, and table entries past a request's pages, are
  *     never read: they may hold anything;
  *   - repeated calls are bit-identical; the attention's sums over a row's keys are grouped
- *     by how the call's tiles are shared out, so a row's last bits may depend on the other
- *     rows' lengths and on n_heads.
+ *     by how the call's tiles are shared out, so a row's last bits (of fp32 sums) may depend on the
+ *     other rows' lengths and on n_heads, its precision does not.
  * Limits: head dims and d_c as for the attention calls; page_size >= 1; page_stride 0 (read
  * as page_size * (d_c + d_rope)) or at least that and a multiple of 8; n_pages * page_size,
  * requests * table_width, rows * n_heads, rows * (table_width * page_size / 32 + 10) and
@@ -406,9 +406,7 @@ LAGA_API laga_status_t laga_cache_append(const laga_paged_t* p, const laga_prolo
  * The product with W_kv_b's K columns is taken on the query's side and the one with its V
  * columns after the softmax. Statistics, sums and joins of a row's parts are fp32. In bf16 the
  * values in between keep 16 bits of mantissa or more, so out is the exact result rounded once, to
- * little more than that; but with d_c = 512, d_rope = 64 and rows of many keys the query's product
- * with the K columns enters the scores with 8 (its rest enters lse, to first order): out is then off
- * by about 1.4 roundings. Workspace: laga_paged_workspace_bytes(p, LAGA_OP_PAGED_ATTN). */
+ * little more than that, for scores of any spread. Workspace: laga_paged_workspace_bytes(p, LAGA_OP_PAGED_ATTN). */
 LAGA_API laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg,
                                        const void* q, const void* w_kv_b, const void* cache,
                                        const int32_t* block_table, const int32_t* row_request,

@@ -92,14 +92,14 @@ struct PagedArgs {
   int32_t* sched;    // layout of the tiles (sched_ints)
   void* qa;          // [T][H][d_c + d_rope]: W_k q_nope, then q_rope
   void* qa_lo;       // bf16: what qa's rounding left, rounded
-  void* qa_low2;     // and what that left
+  void* qa_low2;     // and what that left (in the scores of the band alone; of the rest lse has it)
   float* obar;       // [T][H][d_c]: normalised rows that one worker took whole
   float* part_o;     // [2 * workers][H][d_c]
   float* part_ml;    // [2 * workers][H][2]
   int wide;          // paged_wide.hip's
   int heads_per_wg;  // heads of a head block
   int workers;       // of each head block
-  int groups;        // of 32 heads in heads_per_wg (wide kernel), or 0
+  int groups;        // of 32 heads in heads_per_wg, for few tiles (wide kernel), or 0
 };
 // Layout of the tiles: [units per worker, units, groups, units of a row's cost], units before each row [T + 1], and of
 // each worker's first share (kShareInts) the row, its first tile and end, request and visible keys.
@@ -109,31 +109,30 @@ inline size_t sched_ints(long long T, int workers) { return (size_t)sched_shares
 
 __host__ __device__ inline int tiles_of(int visible) { return (visible + kTileKeys - 1) / kTileKeys; }
 // A row's length in the layout: its tiles and, before them, some units of no tile, which stand for what a
-// share costs besides its tiles (q in, the first tiles' way from memory, its result out). Us without
-// them and with: wide kernel, 2 x 100000 keys, 128 heads 98 and 84 (6 units 88, 24 units 86); 20 x up to
-// 3000 keys, 128 heads 61 and 42; 200 x up to 1500 keys, 32 heads 96 and 72 (24 units 80); the others, 64
-// x up to 4000 keys, d_c = 256, 33 and 32, with 9 units 34.
+// share costs besides its tiles (q in, the first tiles' way from memory, its result out). Us of a call without
+// them and with: wide kernel, 20 x up to 3000 keys, 128 heads 80 and 69 (6 units 71, 24 units 70); 300 x up to 150
+// keys, 128 heads 214 and 174; 200 x up to 1500 keys, 32 heads 115 and 101 (24 units 114); the others, 64 x
+// up to 4000 keys, d_c = 256, 46 and 43, with 9 units 44; d_c = 1024 120 and 114, 117.
 constexpr int kRowCost = 2, kWideRowCost = 9;
 __host__ __device__ inline int units_of(int visible, int cost) { return visible > 0 ? cost + tiles_of(visible) : 0; }
 // Units per worker: even shares.
 __host__ __device__ inline int units_per_worker(int total, int workers) {
   return total > workers ? (int)(((int64_t)total + workers - 1) / workers) : 1;
 }
-// How the wide kernel's workgroups go about their tiles. With few, or short rows, a workgroup takes 32 of
-// its heads (groups of them: one after the other on the workgroups of an XCD) and its four waves share
-// each tile; a tile is then done in a third of the time, no parts of waves have to meet at the end, and
-// the scores have the second part of q W_k^T (the lse of short rows averages no roundings). groups 0:
-// the wide way. Us this way and wide: 1000 rows of up to 32 keys, 16 heads 36 and 70, up to 150 62 and 89, up to
-// 500 122 and 126; 300 rows, 128 heads, up to 32 keys 60 and 53, up to 150 85 and 70; 600 rows of up to 150
-// keys, 64 heads 86 and 83.
+// How the wide kernel's workgroups go about their tiles. With few of them, or rows of about one tile, a workgroup takes
+// 32 of its heads (groups of them: one after the other on the workgroups of an XCD) in the general form, in
+// which a share starts sooner and more workgroups divide a row; groups 0: the wide way. Both hold the same
+// precision. Us of a call this way and wide: 20000 keys, 64 heads 41 and 48; 20 x up to 300 keys, 128 heads 43 and 46;
+// 1000 x up to 32 keys, 16 heads 77 and 82; but 600 x up to 150 keys, 64 heads 187 and 178, 64 x up to 2000,
+// 16 heads 49 and 43, 20 x up to 3000, 128 heads 77 and 65.
 constexpr int kFewTiles = 8;   // units of a worker
-constexpr int kShortRows = 8;  // groups of heads x tiles, in the mean
+constexpr int kShortRows = 2;  // tiles, in the mean
 struct Shares { int per, workers, groups, cost, total; };
 __host__ __device__ inline Shares shares_of(int tiles, int rows, int workers, int groups) {
   const int few = groups > 0 ? workers / (8 * groups) * 8 : 0;
   if (few > 0) {
     const int total = tiles + rows * kRowCost, per = units_per_worker(total, few);
-    if (per <= kFewTiles || (int64_t)tiles * groups < kShortRows * rows) return {per, few, groups, kRowCost, total};
+    if (per <= kFewTiles || tiles < (int64_t)kShortRows * rows) return {per, few, groups, kRowCost, total};
   }
   const int cost = groups > 0 ? kWideRowCost : kRowCost, total = tiles + rows * cost;
   return {units_per_worker(total, workers), workers, 0, cost, total};
@@ -161,7 +160,7 @@ struct PagedPlan {
 inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
   PagedPlan p;
   p.wide = elem_size == 2 && d_c == 512 && d_rope == 64;
-  const int most = p.wide ? 128 : 32;  // heads of a workgroup
+  const int most = p.wide ? 64 : 32;  // heads of a workgroup (all parts of q W_k^T of more would not fit in registers)
   p.head_blocks = (H + most - 1) / most;
   p.heads_per_wg = p.wide ? (H + p.head_blocks - 1) / p.head_blocks : most;
   const int wgs = (elem_size == 2 && d_c <= 256 ? 2 : 1) * kCus;  // what runs at once

@@ -265,10 +265,8 @@ __device__ __forceinline__ RowParts parts_of(const PagedArgs& a, int t) {
   const int w0 = first / per, w1 = (end - 1) / per;
   return {first, w0, w1, true, w0 != w1, 0.f};
 }
-// bf16: the scores lack the third part of q W_k^T, or on the wide kernel's way (not with few tiles) the second and
-// what is behind it: lse's share of this part to first order is scale sum_c dqa_c o_c with the row's
-// normalised sum o (the second order is below 1e-6 for the second part).
-__device__ __forceinline__ const void* lse_lacks(const PagedArgs& a) { return a.wide && a.sched[2] == 0 ? a.qa_lo : a.qa_low2; }
+// bf16: the scores lack the third part of q W_k^T. lse's share of it to first order is scale sum_c dqa_c o_c with the
+// row's normalised sum o; out's is below 2^-16 of a probability.
 // Partials of a row's head, dealt to `groups` threads of the same four columns (c), then joined in order
 // through LDS (room: 24 bytes per thread). The result is complete in the threads of group 0.
 __device__ __forceinline__ Joined join_parts(const PagedArgs& a, const RowParts& r, int h, int c, int group, int groups,
@@ -293,8 +291,8 @@ __device__ __forceinline__ Joined join_parts(const PagedArgs& a, const RowParts&
 }
 
 // Rows that several workers share, put together in obar: a workgroup per row and some heads. Bound by
-// reading the partials (128 heads x 61 rows, 83 MB, 19 us; within the product's own kernel, where a
-// lane had several loads of 16 bytes under way at most, 47 with it against 19 + 17).
+// reading the partials (128 heads x 61 rows 17 us; within the product's own kernel, where a lane had several
+// loads of 16 bytes under way at most, 47 us for both against 19 + 17).
 constexpr int kCombineThreads = 256;
 template <int HEADS>
 __global__ __launch_bounds__(kCombineThreads) void combine_kernel(PagedArgs a) {
@@ -355,7 +353,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tparts) {
   };
   f32x4 x[NST][2];
   quad y[kTwo<T> ? NST : 1][2];
-  const T* lacks = (const T*)lse_lacks(a);
+  const T* lacks = (const T*)a.qa_low2;
   auto load = [&](int i, int t, const Row& r) {
     x[i][0] = x[i][1] = f32x4{r.fill, r.fill, r.fill, r.fill};
     if (r.seen && 16 * (NST * wave + i) < dc) {
@@ -489,7 +487,7 @@ __global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
   // what lse lacks, in the first wave
   float lack[2][8] = {};
   if (kTwo<T> && a.lse && tid < 64 && r.seen) {
-    const T* q = (const T*)lse_lacks(a) + th * (dc + a.d_rope);
+    const T* q = (const T*)a.qa_low2 + th * (dc + a.d_rope);
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       if (8 * tid + 512 * k < dc) load8(q + 8 * tid + 512 * k, lack[k]);
