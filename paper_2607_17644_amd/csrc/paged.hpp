@@ -101,9 +101,10 @@ struct PagedArgs {
   int workers;       // of each head block
   int groups;        // of 32 heads in heads_per_wg, for few tiles (wide kernel), or 0
 };
-// Layout of the tiles: [units per worker, units, groups, units of a row's cost], units before each row [T + 1], and of
+// Layout of the tiles: [units per worker, units, groups, units of a row's cost, whether two successive rows have one
+// request], units before each row [T + 1], and of
 // each worker's first share (kShareInts) the row, its first tile and end, request and visible keys.
-constexpr int kSchedHeader = 4, kShareInts = 8;
+constexpr int kSchedHeader = 5, kShareInts = 8;
 __host__ __device__ inline int64_t sched_shares(int64_t T) { return (kSchedHeader + T + 1 + 7) / 8 * 8; }
 inline size_t sched_ints(long long T, int workers) { return (size_t)sched_shares(T) + (size_t)kShareInts * workers; }
 

@@ -141,14 +141,18 @@ __device__ void lay_out_tiles(const PagedArgs& a) {
   const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
   const bool lds = a.T <= kLayoutLds;
   int32_t* before = a.sched + kSchedHeader;
-  // all tiles, and the rows that have any
+  // all tiles, the rows that have any, and whether one has the request of the row before it
   RowState mine = {0, 0, false};
-  int tiles = 0, rows = 0;
+  int tiles = 0, rows = 0, again = 0;
   for (int t = tid; t < a.T; t += NT) {
     const RowState rs = row_state(a, t);
     if (t < NT) mine = rs;
     tiles += tiles_of(rs.visible);
     rows += rs.visible > 0;
+    if (a.row_request && t > 0 && rs.visible > 0) {
+      const RowState last = row_state(a, t - 1);
+      again |= last.visible > 0 && last.request == rs.request;
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -156,7 +160,7 @@ __device__ void lay_out_tiles(const PagedArgs& a) {
     rows += __shfl_xor(rows, o);
   }
   if (l == 0) sm[wave] = tiles, sm[kAbsorbWaves + wave] = rows;
-  __syncthreads();
+  again = __syncthreads_or(again);
   tiles = rows = 0;
   for (int w = 0; w < kAbsorbWaves; ++w) tiles += sm[w], rows += sm[kAbsorbWaves + w];
   const Shares sh = shares_of(tiles, rows, a.workers, a.groups);
@@ -196,6 +200,7 @@ __device__ void lay_out_tiles(const PagedArgs& a) {
     a.sched[1] = sum;
     a.sched[2] = sh.groups;
     a.sched[3] = sh.cost;
+    a.sched[4] = again != 0;
   }
   __syncthreads();
   const int32_t* sums = lds ? s_before : before;

@@ -39,13 +39,23 @@ __device__ __forceinline__ void scores_done(f32x16& s) { asm volatile("s_nop 15\
 
 // A direct copy of 1 KB to LDS byte address to + at. `base` may have been written by a vector instruction four
 // instructions before this.
+template <bool NT>
 __device__ __forceinline__ void copy_row(const void* base, uint32_t off, uint32_t to, int at) {
-  asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to), "i"(at)
-               : "memory", "m0", "scc");
+  if constexpr (NT)
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(to), "i"(at)
+                 : "memory", "m0", "scc");
+  else
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to), "i"(at)
+                 : "memory", "m0", "scc");
 }
+template <bool NT>
 __device__ __forceinline__ void copy_lanes(const void* g, uint32_t to, int at) {
-  asm volatile("s_add_u32 m0, %1, %2\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(to), "i"(at)
-               : "memory", "m0", "scc");
+  if constexpr (NT)
+    asm volatile("s_add_u32 m0, %1, %2\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(g), "s"(to), "i"(at)
+                 : "memory", "m0", "scc");
+  else
+    asm volatile("s_add_u32 m0, %1, %2\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(to), "i"(at)
+                 : "memory", "m0", "scc");
 }
 
 // Computed here, not where it is read.
@@ -64,32 +74,21 @@ __device__ __forceinline__ V lds_at(uint32_t address) {
   return *(__attribute__((address_space(3))) const V*)(uintptr_t)address;
 }
 
-template <int HG>
-__global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_blocks) {
+// The share of worker w, for heads h0 .. h0 + 64 (HG = 2) or 32, below hb1. NT: see wide_kernel.
+constexpr int kSums = 2 * 4 * 4 * 64;  // partial scores of two tiles, in f32x4
+constexpr int kLds = kStages * kTile * 2 + kSums * 16;
+template <int HG, bool NT>
+__device__ __forceinline__ void wide_shares(const PagedArgs& a, unsigned char* smem, int32_t (*s_page)[kPages], int* s_high, int w,
+                                            int hb0, int hb1, int per, int total) {
   static_assert(HG == 1 || HG == 2);
   constexpr int NP = 4 / HG;
   constexpr int KS = kRow / 16 / NP, KC = kDc / 16 / NP;  // steps of a wave; of them over the latent
   constexpr int NB = kDc / 32 / NP;                       // blocks of columns of a wave
-  constexpr int kSums = 2 * 4 * 4 * 64;                   // partial scores of two tiles, in f32x4
-  constexpr int kLds = kStages * kTile * 2 + kSums * 16, kFew = SplitCfg<bf16, 4>::LDS;
-  __shared__ __attribute__((aligned(256))) unsigned char smem[kLds > kFew ? kLds : kFew];
-  __shared__ int32_t s_page[4][kPages];
-  __shared__ int s_high[4];
   f32x4* sums = (f32x4*)(smem + kStages * kTile * 2);
 
   const int l = threadIdx.x & 63, n = l & 31, g = l >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hg = wave % HG, part = wave / HG;
-  // the head blocks of a worker follow each other on one XCD: its L2 serves all but the first
-  const int id = blockIdx.x, hb = id / 8 % head_blocks, w = id / (8 * head_blocks) * 8 + id % 8;
-  const int per = uniform(a.sched[0]), total = uniform(a.sched[1]), groups = uniform(a.sched[2]);
-  const int hb0 = hb * a.heads_per_wg, hb1 = min(a.H, hb0 + a.heads_per_wg);
-  if (groups > 0) {  // few tiles
-    const int hf = hb0 + 32 * (w / 8 % groups);
-    if (w / (8 * groups) < a.workers / (8 * groups) && hf < hb1)
-      split_shares<bf16, 4>(a, smem, w / (8 * groups) * 8 + w % 8, hf, min(32, hb1 - hf), per, total);
-    return;
-  }
   const int h0 = hb0 + 32 * hg, nh = min(32, hb1 - h0);  // nh <= 0: this wave's results are not stored
   const int64_t start = (int64_t)w * per;
   if (start >= total) return;
@@ -180,8 +179,8 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
     };
     auto copy = [&](const Rows& x, const void* place, uint32_t tile, int j) {
       // swz<16>(wave + 4 j) is swz<16>(wave) and two bits of j
-      if (j < NMAIN) copy_row(place, at_copy ^ (16 * swz<16>(4 * j)), tile + 2 * wave * kDc, 8 * j * kDc);
-      else copy_lanes((const char*)((uintptr_t)(uint32_t)x.band_lo | ((uintptr_t)(uint32_t)x.band_hi << 32)) + at_band, tile + 1024 * wave, 2 * kMain);
+      if (j < NMAIN) copy_row<NT>(place, at_copy ^ (16 * swz<16>(4 * j)), tile + 2 * wave * kDc, 8 * j * kDc);
+      else copy_lanes<NT>((const char*)((uintptr_t)(uint32_t)x.band_lo | ((uintptr_t)(uint32_t)x.band_hi << 32)) + at_band, tile + 1024 * wave, 2 * kMain);
     };
     auto fetch = [&](int it, uint32_t tile) {  // a whole tile at once
       refill(it);
@@ -439,6 +438,31 @@ __global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_bloc
     share = next_share(a, t, at);
     at = share.first;
     if (at >= end) return;
+  }
+}
+
+// Where each row has a request of its own, a tile's copies pass the caches by (a hint: nt); successive rows of one
+// request read the same pages again, from there. Us of a call with the hint and without: 64 requests x up to
+// 8192 keys, 16 heads 95 and 103; 61, 128 heads 199 and 207; 64 x 4000, 64 heads 89 and 92; but 4 tokens for each
+// of 64 requests, 16 heads 289 and 275, 512 tokens of one request over 8192 keys 872 and 726.
+template <int HG>
+__global__ __launch_bounds__(256, 1) void wide_kernel(PagedArgs a, int head_blocks) {
+  constexpr int kFew = SplitCfg<bf16, 4>::LDS;
+  __shared__ __attribute__((aligned(256))) unsigned char smem[kLds > kFew ? kLds : kFew];
+  __shared__ int32_t s_page[4][kPages];
+  __shared__ int s_high[4];
+  // the head blocks of a worker follow each other on one XCD: its L2 serves all but the first
+  const int id = blockIdx.x, hb = id / 8 % head_blocks, w = id / (8 * head_blocks) * 8 + id % 8;
+  const int per = uniform(a.sched[0]), total = uniform(a.sched[1]), groups = uniform(a.sched[2]);
+  const int hb0 = hb * a.heads_per_wg, hb1 = min(a.H, hb0 + a.heads_per_wg);
+  if (groups > 0) {  // few tiles
+    const int hf = hb0 + 32 * (w / 8 % groups);
+    if (w / (8 * groups) < a.workers / (8 * groups) && hf < hb1)
+      split_shares<bf16, 4>(a, smem, w / (8 * groups) * 8 + w % 8, hf, min(32, hb1 - hf), per, total);
+  } else if (uniform(a.sched[4])) {
+    wide_shares<HG, false>(a, smem, s_page, s_high, w, hb0, hb1, per, total);
+  } else {
+    wide_shares<HG, true>(a, smem, s_page, s_high, w, hb0, hb1, per, total);
   }
 }
 
