@@ -2,13 +2,17 @@
 
 Each ``laga_*`` function takes torch tensors, checks dtype/shape/device/
 contiguity, passes raw pointers and the current HIP stream to the C entry point
-of the same name, and raises :class:`LagaError` on a non-zero status. Outputs
-that are not supplied are allocated with torch (the C library never allocates).
+of the same name, and raises :class:`LagaError` on a non-zero status. Outputs and
+workspaces that are not supplied are allocated with torch (the C library never allocates),
+on the stream that the call runs on; where that is not the current one (``stream=``), outputs are kept
+from reuse until the current stream, too, has done what it was given before they were dropped.
 """
 from __future__ import annotations
 
 import ctypes
 import dataclasses
+import functools
+import inspect
 import os
 
 import torch
@@ -256,6 +260,32 @@ def _stream(stream):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _kept(tensors, stream):
+    """Outputs allocated on `stream` and handed to the caller, whose own work is on the current stream."""
+    now = torch.cuda.current_stream(stream.device)
+    if now != stream:
+        for t in tensors:
+            t.record_stream(now)
+
+
+def _on_its_stream(call):
+    """What the call allocates belongs to the stream that it runs on. (A block of another stream's could be
+    dropped, as a workspace is on return, and given out again there while the call still uses it.)"""
+    at = list(inspect.signature(call).parameters).index("stream")
+
+    @functools.wraps(call)
+    def on_its_stream(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return call(*args, **kw)
+        with torch.cuda.stream(stream):
+            result = call(*args, **kw)
+        _kept([t for t in (result if isinstance(result, (tuple, list)) else (result,)) if isinstance(t, torch.Tensor)], stream)
+        return result
+
+    return on_its_stream
+
+
 def _check(status, where):
     if status != 0:
         raise LagaError(status, where)
@@ -265,6 +295,7 @@ def _new(p, name, dtype, device):
     return torch.empty(p.shapes()[name], dtype=dtype, device=device)
 
 
+@_on_its_stream
 def laga_reconstruct_kv(p: Problem, c_kv, w_kv_b, kv=None, stream=None):
     """kv = c_kv @ w_kv_b as [B,S,H,d_nope+d_v] (Alg. 1 step 4)."""
     sh, dt = p.shapes(), p.torch_dtype
@@ -283,6 +314,7 @@ def _workspace(p, op, workspace, device):
     return workspace
 
 
+@_on_its_stream
 def laga_attn_fwd(p: Problem, q, c_kv, k_pe, w_kv_b, kv=None, out=None, lse=None, workspace=None,
                   stream=None):
     """Causal MLA attention forward of the shard's heads; returns (out, lse)."""
@@ -328,6 +360,7 @@ def _bwd_outputs(p, dev, dq, dc_kv, dk_pe, dw_kv_b, workspace):
     return dq, dc_kv, dk_pe, dw_kv_b, workspace
 
 
+@_on_its_stream
 def laga_attn_bwd(p: Problem, q, c_kv, k_pe, w_kv_b, kv, out, lse, dout, dq=None, dc_kv=None,
                   dk_pe=None, dw_kv_b=None, workspace=None, stream=None):
     """Backward of the block; returns (dq, dc_kv, dk_pe, dw_kv_b) — dq in the element
@@ -338,6 +371,7 @@ def laga_attn_bwd(p: Problem, q, c_kv, k_pe, w_kv_b, kv, out, lse, dout, dq=None
     return dq, dc_kv, dk_pe, dw_kv_b
 
 
+@_on_its_stream
 def laga_attn_bwd_noalloc(p: Problem, q, c_kv, k_pe, w_kv_b, kv, out, lse, dout, dq=None, dc_kv=None,
                           dk_pe=None, dw_kv_b=None, stream=None):
     """laga_attn_bwd with the library's fixed device scratch array as its workspace (for
@@ -365,6 +399,7 @@ def laga_out_proj_workspace_bytes(p: OutProj) -> int:
     return int(_lib.laga_out_proj_workspace_bytes(ctypes.byref(p.c())))
 
 
+@_on_its_stream
 def laga_out_proj_fwd(p: OutProj, out, w_o, y=None, stream=None):
     """Alg. 1 step 7: y = reshape(out) @ w_o; out [T, n_heads, d_v], w_o [F, d_model]."""
     sh, dt = p.shapes(), p.torch_dtype
@@ -376,6 +411,7 @@ def laga_out_proj_fwd(p: OutProj, out, w_o, y=None, stream=None):
     return y
 
 
+@_on_its_stream
 def laga_out_proj_bwd(p: OutProj, out, w_o, dy, d_out=None, dw_o=None, workspace=None, stream=None):
     """Backward of laga_out_proj_fwd: (d_out in the element dtype, dw_o in fp32)."""
     sh, dt = p.shapes(), p.torch_dtype
@@ -395,6 +431,7 @@ def laga_out_proj_bwd(p: OutProj, out, w_o, dy, d_out=None, dw_o=None, workspace
     return d_out, dw_o
 
 
+@_on_its_stream
 def laga_prologue_fwd(p: Problem, latent_raw, kpe_raw, q=None, gamma=None, eps=1e-6, rope_base=10000.0,
                       position_offset=0, c_kv=None, k_pe=None, rstd=None, stream=None):
     """Latent normalisation and decoupled RoPE before the all-gather; returns (c_kv, k_pe,
@@ -417,6 +454,7 @@ def laga_prologue_fwd(p: Problem, latent_raw, kpe_raw, q=None, gamma=None, eps=1
     return c_kv, k_pe, rstd
 
 
+@_on_its_stream
 def laga_prologue_bwd(p: Problem, latent_raw, rstd, dc_kv, dk_pe, dq=None, gamma=None, eps=1e-6,
                       rope_base=10000.0, position_offset=0, d_latent_raw=None, d_kpe_raw=None, d_gamma=None,
                       workspace=None, stream=None):
@@ -518,18 +556,28 @@ def _serve(where, index, stream, function, *args):
         raise LagaError(status, where)
 
 
-def _empty(shape, dtype, index):
-    return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
+def _empty(shape, dtype, index, stream):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
 
 
-def _int32(sh, name, t, index):
-    return _empty(sh[name], torch.int32, index) if t is None else t
+def _output(shape, dtype, index, stream):
+    t = _empty(shape, dtype, index, stream)
+    if stream is not None:
+        _kept((t,), stream)
+    return t
 
 
-def _serve_workspace(p, op, workspace, index):
+def _int32(sh, name, t, index, stream):
+    return _output(sh[name], torch.int32, index, stream) if t is None else t
+
+
+def _serve_workspace(p, op, workspace, index, stream):
     """(workspace, its bytes)."""
     if workspace is None:
-        workspace = _empty((max(1, laga_paged_workspace_bytes(p, op)),), torch.uint8, index)
+        workspace = _empty((max(1, laga_paged_workspace_bytes(p, op)),), torch.uint8, index, stream)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise _fault(workspace, "workspace", tuple(workspace.shape), workspace.dtype, index)
     return workspace, workspace.numel() * workspace.element_size()
@@ -542,11 +590,11 @@ def laga_page_plan(p: Paged, lengths, fresh, block_table, free_pages, free_count
     status); lengths_out may be lengths, and free_count_out free_count. Nothing is read on the
     host: status[0] (PLAN_*) says on the device whether the step fits."""
     sh, i32, d = p.shapes(), torch.int32, _device_of(lengths, "lengths")
-    lengths_out, free_count_out = _int32(sh, "lengths_out", lengths_out, d), _int32(sh, "free_count_out", free_count_out, d)
-    row_begin, row_request = _int32(sh, "row_begin", row_begin, d), _int32(sh, "row_request", row_request, d)
-    position, slot = _int32(sh, "position", position, d), _int32(sh, "slot", slot, d)
-    status = _int32(sh, "status", status, d)
-    workspace, nbytes = _serve_workspace(p, OP_PAGE_PLAN, workspace, d)
+    lengths_out, free_count_out = _int32(sh, "lengths_out", lengths_out, d, stream), _int32(sh, "free_count_out", free_count_out, d, stream)
+    row_begin, row_request = _int32(sh, "row_begin", row_begin, d, stream), _int32(sh, "row_request", row_request, d, stream)
+    position, slot = _int32(sh, "position", position, d, stream), _int32(sh, "slot", slot, d, stream)
+    status = _int32(sh, "status", status, d, stream)
+    workspace, nbytes = _serve_workspace(p, OP_PAGE_PLAN, workspace, d, stream)
     _serve("laga_page_plan", d, stream, _lib.laga_page_plan, p.ref(), _at(lengths, "lengths", sh["lengths"], i32, d),
            _at(fresh, "fresh", sh["fresh"], i32, d), _at(block_table, "block_table", sh["block_table"], i32, d),
            _at(free_pages, "free_pages", sh["free_pages"], i32, d), _at(free_count, "free_count", (1,), i32, d),
@@ -562,9 +610,9 @@ def laga_page_release(p: Paged, lengths, drop, block_table, free_pages, free_cou
     """The pages of the requests with drop[r] != 0 go back on the stack (free_pages is updated in
     place); returns (lengths_out, free_count_out, status)."""
     sh, i32, d = p.shapes(), torch.int32, _device_of(lengths, "lengths")
-    lengths_out, free_count_out = _int32(sh, "lengths_out", lengths_out, d), _int32(sh, "free_count_out", free_count_out, d)
-    status = _int32(sh, "status", status, d)
-    workspace, nbytes = _serve_workspace(p, OP_PAGE_PLAN, workspace, d)
+    lengths_out, free_count_out = _int32(sh, "lengths_out", lengths_out, d, stream), _int32(sh, "free_count_out", free_count_out, d, stream)
+    status = _int32(sh, "status", status, d, stream)
+    workspace, nbytes = _serve_workspace(p, OP_PAGE_PLAN, workspace, d, stream)
     _serve("laga_page_release", d, stream, _lib.laga_page_release, p.ref(), _at(lengths, "lengths", sh["lengths"], i32, d),
            _at(drop, "drop", sh["drop"], i32, d), _at(block_table, "block_table", sh["block_table"], i32, d),
            _at(free_pages, "free_pages", sh["free_pages"], i32, d), _at(free_count, "free_count", (1,), i32, d),
@@ -593,10 +641,10 @@ def laga_paged_attn(p: Paged, q, w_kv_b, cache, block_table, position, row_reque
     lse). With rope_base q's rope band is turned by the row's position first (without, it has been)."""
     sh, dt, i32, d = p.shapes(), p.torch_dtype, torch.int32, _device_of(q, "q")
     if out is None:
-        out = _empty(sh["out"], dt, d)
+        out = _output(sh["out"], dt, d, stream)
     if lse is None:
-        lse = _empty(sh["lse"], torch.float32, d)
-    workspace, nbytes = _serve_workspace(p, OP_PAGED_ATTN, workspace, d)
+        lse = _output(sh["lse"], torch.float32, d, stream)
+    workspace, nbytes = _serve_workspace(p, OP_PAGED_ATTN, workspace, d, stream)
     cfg = None if rope_base is None else ctypes.byref(_CPrologue(0.0, rope_base, position_offset))
     _serve("laga_paged_attn", d, stream, _lib.laga_paged_attn, p.ref(), cfg, _at(q, "q", sh["q"], dt, d),
            _at(w_kv_b, "w_kv_b", sh["w_kv_b"], dt, d), _cache_at(p, cache, d),
