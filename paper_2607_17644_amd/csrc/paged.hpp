@@ -34,6 +34,23 @@ constexpr int kPlanHeader = 4;
 inline size_t plan_ws_ints(long long R) { return kPlanHeader + (size_t)(R + 1) + (size_t)R; }
 hipError_t launch_plan(const PlanArgs& a, hipStream_t st);
 
+// Items first, first + step, ... below n: n may be 2^31 - 1, past which a signed item would wrap (step: the
+// threads of a launch, below 2^31).
+template <typename F>
+__host__ __device__ __forceinline__ void each_item(int first, int step, int n, F&& f) {
+  for (uint32_t k = (uint32_t)first; k < (uint32_t)n; k += (uint32_t)step) f((int)k);
+}
+// The last r in [0, n) with sums[r] <= k (sums[0] = 0 <= k < the whole sum: the request of item k).
+template <typename Sums>
+__host__ __device__ __forceinline__ int find_request(const Sums& sums, int n, int k) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = lo + ((hi - lo) >> 1);  // (lo + hi may pass 2^31)
+    if (sums[mid] <= k) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
 struct AppendArgs {
   const void *latent, *kpe, *gamma;  // [T, d_c], [T, d_rope], [d_c] or NULL
   int64_t latent_stride, kpe_stride;  // elements between rows

@@ -51,16 +51,6 @@ __device__ void block_scan(int64_t& rows, int& pages, int64_t (&total)[2], int64
   pages = (int)pb + p - pages;
 }
 
-// last r in [0, n) with sums[r] <= k (sums[0] = 0 <= k < the whole sum: the request of item k)
-__device__ __forceinline__ int find_request(const int32_t* sums, int n, int k) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (sums[mid] <= k) lo = mid; else hi = mid;
-  }
-  return lo;
-}
-
 // What a plan or release hands out, and where to find it: sums and the lengths before the step, by request.
 struct Handout {
   const int32_t *pages_before, *row_begin, *lengths;
@@ -68,14 +58,14 @@ struct Handout {
 };
 // Rows and pages first, first + step, ... of it.
 __device__ __forceinline__ void expand(const PlanArgs& a, const Handout& x, int first, int step) {
-  for (int k = first; k < x.pages; k += step) {
+  each_item(first, step, x.pages, [&](int k) {
     const int r = find_request(x.pages_before, a.R, k), j = k - x.pages_before[r];
     int32_t* entry = a.table + (int64_t)r * a.width + j;
     if (a.release) a.free_pages[x.count + k] = *entry;
     else entry[pages_of(a, x.lengths[r])] = a.free_pages[x.count - 1 - k];
-  }
+  });
   if (a.release) return;
-  for (int t = first; t < a.rows; t += step) {
+  each_item(first, step, a.rows, [&](int t) {
     int request = -1, position = -1, slot = -1;
     if (t < x.rows) {
       request = find_request(x.row_begin, a.R, t);
@@ -91,7 +81,7 @@ __device__ __forceinline__ void expand(const PlanArgs& a, const Handout& x, int 
     a.row_request[t] = request;
     a.position[t] = position;
     a.slot[t] = slot;
-  }
+  });
 }
 
 // FILL: this workgroup also expands the sums (small steps: one launch), from LDS up to kSearchLds requests.
