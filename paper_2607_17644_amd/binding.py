@@ -107,6 +107,10 @@ class Paged:
         object.__setattr__(self, name, value)
         self.__dict__.pop("_made", None)  # what was made of the fields before
 
+    def __getstate__(self):
+        """The fields: a reference into C memory is neither copied nor pickled."""
+        return {k: v for k, v in self.__dict__.items() if k != "_made"}
+
     def _forms(self):
         """(reference to the C struct, shapes), made once for these fields: a step passes them to each call."""
         made = self.__dict__.get("_made")
