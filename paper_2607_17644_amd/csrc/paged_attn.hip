@@ -48,6 +48,23 @@ __device__ __forceinline__ void store_parts(const PagedArgs& a, int64_t at, cons
   }
 }
 
+// A value of the band in three bf16 parts, each cut off what the ones before leave, so that all have the value's sign
+// (and 3 x 8 bits are the whole of it): a cached key may be infinite, and the sum of its products with the parts has
+// to be the infinity that its product with the value is. Nor may a part be zero beside one that is not: it is
+// 2^-126 then, less than 2^-26 of any value from 2^-100 on.
+__device__ __forceinline__ void band_parts(float y, bf16 (&part)[3]) {
+  auto cut = [](float x) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u); };
+  float p[3];
+  p[0] = cut(y);
+  p[1] = cut(y - p[0]);
+  p[2] = cut((y - p[0]) - p[1]);
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    if (i > 0 && p[i] == 0.f && p[0] != 0.f) p[i] = __builtin_copysignf(0x1p-126f, p[0]);
+    part[i] = (bf16)p[i];
+  }
+}
+
 template <typename T, int DN>
 __device__ void absorb_product(const PagedArgs& a, int blk, int cblocks, int tpart, int tparts) {
   constexpr int E = 16 / sizeof(T), CPR = DN / E, PO = kAbsorbRows + 4;  // chunks of a row; pitch of the results
@@ -126,7 +143,17 @@ __device__ void absorb_band(const PagedArgs& a, int t) {
       if (h0 + u * step >= a.H) break;
       const float x0 = to_f32(x[u][0]), x1 = to_f32(x[u][1]);
       const float y[2] = {x0 * cs - x1 * sn, x0 * sn + x1 * cs};
-      store_parts<T, 2>(a, ((int64_t)t * a.H + h0 + u * step) * W + a.d_c + 2 * i, y);
+      const int64_t at = ((int64_t)t * a.H + h0 + u * step) * W + a.d_c + 2 * i;
+      if constexpr (kTwo<T>) {
+        bf16 part[2][3];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) band_parts(y[e], part[e]);
+        *reinterpret_cast<pair*>((T*)a.qa + at) = pair{part[0][0], part[1][0]};
+        *reinterpret_cast<pair*>((T*)a.qa_lo + at) = pair{part[0][1], part[1][1]};
+        *reinterpret_cast<pair*>((T*)a.qa_low2 + at) = pair{part[0][2], part[1][2]};
+      } else {
+        *reinterpret_cast<pair*>((T*)a.qa + at) = pair{y[0], y[1]};
+      }
     }
   }
 }
