@@ -199,7 +199,7 @@ constexpr int kWaves = 4;
 
 // One wave takes TPW tokens: their latent rows are held in registers (CH chunks of 8 elements
 // per lane), then its lanes take one pair of the shared key each, of 64 / (d_rope / 2) tokens
-// at a time, so that no lane forms more than TPW / 2 angles.
+// at a time, so that no lane forms more than one angle.
 template <typename T, int TPW, int CH>
 __global__ __launch_bounds__(64 * kWaves) void append_kernel(AppendArgs a) {
   const int l = threadIdx.x & 63;
@@ -299,10 +299,12 @@ static void launch_append_t(const AppendArgs& a, hipStream_t st) {
 
 template <typename T>
 hipError_t launch_append(const AppendArgs& a, hipStream_t st) {
-  // a wave per token while that is what the GPU holds at once, else four tokens one after the other: 64 tokens
-  // 3.8 us and 5.8, 1024 tokens 4.3 and 6.3, 16384 tokens 15.1 and 13.7 (5.5 TB/s at its best, 11.8 us)
-  if (a.T <= 4 * kCus) launch_append_t<T, 1>(a, st);
-  else launch_append_t<T, 4>(a, st);
+  // A wave per token up to 16 waves per CU, then two tokens one after the other, which halves the waves that wait to
+  // begin. Us with one, two and four per wave (bf16, d_c = 512, 64 wide band): 64 tokens 3.2, 3.7, 5.2; 2048 3.9, 4.1, 5.5;
+  // 4096 5.5, 5.4, 6.7; 8192 9.1, 8.3, 9.5; 16384 14.4, 12.7, 13.0 (37.9 MB read and written: 3.0 TB/s). d_c = 64: 1024 4.1,
+  // 4.4, 6.6; 8192 7.1, 5.8, 5.9; d_c = 1024: 2048 5.2, 5.8, 8.3; 16384 21.9, 19.9, 21.1; fp32: 2048 4.4, 4.6, 5.9; 16384 20.4, 19.7, 19.9.
+  if (a.T <= 16 * kCus) launch_append_t<T, 1>(a, st);
+  else launch_append_t<T, 2>(a, st);
   return hipGetLastError();
 }
 
