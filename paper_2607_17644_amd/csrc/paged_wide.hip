@@ -37,15 +37,15 @@ __device__ __forceinline__ void score_step_low(f32x16& s, const bf16x8& k, const
 }
 __device__ __forceinline__ void scores_done(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
 
-// A direct copy of 1 KB to LDS byte address to + at. `base` may have been written by a vector instruction four
-// instructions before this.
+// A direct copy of 1 KB to LDS byte address to + at. (A base that a vector instruction wrote may be read five wait
+// states after it: the addition and four more.)
 template <bool NT>
 __device__ __forceinline__ void copy_row(const void* base, uint32_t off, uint32_t to, int at) {
   if constexpr (NT)
-    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(to), "i"(at)
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(to), "i"(at)
                  : "memory", "m0", "scc");
   else
-    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to), "i"(at)
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to), "i"(at)
                  : "memory", "m0", "scc");
 }
 template <bool NT>
@@ -189,7 +189,6 @@ __device__ __forceinline__ void wide_shares(const PagedArgs& a, unsigned char* s
       const void* base[NCOPY];
 #pragma unroll
       for (int j = 0; j < NCOPY; ++j) base[j] = place(x, j);
-      asm volatile("s_nop 3");
 #pragma unroll
       for (int j = 0; j < NCOPY; ++j) copy(x, base[j], tile, j);
       return x.bad;
