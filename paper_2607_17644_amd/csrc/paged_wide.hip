@@ -38,14 +38,14 @@ __device__ __forceinline__ void score_step_low(f32x16& s, const bf16x8& k, const
 __device__ __forceinline__ void scores_done(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
 
 // A direct copy of 1 KB to LDS byte address to + at. (A base that a vector instruction wrote may be read five wait
-// states after it: the addition and four more.)
+// states after it: four are here, and between the two the caller has a written-out instruction, too.)
 template <bool NT>
 __device__ __forceinline__ void copy_row(const void* base, uint32_t off, uint32_t to, int at) {
   if constexpr (NT)
-    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(to), "i"(at)
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(to), "i"(at)
                  : "memory", "m0", "scc");
   else
-    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to), "i"(at)
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to), "i"(at)
                  : "memory", "m0", "scc");
 }
 template <bool NT>
@@ -189,6 +189,7 @@ __device__ __forceinline__ void wide_shares(const PagedArgs& a, unsigned char* s
       const void* base[NCOPY];
 #pragma unroll
       for (int j = 0; j < NCOPY; ++j) base[j] = place(x, j);
+      asm volatile("s_nop 0");
 #pragma unroll
       for (int j = 0; j < NCOPY; ++j) copy(x, base[j], tile, j);
       return x.bad;
