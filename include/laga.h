@@ -351,7 +351,7 @@ enum {
   LAGA_PLAN_INVALID = 8  /* a negative length or count, or free_count outside [0, n_pages] */
 };
 
-typedef enum { LAGA_OP_PAGE_PLAN = 3, LAGA_OP_PAGED_ATTN = 4 } laga_paged_op_t;
+typedef enum { LAGA_OP_PAGE_PLAN = 3, LAGA_OP_PAGED_ATTN = 4, LAGA_OP_PAGED_ATTN_Q8 = 5 } laga_paged_op_t;
 
 /* Pages, slots and positions of a step that adds fresh[r] >= 0 tokens to request r:
  *   request r's ceil((lengths[r] + fresh[r]) / page_size) - ceil(lengths[r] / page_size) new
@@ -412,6 +412,51 @@ LAGA_API laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologu
                                        const int32_t* block_table, const int32_t* row_request,
                                        const int32_t* position, void* out, float* lse,
                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- The same from a cache held in 8 bits ---------------------------------------
+ * About half the bytes of a bf16 cache, kept and read. A cached position is d_c + d_rope
+ * numbers of 8 bits, and one scale for each of its two parts, the latent and the shared key:
+ *   cache   [n_pages][page_size, d_c + d_rope]  e4m3 (finite, 448 the largest; one byte), rows
+ *                      contiguous, pages page_stride BYTES apart (a multiple of 16; 0:
+ *                      page_size * (d_c + d_rope), which then has to be one)
+ *   scales  [n_pages][page_size][2]  uint8, contiguous: byte x stands for 2^(x - 127), [0] for the
+ *                      latent's numbers and [1] for the key's
+ * so element j of the latent is cache[j] * 2^(scales[0] - 127). laga_paged_t and the conventions
+ * of the calls above hold as they are (dtype: of q, W_kv_b, out and the tokens), pages are planned
+ * and released by the same calls, and the limits are theirs.
+ *
+ * laga_cache_append_q8: laga_cache_append, its row quantised as it is written. With a the
+ * largest finite magnitude of a part's elements, the part's scale is 2^e, e the least whole
+ * number with a <= 448 * 2^e, -100 at least and 119 at most, and each element the e4m3 number
+ * nearest to x / 2^e (ties to even), +-448 beyond them, NaN where x is not finite. The row is formed
+ * in double precision, so the byte is that of the exact value. Slots of one call must differ (of
+ * two tokens with one slot, either's bytes and scales may be stored).
+ *
+ * laga_cache_read_q8: cached positions back as numbers, row t the position[t] of request
+ * row_request[t] (NULL: of request t):
+ *   c_kv [rows, d_c], k_pe [rows, d_rope]  element dtype
+ * for instance all of a request's before the next chunk of its prompt goes through
+ * laga_reconstruct_kv and laga_attn_fwd. Exact in both element types (in bf16 and fp32 an e4m3
+ * number times a power of two that the append writes has all its bits). A row at a negative position is 0; one
+ * outside the table, or whose page lies outside the pool, NaN.
+ *
+ * laga_paged_attn_q8: laga_paged_attn on the numbers that the cache stands for. A NaN
+ * among the visible ones makes the rows that see it NaN, as would an infinity's product with zero. Statistics, sums and
+ * joins are fp32, the products take the queries with 22 bits or more and, in bf16, a probability with 11. */
+LAGA_API laga_status_t laga_cache_append_q8(const laga_paged_t* p, const laga_prologue_t* cfg,
+                                            const void* latent_raw, int64_t latent_stride,
+                                            const void* gamma, const void* kpe_raw, int64_t kpe_stride,
+                                            const int32_t* position, const int32_t* slot, void* cache,
+                                            uint8_t* scales, void* stream);
+LAGA_API laga_status_t laga_cache_read_q8(const laga_paged_t* p, const void* cache, const uint8_t* scales,
+                                          const int32_t* block_table, const int32_t* row_request,
+                                          const int32_t* position, void* c_kv, void* k_pe, void* stream);
+LAGA_API laga_status_t laga_paged_attn_q8(const laga_paged_t* p, const laga_prologue_t* cfg,
+                                          const void* q, const void* w_kv_b, const void* cache,
+                                          const uint8_t* scales, const int32_t* block_table,
+                                          const int32_t* row_request, const int32_t* position, void* out,
+                                          float* lse, void* workspace, size_t workspace_bytes,
+                                          void* stream);
 
 /* Workspace bytes of op (laga_paged_op_t); 0 if p is invalid. */
 LAGA_API size_t laga_paged_workspace_bytes(const laga_paged_t* p, int op);

@@ -13,7 +13,8 @@ from .binding import (LagaError, Problem, DTYPE_BF16, DTYPE_FP32, DQ_FROM_STORE,
                       OutProj, laga_out_proj_fwd, laga_out_proj_bwd, laga_out_proj_workspace_bytes,
                       Paged, OP_PAGE_PLAN, OP_PAGED_ATTN, PLAN_ROWS, PLAN_TABLE, PLAN_PAGES, PLAN_INVALID,
                       laga_page_plan, laga_page_release, laga_cache_append, laga_paged_attn,
-                      laga_paged_workspace_bytes)
+                      laga_paged_workspace_bytes, OP_PAGED_ATTN_Q8, laga_cache_append_q8, laga_cache_read_q8,
+                      laga_paged_attn_q8)
 
 __all__ = ["LagaError", "Problem", "DTYPE_BF16", "DTYPE_FP32", "DQ_FROM_STORE", "DQ_RECOMPUTE", "KV_MATERIALIZED",
            "KV_FUSED", "OP_FWD", "OP_BWD", "OP_PROLOGUE_BWD", "BWD_PREPARE", "BWD_DKDV", "BWD_DQ",
@@ -23,4 +24,5 @@ __all__ = ["LagaError", "Problem", "DTYPE_BF16", "DTYPE_FP32", "DQ_FROM_STORE", 
            "OutProj", "laga_out_proj_fwd", "laga_out_proj_bwd", "laga_out_proj_workspace_bytes",
            "Paged", "OP_PAGE_PLAN", "OP_PAGED_ATTN", "PLAN_ROWS", "PLAN_TABLE", "PLAN_PAGES", "PLAN_INVALID",
            "laga_page_plan", "laga_page_release", "laga_cache_append", "laga_paged_attn",
-           "laga_paged_workspace_bytes"]
+           "laga_paged_workspace_bytes", "OP_PAGED_ATTN_Q8", "laga_cache_append_q8", "laga_cache_read_q8",
+           "laga_paged_attn_q8"]

@@ -24,7 +24,7 @@ DTYPE_BF16, DTYPE_FP32 = 0, 1
 DQ_FROM_STORE, DQ_RECOMPUTE = 0, 1
 KV_MATERIALIZED, KV_FUSED = 0, 1
 OP_FWD, OP_BWD, OP_PROLOGUE_BWD = 0, 1, 2
-OP_PAGE_PLAN, OP_PAGED_ATTN = 3, 4  # laga_paged_workspace_bytes
+OP_PAGE_PLAN, OP_PAGED_ATTN, OP_PAGED_ATTN_Q8 = 3, 4, 5  # laga_paged_workspace_bytes
 PLAN_ROWS, PLAN_TABLE, PLAN_PAGES, PLAN_INVALID = 1, 2, 4, 8  # bits of a plan's status
 BWD_PREPARE, BWD_DKDV, BWD_DQ, BWD_FINISH = 0, 1, 2, 3
 
@@ -136,6 +136,7 @@ class Paged:
     def _shapes(self) -> dict:
         T, R, H = self.rows, self.requests, self.n_heads
         return {"gamma": (self.d_c,), "cache": (self.n_pages, self.page_size, self.d_c + self.d_rope), "block_table": (R, self.table_width),
+                "scales": (self.n_pages, self.page_size, 2), "c_kv": (T, self.d_c), "k_pe": (T, self.d_rope),
                 "free_pages": (self.n_pages,), "free_count": (1,), "free_count_out": (1,), "status": (1,),
                 "lengths": (R,), "lengths_out": (R,), "fresh": (R,), "drop": (R,), "row_begin": (R + 1,),
                 "row_request": (T,), "position": (T,), "slot": (T,), "latent_raw": (T, self.d_c),
@@ -222,6 +223,12 @@ def _load():
     L.laga_cache_append.argtypes = [G, Q, vp, ctypes.c_int64, vp, vp, ctypes.c_int64, vp, vp, vp, vp]
     L.laga_paged_attn.restype = ctypes.c_int
     L.laga_paged_attn.argtypes = [G, Q] + [vp] * 9 + [ctypes.c_size_t, vp]
+    L.laga_cache_append_q8.restype = ctypes.c_int
+    L.laga_cache_append_q8.argtypes = [G, Q, vp, ctypes.c_int64, vp, vp, ctypes.c_int64, vp, vp, vp, vp, vp]
+    L.laga_cache_read_q8.restype = ctypes.c_int
+    L.laga_cache_read_q8.argtypes = [G] + [vp] * 8
+    L.laga_paged_attn_q8.restype = ctypes.c_int
+    L.laga_paged_attn_q8.argtypes = [G, Q] + [vp] * 10 + [ctypes.c_size_t, vp]
     return L
 
 
@@ -539,11 +546,11 @@ def _rows_at(t, name, shape, dtype, index):
     return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
 
 
-def _cache_at(p, t, index):
+def _cache_at(p, t, index, dtype=None):
     """Address of the pool: rows contiguous in a page, pages p.page_stride elements apart."""
-    shape = p.shapes()["cache"]
-    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not p.torch_dtype or t.get_device() != index:
-        raise _fault(t, "cache", shape, p.torch_dtype, index)
+    shape, dtype = p.shapes()["cache"], dtype or p.torch_dtype
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+        raise _fault(t, "cache", shape, dtype, index)
     want = (p.page_stride or shape[1] * shape[2], shape[2], 1)
     if t.stride() != want and any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), want)):
         raise ValueError(f"cache has strides {t.stride()}, expected {want}")
@@ -652,6 +659,62 @@ def laga_paged_attn(p: Paged, q, w_kv_b, cache, block_table, position, row_reque
     cfg = None if rope_base is None else ctypes.byref(_CPrologue(0.0, rope_base, position_offset))
     _serve("laga_paged_attn", d, stream, _lib.laga_paged_attn, p.ref(), cfg, _at(q, "q", sh["q"], dt, d),
            _at(w_kv_b, "w_kv_b", sh["w_kv_b"], dt, d), _cache_at(p, cache, d),
+           _at(block_table, "block_table", sh["block_table"], i32, d),
+           None if row_request is None else _at(row_request, "row_request", sh["row_request"], i32, d),
+           _at(position, "position", sh["position"], i32, d), _at(out, "out", sh["out"], dt, d),
+           _at(lse, "lse", sh["lse"], torch.float32, d), workspace.data_ptr(), nbytes)
+    return out, lse
+
+
+def _cache_q8_at(p, cache, scales, index):
+    """Addresses of a pool in 8 bits and of its scales."""
+    return (_cache_at(p, cache, index, torch.float8_e4m3fn), _at(scales, "scales", p.shapes()["scales"], torch.uint8, index))
+
+
+def laga_cache_append_q8(p: Paged, latent_raw, kpe_raw, position, slot, cache, scales, gamma=None, eps=1e-6,
+                         rope_base=10000.0, position_offset=0, stream=None):
+    """laga_cache_append into a cache in 8 bits: cache [n_pages, page_size, d_c + d_rope] float8_e4m3fn, scales [n_pages,
+    page_size, 2] uint8, the exponents plus 127 of the powers of two that a row's latent and shared key are multiplied by.
+    Returns (cache, scales)."""
+    sh, dt, i32, d = p.shapes(), p.torch_dtype, torch.int32, _device_of(cache, "cache")
+    lat, lat_stride = _rows_at(latent_raw, "latent_raw", sh["latent_raw"], dt, d)
+    kpe, kpe_stride = _rows_at(kpe_raw, "kpe_raw", sh["kpe_raw"], dt, d)
+    cfg = _CPrologue(eps, rope_base, position_offset)
+    _serve("laga_cache_append_q8", d, stream, _lib.laga_cache_append_q8, p.ref(), ctypes.byref(cfg), lat, lat_stride,
+           None if gamma is None else _at(gamma, "gamma", sh["gamma"], dt, d), kpe, kpe_stride,
+           _at(position, "position", sh["position"], i32, d), _at(slot, "slot", sh["slot"], i32, d),
+           *_cache_q8_at(p, cache, scales, d))
+    return cache, scales
+
+
+def laga_cache_read_q8(p: Paged, cache, scales, block_table, position, row_request=None, c_kv=None, k_pe=None, stream=None):
+    """The numbers that cached positions stand for, row t the position[t] of request row_request[t] (or t); returns (c_kv
+    [rows, d_c], k_pe [rows, d_rope]) in p's element type, exactly."""
+    sh, dt, i32, d = p.shapes(), p.torch_dtype, torch.int32, _device_of(cache, "cache")
+    if c_kv is None:
+        c_kv = _output(sh["c_kv"], dt, d, stream)
+    if k_pe is None:
+        k_pe = _output(sh["k_pe"], dt, d, stream)
+    _serve("laga_cache_read_q8", d, stream, _lib.laga_cache_read_q8, p.ref(), *_cache_q8_at(p, cache, scales, d),
+           _at(block_table, "block_table", sh["block_table"], i32, d),
+           None if row_request is None else _at(row_request, "row_request", sh["row_request"], i32, d),
+           _at(position, "position", sh["position"], i32, d), _at(c_kv, "c_kv", sh["c_kv"], dt, d),
+           _at(k_pe, "k_pe", sh["k_pe"], dt, d))
+    return c_kv, k_pe
+
+
+def laga_paged_attn_q8(p: Paged, q, w_kv_b, cache, scales, block_table, position, row_request=None, rope_base=None,
+                       position_offset=0, out=None, lse=None, workspace=None, stream=None):
+    """laga_paged_attn on the numbers that a cache in 8 bits stands for; returns (out, lse)."""
+    sh, dt, i32, d = p.shapes(), p.torch_dtype, torch.int32, _device_of(q, "q")
+    if out is None:
+        out = _output(sh["out"], dt, d, stream)
+    if lse is None:
+        lse = _output(sh["lse"], torch.float32, d, stream)
+    workspace, nbytes = _serve_workspace(p, OP_PAGED_ATTN_Q8, workspace, d, stream)
+    cfg = None if rope_base is None else ctypes.byref(_CPrologue(0.0, rope_base, position_offset))
+    _serve("laga_paged_attn_q8", d, stream, _lib.laga_paged_attn_q8, p.ref(), cfg, _at(q, "q", sh["q"], dt, d),
+           _at(w_kv_b, "w_kv_b", sh["w_kv_b"], dt, d), *_cache_q8_at(p, cache, scales, d),
            _at(block_table, "block_table", sh["block_table"], i32, d),
            None if row_request is None else _at(row_request, "row_request", sh["row_request"], i32, d),
            _at(position, "position", sh["position"], i32, d), _at(out, "out", sh["out"], dt, d),

@@ -200,6 +200,12 @@ laga_status_t validate_paged(const laga_paged_t* p, PagedDims* d) {
 }
 size_t elem_size(const laga_paged_t* p) { return p->dtype == LAGA_DTYPE_BF16 ? 2 : 4; }
 
+// A cache in 8 bits: its rows are bytes, and a page begins at one divisible by 16.
+laga_status_t validate_paged_q8(const laga_paged_t* p, PagedDims* d) {
+  const laga_status_t s = validate_paged(p, d);
+  return s == LAGA_OK && d->page_stride % 16 != 0 ? LAGA_ERR_UNSUPPORTED : s;
+}
+
 // [schedule | absorbed queries | their second and third parts (bf16) | whole rows | partials: outputs, statistics]
 struct PagedWs {
   size_t sched, qa, qa_lo, qa_low2, obar, part_o, part_ml, total;
@@ -218,6 +224,40 @@ PagedWs paged_layout(const laga_paged_t* p, const PagedDims& d, const PagedPlan&
   w.part_ml = off; off += round_up(sizeof(float) * places * 2);
   w.total = off;
   return w;
+}
+
+// [schedule | absorbed queries (fp32) | their blocks' maxima | whole rows | partials: outputs, statistics]
+struct PagedQ8Ws {
+  size_t sched, qa, qa_max, obar, part_o, part_ml, total;
+};
+PagedQ8Ws paged_q8_layout(const PagedDims& d, const PagedPlan& plan) {
+  PagedQ8Ws w{};
+  const size_t rows = (size_t)d.T * d.H, places = (size_t)2 * plan.workers * d.H;
+  size_t off = 0;
+  w.sched = off; off += round_up(sizeof(int32_t) * sched_ints(d.T, plan.workers));
+  w.qa = off; off += round_up(sizeof(float) * rows * (d.d_c + d.dr));
+  w.qa_max = off; off += round_up(sizeof(float) * rows * qa_blocks(d.d_c));
+  w.obar = off; off += round_up(sizeof(float) * rows * d.d_c);
+  w.part_o = off; off += round_up(sizeof(float) * places * d.d_c);
+  w.part_ml = off; off += round_up(sizeof(float) * places * 2);
+  w.total = off;
+  return w;
+}
+
+// The attention's arguments that do not depend on what the cache holds.
+PagedArgs paged_args(const laga_paged_t* p, const laga_prologue_t* cfg, const PagedDims& d, const PagedPlan& plan) {
+  PagedArgs a{};
+  a.page_stride = d.page_stride; a.T = d.T; a.R = d.R; a.width = d.width;
+  a.n_pages = d.n_pages; a.page = d.page; a.H = d.H; a.d_c = d.d_c; a.d_nope = d.dn; a.d_rope = d.dr; a.d_v = d.dv;
+  a.scale_log2 = p->softmax_scale * 1.4426950408889634f;
+  page_division(d.page, &a.page_magic, &a.page_shift);
+  if (cfg) {
+    a.rotate = 1;
+    a.position_offset = cfg->position_offset;
+    a.log2_base = log2((double)cfg->rope_base);
+  }
+  a.wide = plan.wide; a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.groups = plan.groups;
+  return a;
 }
 
 size_t plan_ws_bytes(const PagedDims& d) { return round_up(sizeof(int32_t) * plan_ws_ints(d.R)); }
@@ -248,6 +288,27 @@ laga_status_t page_plan(const laga_paged_t* p, bool release, const int32_t* leng
   a.rows = d.T; a.R = d.R; a.width = d.width; a.n_pages = d.n_pages; a.page = d.page; a.release = release;
   page_division(d.page, &a.page_magic, &a.page_shift);
   return from_hip(launch_plan(a, (hipStream_t)stream));
+}
+
+// What both forms of the append check after the sizes.
+laga_status_t append_args(const PagedDims& d, const laga_prologue_t* cfg, const void* latent_raw, int64_t latent_stride,
+                          const void* gamma, const void* kpe_raw, int64_t kpe_stride, const int32_t* position,
+                          const int32_t* slot, void* cache, AppendArgs* out) {
+  const laga_status_t s = validate_rope(cfg, d.width * (int64_t)d.page, d.dr);
+  if (s != LAGA_OK) return s;
+  if (!latent_raw || !kpe_raw || !position || !slot || !cache) return LAGA_ERR_NULL;
+  if (latent_stride < d.d_c || kpe_stride < d.dr) return LAGA_ERR_SHAPE;
+  if (latent_stride % 8 != 0 || kpe_stride % 8 != 0 || latent_stride >= kMaxElems || kpe_stride >= kMaxElems)
+    return LAGA_ERR_UNSUPPORTED;
+  if (misaligned(latent_raw) || misaligned(kpe_raw) || misaligned(gamma) || misaligned(position) || misaligned(slot) ||
+      misaligned(cache))
+    return LAGA_ERR_ALIGN;
+  AppendArgs& a = *out;
+  a.latent = latent_raw; a.kpe = kpe_raw; a.gamma = gamma; a.latent_stride = latent_stride; a.kpe_stride = kpe_stride;
+  a.position = position; a.slot = slot; a.cache = cache; a.page_stride = d.page_stride;
+  a.position_offset = cfg->position_offset; a.T = d.T; a.d_c = d.d_c; a.d_rope = d.dr;
+  a.n_slots = d.n_pages * d.page; a.page = d.page; a.eps = cfg->eps; a.log2_base = log2((double)cfg->rope_base);
+  return LAGA_OK;
 }
 
 template <typename T>
@@ -325,6 +386,8 @@ size_t laga_paged_workspace_bytes(const laga_paged_t* p, int op) {
   if (op == LAGA_OP_PAGE_PLAN) return plan_ws_bytes(d);
   if (op == LAGA_OP_PAGED_ATTN)
     return paged_layout(p, d, paged_plan(d.H, d.d_c, d.dr, (int)elem_size(p))).total;
+  if (op == LAGA_OP_PAGED_ATTN_Q8 && validate_paged_q8(p, &d) == LAGA_OK)
+    return paged_q8_layout(d, paged_plan_q8(d.H, d.d_c)).total;
   return 0;
 }
 
@@ -348,24 +411,78 @@ laga_status_t laga_cache_append(const laga_paged_t* p, const laga_prologue_t* cf
                                 int64_t latent_stride, const void* gamma, const void* kpe_raw, int64_t kpe_stride,
                                 const int32_t* position, const int32_t* slot, void* cache, void* stream) {
   PagedDims d;
-  laga_status_t s = validate_paged(p, &d);
-  if (s != LAGA_OK) return s;
-  s = validate_rope(cfg, d.width * (int64_t)d.page, d.dr);
-  if (s != LAGA_OK) return s;
-  if (!latent_raw || !kpe_raw || !position || !slot || !cache) return LAGA_ERR_NULL;
-  if (latent_stride < d.d_c || kpe_stride < d.dr) return LAGA_ERR_SHAPE;
-  if (latent_stride % 8 != 0 || kpe_stride % 8 != 0 || latent_stride >= kMaxElems || kpe_stride >= kMaxElems)
-    return LAGA_ERR_UNSUPPORTED;
-  if (misaligned(latent_raw) || misaligned(kpe_raw) || misaligned(gamma) || misaligned(position) || misaligned(slot) ||
-      misaligned(cache))
-    return LAGA_ERR_ALIGN;
   AppendArgs a{};
-  a.latent = latent_raw; a.kpe = kpe_raw; a.gamma = gamma; a.latent_stride = latent_stride; a.kpe_stride = kpe_stride;
-  a.position = position; a.slot = slot; a.cache = cache; a.page_stride = d.page_stride;
-  a.position_offset = cfg->position_offset; a.T = d.T; a.d_c = d.d_c; a.d_rope = d.dr;
-  a.n_slots = d.n_pages * d.page; a.page = d.page; a.eps = cfg->eps; a.log2_base = log2((double)cfg->rope_base);
+  laga_status_t s = validate_paged(p, &d);
+  if (s == LAGA_OK) s = append_args(d, cfg, latent_raw, latent_stride, gamma, kpe_raw, kpe_stride, position, slot, cache, &a);
+  if (s != LAGA_OK) return s;
   hipStream_t st = (hipStream_t)stream;
   return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_append<bf16>(a, st) : launch_append<float>(a, st));
+}
+
+laga_status_t laga_cache_append_q8(const laga_paged_t* p, const laga_prologue_t* cfg, const void* latent_raw,
+                                   int64_t latent_stride, const void* gamma, const void* kpe_raw, int64_t kpe_stride,
+                                   const int32_t* position, const int32_t* slot, void* cache, uint8_t* scales,
+                                   void* stream) {
+  PagedDims d;
+  AppendQ8Args a{};
+  laga_status_t s = validate_paged_q8(p, &d);
+  if (s == LAGA_OK && !scales) s = LAGA_ERR_NULL;
+  if (s == LAGA_OK) s = append_args(d, cfg, latent_raw, latent_stride, gamma, kpe_raw, kpe_stride, position, slot, cache, &a.a);
+  if (s != LAGA_OK) return s;
+  if (misaligned(scales)) return LAGA_ERR_ALIGN;
+  a.scales = scales;
+  hipStream_t st = (hipStream_t)stream;
+  return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_append_q8<bf16>(a, st) : launch_append_q8<float>(a, st));
+}
+
+laga_status_t laga_cache_read_q8(const laga_paged_t* p, const void* cache, const uint8_t* scales, const int32_t* block_table,
+                                 const int32_t* row_request, const int32_t* position, void* c_kv, void* k_pe, void* stream) {
+  PagedDims d;
+  const laga_status_t s = validate_paged_q8(p, &d);
+  if (s != LAGA_OK) return s;
+  if (!cache || !scales || !block_table || !position || !c_kv || !k_pe) return LAGA_ERR_NULL;
+  const void* ptrs[] = {cache, scales, block_table, row_request, position, c_kv, k_pe};
+  for (const void* x : ptrs)
+    if (misaligned(x)) return LAGA_ERR_ALIGN;
+  if (!row_request && d.T > d.R) return LAGA_ERR_SHAPE;
+  ReadQ8Args a{};
+  a.cache = (const uint8_t*)cache; a.scales = scales; a.table = block_table; a.row_request = row_request;
+  a.position = position; a.c_kv = c_kv; a.k_pe = k_pe; a.page_stride = d.page_stride; a.T = d.T; a.R = d.R;
+  a.width = d.width; a.n_pages = d.n_pages; a.page = d.page; a.d_c = d.d_c; a.d_rope = d.dr;
+  page_division(d.page, &a.page_magic, &a.page_shift);
+  hipStream_t st = (hipStream_t)stream;
+  return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_read_q8<bf16>(a, st) : launch_read_q8<float>(a, st));
+}
+
+laga_status_t laga_paged_attn_q8(const laga_paged_t* p, const laga_prologue_t* cfg, const void* q, const void* w_kv_b,
+                                 const void* cache, const uint8_t* scales, const int32_t* block_table,
+                                 const int32_t* row_request, const int32_t* position, void* out, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  PagedDims d;
+  laga_status_t s = validate_paged_q8(p, &d);
+  if (s != LAGA_OK) return s;
+  if (cfg) {
+    s = validate_rope(cfg, d.width * (int64_t)d.page, d.dr);
+    if (s != LAGA_OK) return s;
+  }
+  if (!q || !w_kv_b || !cache || !scales || !block_table || !position || !out) return LAGA_ERR_NULL;
+  const void* ptrs[] = {q, w_kv_b, cache, scales, block_table, row_request, position, out, lse};
+  for (const void* x : ptrs)
+    if (misaligned(x)) return LAGA_ERR_ALIGN;
+  // a row's request must be known: without row_request there is one row per request at most
+  if (!row_request && d.T > d.R) return LAGA_ERR_SHAPE;
+  const PagedPlan plan = paged_plan_q8(d.H, d.d_c);
+  const PagedQ8Ws ws = paged_q8_layout(d, plan);
+  if (!workspace || workspace_bytes < ws.total) return LAGA_ERR_WORKSPACE;
+  if (misaligned(workspace)) return LAGA_ERR_ALIGN;
+  char* wsb = (char*)workspace;
+  PagedArgs a = paged_args(p, cfg, d, plan);
+  a.q = q; a.w = w_kv_b; a.cache = cache; a.scales = scales; a.table = block_table; a.row_request = row_request;
+  a.position = position; a.out = out; a.lse = lse;
+  a.sched = (int32_t*)(wsb + ws.sched); a.qa = wsb + ws.qa; a.qa_max = (float*)(wsb + ws.qa_max);
+  a.obar = (float*)(wsb + ws.obar); a.part_o = (float*)(wsb + ws.part_o); a.part_ml = (float*)(wsb + ws.part_ml);
+  hipStream_t st = (hipStream_t)stream;
+  return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_paged_attn_q8<bf16>(a, st) : launch_paged_attn_q8<float>(a, st));
 }
 
 laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg, const void* q, const void* w_kv_b,
@@ -390,20 +507,11 @@ laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologue_t* cfg,
   if (!workspace || workspace_bytes < ws.total) return LAGA_ERR_WORKSPACE;
   if (misaligned(workspace)) return LAGA_ERR_ALIGN;
   char* wsb = (char*)workspace;
-  PagedArgs a{};
+  PagedArgs a = paged_args(p, cfg, d, plan);
   a.q = q; a.w = w_kv_b; a.cache = cache; a.table = block_table; a.row_request = row_request; a.position = position;
-  a.out = out; a.lse = lse; a.page_stride = d.page_stride; a.T = d.T; a.R = d.R; a.width = d.width;
-  a.n_pages = d.n_pages; a.page = d.page; a.H = d.H; a.d_c = d.d_c; a.d_nope = d.dn; a.d_rope = d.dr; a.d_v = d.dv;
-  a.scale_log2 = p->softmax_scale * 1.4426950408889634f;
-  page_division(d.page, &a.page_magic, &a.page_shift);
-  if (cfg) {
-    a.rotate = 1;
-    a.position_offset = cfg->position_offset;
-    a.log2_base = log2((double)cfg->rope_base);
-  }
+  a.out = out; a.lse = lse;
   a.sched = (int32_t*)(wsb + ws.sched); a.qa = wsb + ws.qa; a.qa_lo = wsb + ws.qa_lo; a.qa_low2 = wsb + ws.qa_low2;
   a.obar = (float*)(wsb + ws.obar); a.part_o = (float*)(wsb + ws.part_o); a.part_ml = (float*)(wsb + ws.part_ml);
-  a.wide = plan.wide; a.heads_per_wg = plan.heads_per_wg; a.workers = plan.workers; a.groups = plan.groups;
   hipStream_t st = (hipStream_t)stream;
   return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_paged_attn<bf16>(a, st) : launch_paged_attn<float>(a, st));
 }

@@ -64,6 +64,29 @@ struct AppendArgs {
 template <typename T>
 hipError_t launch_append(const AppendArgs& a, hipStream_t st);
 
+// ---------------------------------------------------------------- the cache in 8 bits
+// A cached position is d_c + d_rope e4m3 numbers (AppendArgs::cache, page_stride bytes between pages) and, in `scales`
+// [n_pages][page][2], the exponents + kScaleBias of the powers of two that its latent and its shared key stand for.
+constexpr int kScaleBias = 127;
+constexpr int kLeastScale = -100, kMostScale = 119;  // exponents that are written
+struct AppendQ8Args {
+  AppendArgs a;
+  uint8_t* scales;
+};
+template <typename T>
+hipError_t launch_append_q8(const AppendQ8Args& a, hipStream_t st);
+
+struct ReadQ8Args {
+  const uint8_t *cache, *scales;
+  const int32_t *table, *row_request, *position;  // as in PagedArgs
+  void *c_kv, *k_pe;                              // [T, d_c], [T, d_rope]
+  int64_t page_stride;
+  int T, R, width, n_pages, page, d_c, d_rope;
+  uint32_t page_magic, page_shift;
+};
+template <typename T>
+hipError_t launch_read_q8(const ReadQ8Args& a, hipStream_t st);
+
 // 8 contiguous elements to and from fp32 (bf16 rounds to nearest even)
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
@@ -117,7 +140,12 @@ struct PagedArgs {
   int heads_per_wg;  // heads of a head block
   int workers;       // of each head block
   int groups;        // of 32 heads in heads_per_wg, for few tiles (wide kernel), or 0
+  // a cache in 8 bits: qa is fp32, and
+  const uint8_t* scales;  // [n_pages][page][2]
+  float* qa_max;          // [T][H][qa_blocks(d_c)]: largest magnitudes of qa's blocks of kQaBlock columns, and of the band's
 };
+constexpr int kQaBlock = 128;
+__host__ __device__ inline int qa_blocks(int d_c) { return (d_c + kQaBlock - 1) / kQaBlock + 1; }
 // Layout of the tiles: [units per worker, units, groups, units of a row's cost, whether two successive rows have one
 // request], units before each row [T + 1], and of
 // each worker's first share (kShareInts) the row, its first tile and end, request and visible keys.
@@ -188,8 +216,24 @@ inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
   return p;
 }
 
+// A cache in 8 bits: a wave has 16 heads, with all that they need in its registers up to d_c = 512; above, two waves halve
+// the columns of their sums.
+inline PagedPlan paged_plan_q8(int H, int d_c) {
+  PagedPlan p{};
+  const int most = d_c <= 512 ? 64 : 32;
+  p.head_blocks = (H + most - 1) / most;
+  p.heads_per_wg = (H + p.head_blocks - 1) / p.head_blocks;
+  const int w = kCus / p.head_blocks / 8 * 8;  // whole rounds over the 8 XCDs
+  p.workers = w > 8 ? w : 8;
+  return p;
+}
+
 void launch_paged_wide(const PagedArgs& a, int head_blocks, hipStream_t st);
 template <typename T>
 hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t st);
+template <typename T>
+void launch_paged_split_q8(const PagedArgs& a, int head_blocks, hipStream_t st);
+template <typename T>
+hipError_t launch_paged_attn_q8(const PagedArgs& a, hipStream_t st);
 
 }  // namespace laga

@@ -27,6 +27,7 @@ namespace {
 // leave through LDS in rows of 256 bytes. Beside them one workgroup per token turns its
 // q_rope, and one lays out the tiles.
 constexpr int kAbsorbWaves = 4, kAbsorbRows = 32 * kAbsorbWaves;
+static_assert(kAbsorbRows == kQaBlock);
 
 // N elements of qa; bf16 in three parts, each the rounding of what the ones before leave (the sum is
 // within 2^-25 of the value: the scores of a row with one key are its lse, and two parts left 2.5e-6 there).
@@ -65,7 +66,8 @@ __device__ __forceinline__ void band_parts(float y, bf16 (&part)[3]) {
   }
 }
 
-template <typename T, int DN>
+// Q8 (here and below): qa stays in fp32, and the largest magnitude of each row of a block is left beside it.
+template <typename T, int DN, bool Q8>
 __device__ void absorb_product(const PagedArgs& a, int blk, int cblocks, int tpart, int tparts) {
   constexpr int E = 16 / sizeof(T), CPR = DN / E, PO = kAbsorbRows + 4;  // chunks of a row; pitch of the results
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -107,11 +109,24 @@ __device__ void absorb_product(const PagedArgs& a, int blk, int cblocks, int tpa
     lds_barrier();
     for (int x = threadIdx.x; x < nt * (kAbsorbRows / E); x += 64 * kAbsorbWaves) {
       const int r = x / (kAbsorbRows / E), c = x % (kAbsorbRows / E) * E;
-      if (c >= nc) continue;
+      const int64_t th = (int64_t)(t0 + r) * a.H + h;
+      if (!Q8 && c >= nc) continue;
       float y[E];
 #pragma unroll
       for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>(y + i) = *reinterpret_cast<const f32x4*>(so + r * PO + c + i);
-      store_parts<T, E>(a, ((int64_t)(t0 + r) * a.H + h) * W + c0 + c, y);
+      if constexpr (Q8) {
+        float top = 0.f;  // (rows of W past the end repeat the last one: they change no maximum)
+#pragma unroll
+        for (int i = 0; i < E; ++i) top = fmaxf(top, fabsf(y[i]));
+#pragma unroll
+        for (int o = 1; o < kAbsorbRows / E; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));  // (the lanes of a row are all here)
+        if (c == 0) a.qa_max[th * qa_blocks(a.d_c) + c0 / kQaBlock] = top;
+        if (c < nc)
+#pragma unroll
+          for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>((float*)a.qa + th * W + c0 + c + i) = *reinterpret_cast<f32x4*>(y + i);
+      } else {
+        store_parts<T, E>(a, th * W + c0 + c, y);
+      }
     }
     if (t0 + tparts * 32 < a.T) lds_barrier();  // q and the results are read
   }
@@ -124,7 +139,7 @@ constexpr size_t absorb_lds() {
 // q_rope of one token, every head: a thread keeps one pair's angle and has eight heads' pairs under way (one
 // after the other, the launch took 11 us for 2 rows of 128 heads, so 7)
 constexpr int kBandHeads = 8;
-template <typename T>
+template <typename T, bool Q8>
 __device__ void absorb_band(const PagedArgs& a, int t) {
   const int pairs = a.d_rope / 2, i = threadIdx.x % pairs;
   const int W = a.d_c + a.d_rope, dqk = a.d_nope + a.d_rope;
@@ -143,8 +158,14 @@ __device__ void absorb_band(const PagedArgs& a, int t) {
       if (h0 + u * step >= a.H) break;
       const float x0 = to_f32(x[u][0]), x1 = to_f32(x[u][1]);
       const float y[2] = {x0 * cs - x1 * sn, x0 * sn + x1 * cs};
-      const int64_t at = ((int64_t)t * a.H + h0 + u * step) * W + a.d_c + 2 * i;
-      if constexpr (kTwo<T>) {
+      const int64_t th = (int64_t)t * a.H + h0 + u * step, at = th * W + a.d_c + 2 * i;
+      if constexpr (Q8) {
+        float top = fmaxf(fabsf(y[0]), fabsf(y[1]));
+        for (int o = 1; o < pairs; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));  // (the lanes of a head are all here)
+        const int blocks = qa_blocks(a.d_c);
+        if (i == 0) a.qa_max[th * blocks + blocks - 1] = top;
+        *reinterpret_cast<float2*>((float*)a.qa + at) = float2{y[0], y[1]};
+      } else if constexpr (kTwo<T>) {
         bf16 part[2][3];
 #pragma unroll
         for (int e = 0; e < 2; ++e) band_parts(y[e], part[e]);
@@ -249,13 +270,13 @@ __device__ void lay_out_tiles(const PagedArgs& a) {
 }
 constexpr size_t layout_lds() { return sizeof(int32_t) * (3 * kLayoutLds + 2 * kAbsorbWaves); }
 
-template <typename T, int DN>
+template <typename T, int DN, bool Q8>
 __global__ __launch_bounds__(64 * kAbsorbWaves) void absorb_kernel(PagedArgs a, int cblocks, int tparts) {
   // the few long jobs first
   const int others = a.T + 1, id = blockIdx.x;
   if (id == 0) lay_out_tiles(a);
-  else if (id < others) absorb_band<T>(a, id - 1);
-  else absorb_product<T, DN>(a, (id - others) / tparts, cblocks, (id - others) % tparts, tparts);
+  else if (id < others) absorb_band<T, Q8>(a, id - 1);
+  else absorb_product<T, DN, Q8>(a, (id - others) / tparts, cblocks, (id - others) % tparts, tparts);
 }
 
 // ---------------------------------------------------------------- split attention
@@ -352,7 +373,7 @@ constexpr int kJoinRed = 16384;  // LDS in which the waves' sums meet
 // once. A workgroup takes every tparts-th block of rows, and reads the next one's o beside this one's
 // products: with one block per workgroup, each waited for W_v and o (300 rows, 128 heads: 72 us, so 46). Bound by
 // the latency of those two reads with few rows, by reading o with many.
-template <typename T, int DV, int NB, int NST>  // NB 32-column blocks of out; NST steps of 16 per wave
+template <typename T, int DV, int NB, int NST, bool FIX>  // NB 32-column blocks of out; NST steps of 16 per wave; FIX: lse lacks qa_low2's share
 __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tparts) {
   constexpr int E = 16 / sizeof(T), CPR = 32 * NB / E;  // 16-byte chunks of a staged row
   typedef typename FragOf<T>::half quad;
@@ -367,7 +388,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tparts) {
   const int dc = a.d_c, nch = dc * CPR, step = 32 * tparts;
   const int64_t ldw = (int64_t)a.H * (a.d_nope + DV);
   const T* wv = (const T*)a.w + (int64_t)h * (a.d_nope + DV) + a.d_nope + 32 * NB * vb;
-  const bool fix = kTwo<T> && a.lse && vb == 0;
+  const bool fix = FIX && a.lse && vb == 0;
   const int32_t* before = a.sched + kSchedHeader;
   // step i of this wave: columns 16 (NST wave + i) + {4 g .. + 3, 8 + 4 g .. + 3}
   const int c0 = 16 * NST * wave + 4 * g;
@@ -384,7 +405,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tparts) {
     return r;
   };
   f32x4 x[NST][2];
-  quad y[kTwo<T> ? NST : 1][2];
+  quad y[FIX ? NST : 1][2];
   const T* lacks = (const T*)a.qa_low2;
   auto load = [&](int i, int t, const Row& r) {
     x[i][0] = x[i][1] = f32x4{r.fill, r.fill, r.fill, r.fill};
@@ -393,7 +414,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tparts) {
       const float* o = a.obar + th * dc + c0 + 16 * i;
       x[i][0] = *reinterpret_cast<const f32x4*>(o);
       x[i][1] = *reinterpret_cast<const f32x4*>(o + 8);
-      if constexpr (kTwo<T>)
+      if constexpr (FIX)
         if (fix) {
           const T* q = lacks + th * (dc + a.d_rope) + c0 + 16 * i;
           y[i][0] = *reinterpret_cast<const quad*>(q);
@@ -421,7 +442,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tparts) {
     if (fix) {
       if (now.seen) lse = a.lse[th];
       float dot = 0.f;
-      if constexpr (kTwo<T>)
+      if constexpr (FIX)
         if (now.seen)
 #pragma unroll
           for (int i = 0; i < NST; ++i)
@@ -484,24 +505,24 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int tparts) {
   }
 }
 
-template <typename T, int DV, int NB>
+template <typename T, int DV, bool FIX, int NB>
 void launch_join_product(const PagedArgs& a, hipStream_t st) {
   const size_t lds = kJoinRed + (size_t)a.d_c * 32 * NB * sizeof(T);
   const int64_t blocks = (int64_t)a.H * (DV / (32 * NB));
   const int tb = (a.T + 31) / 32, want = (int)((kCus * (160 * 1024 / lds) + blocks - 1) / blocks);  // what runs at once
   const int tparts = tb < want ? tb : want;
   const unsigned wgs = (unsigned)(blocks * tparts);
-  if (a.d_c <= 128) join_kernel<T, DV, NB, 2><<<wgs, 256, lds, st>>>(a, tparts);
-  else if (a.d_c <= 256) join_kernel<T, DV, NB, 4><<<wgs, 256, lds, st>>>(a, tparts);
-  else if (a.d_c <= 512) join_kernel<T, DV, NB, 8><<<wgs, 256, lds, st>>>(a, tparts);
-  else if constexpr (NB == 1 || 64 * NB == DV) join_kernel<T, DV, NB, 16><<<wgs, 256, lds, st>>>(a, tparts);
+  if (a.d_c <= 128) join_kernel<T, DV, NB, 2, FIX><<<wgs, 256, lds, st>>>(a, tparts);
+  else if (a.d_c <= 256) join_kernel<T, DV, NB, 4, FIX><<<wgs, 256, lds, st>>>(a, tparts);
+  else if (a.d_c <= 512) join_kernel<T, DV, NB, 8, FIX><<<wgs, 256, lds, st>>>(a, tparts);
+  else if constexpr (NB == 1 || 64 * NB == DV) join_kernel<T, DV, NB, 16, FIX><<<wgs, 256, lds, st>>>(a, tparts);
 }
 
 // The same for one row and head per workgroup, partials and all, in fp32: where there are no more of
 // them than CUs. W_v's rows are on their way to registers (16 bytes of a row per thread, up to
 // kVecRows rows) before the partials are known. 256 threads for small heads, else 1024.
 constexpr int kVecRows = 16;
-template <typename T, int DV, int NT>
+template <typename T, int DV, int NT, bool FIX>
 __global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
   constexpr int E = 16 / sizeof(T), CPR = DV / E, SLICES = NT / CPR;  // columns of a thread; threads of a row
   typedef __attribute__((__vector_size__(16))) T chunk_t;
@@ -518,7 +539,7 @@ __global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
   const RowParts r = parts_of(a, t);
   // what lse lacks, in the first wave
   float lack[2][8] = {};
-  if (kTwo<T> && a.lse && tid < 64 && r.seen) {
+  if (FIX && a.lse && tid < 64 && r.seen) {
     const T* q = (const T*)a.qa_low2 + th * (dc + a.d_rope);
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -548,7 +569,7 @@ __global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
   __syncthreads();
   if (a.lse && tid < 64) {
     float dot = 0.f;
-    if (kTwo<T> && r.seen) {
+    if (FIX && r.seen) {
 #pragma unroll
       for (int k = 0; k < 2; ++k)
         if (8 * tid + 512 * k < dc)
@@ -589,15 +610,15 @@ __global__ __launch_bounds__(NT) void join_vec_kernel(PagedArgs a) {
   }
 }
 
-template <typename T, int DV>
+template <typename T, int DV, bool FIX>
 void launch_join(const PagedArgs& a, hipStream_t st) {
   const int64_t pairs = (int64_t)a.T * a.H;
   // both in one launch where no workgroup would wait for another: 16 heads of one row 7.6 us (4.7 + 6.7 in two), 2
   // rows of 128 heads 23.6 (18.4 + 10.4). Small heads with 256 threads: 5.1 us, 8.9 with 1024 (8 rows, 4
   // heads, d_c = 64, fp32).
   if (pairs <= kCus) {
-    if (a.d_c * DV <= 128 * 64) join_vec_kernel<T, DV, 256><<<(unsigned)pairs, 256, 0, st>>>(a);
-    else join_vec_kernel<T, DV, 1024><<<(unsigned)pairs, 1024, 0, st>>>(a);
+    if (a.d_c * DV <= 128 * 64) join_vec_kernel<T, DV, 256, FIX><<<(unsigned)pairs, 256, 0, st>>>(a);
+    else join_vec_kernel<T, DV, 1024, FIX><<<(unsigned)pairs, 1024, 0, st>>>(a);
     return;
   }
   // one head per workgroup; eight where most rows cannot be shared, being more than the workers (300 rows, 128
@@ -610,32 +631,33 @@ void launch_join(const PagedArgs& a, hipStream_t st) {
   constexpr int NB = DV / 32;
   if constexpr (sizeof(T) == 2 && NB > 1)
     if ((int64_t)a.H * ((a.T + 31) / 32) >= kCus / 2) {
-      if (a.d_c <= 512) return launch_join_product<T, DV, NB>(a, st);
-      return launch_join_product<T, DV, NB / 2>(a, st);
+      if (a.d_c <= 512) return launch_join_product<T, DV, FIX, NB>(a, st);
+      return launch_join_product<T, DV, FIX, NB / 2>(a, st);
     }
-  launch_join_product<T, DV, 1>(a, st);
+  launch_join_product<T, DV, FIX, 1>(a, st);
 }
 
-template <typename T, int DN>
+template <typename T, int DN, bool Q8>
 hipError_t launch_paged_t(const PagedArgs& a, hipStream_t st) {
   const int cblocks = (a.d_c + kAbsorbRows - 1) / kAbsorbRows;
   const int64_t blocks = (int64_t)a.H * cblocks;
   const int ttiles = (a.T + 31) / 32;
   const int want = (int)((4 * kCus + blocks - 1) / blocks), tparts = ttiles < want ? ttiles : want;
-  absorb_kernel<T, DN><<<(unsigned)(a.T + 1 + blocks * tparts), 64 * kAbsorbWaves, max(absorb_lds<T, DN>(), layout_lds()), st>>>(
+  absorb_kernel<T, DN, Q8><<<(unsigned)(a.T + 1 + blocks * tparts), 64 * kAbsorbWaves, max(absorb_lds<T, DN>(), layout_lds()), st>>>(
       a, cblocks, tparts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int hb = (a.H + a.heads_per_wg - 1) / a.heads_per_wg;
   const unsigned wgs = (unsigned)(hb * a.workers);
-  if (a.wide) launch_paged_wide(a, hb, st);
+  if constexpr (Q8) launch_paged_split_q8<T>(a, hb, st);
+  else if (a.wide) launch_paged_wide(a, hb, st);
   else if (a.d_c <= 128) split_kernel<T, 1><<<wgs, 256, 0, st>>>(a, hb);
   else if (a.d_c <= 256) split_kernel<T, 2><<<wgs, 256, 0, st>>>(a, hb);
   else if (a.d_c <= 512) split_kernel<T, 4><<<wgs, 256, 0, st>>>(a, hb);
   else split_kernel<T, 8><<<wgs, 256, 0, st>>>(a, hb);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  launch_join<T, DN>(a, st);
+  launch_join<T, DN, kTwo<T> && !Q8>(a, st);
   return hipGetLastError();
 }
 
@@ -643,12 +665,20 @@ hipError_t launch_paged_t(const PagedArgs& a, hipStream_t st) {
 
 template <typename T>
 hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t st) {
-  if (a.d_nope == 128) return launch_paged_t<T, 128>(a, st);
-  if (a.d_nope == 64) return launch_paged_t<T, 64>(a, st);
-  return launch_paged_t<T, 32>(a, st);
+  if (a.d_nope == 128) return launch_paged_t<T, 128, false>(a, st);
+  if (a.d_nope == 64) return launch_paged_t<T, 64, false>(a, st);
+  return launch_paged_t<T, 32, false>(a, st);
+}
+template <typename T>
+hipError_t launch_paged_attn_q8(const PagedArgs& a, hipStream_t st) {
+  if (a.d_nope == 128) return launch_paged_t<T, 128, true>(a, st);
+  if (a.d_nope == 64) return launch_paged_t<T, 64, true>(a, st);
+  return launch_paged_t<T, 32, true>(a, st);
 }
 
 template hipError_t launch_paged_attn<bf16>(const PagedArgs&, hipStream_t);
 template hipError_t launch_paged_attn<float>(const PagedArgs&, hipStream_t);
+template hipError_t launch_paged_attn_q8<bf16>(const PagedArgs&, hipStream_t);
+template hipError_t launch_paged_attn_q8<float>(const PagedArgs&, hipStream_t);
 
 }  // namespace laga

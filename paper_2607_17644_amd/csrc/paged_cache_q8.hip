@@ -1,0 +1,220 @@
+// Rows of a paged cache held in 8 bits: written as they are quantised, and read back.
+//
+// Of each part x of a row (the normalised latent, the rotated key), with a its largest finite magnitude:
+//   e = the least whole number with a <= 448 2^e (448 the largest e4m3 number), kLeastScale at least, kMostScale at most
+//   byte j = e4m3(x_j 2^-e), to nearest, ties to even, at most 448 in magnitude; NaN where x_j is no finite number
+// A power of two leaves every bit of the mantissa to the number, and its product with one is exact in bf16 and fp32.
+#include "common.hpp"
+#include "paged.hpp"
+#include "rope.hpp"
+
+namespace laga {
+namespace {
+
+typedef __attribute__((__vector_size__(2 * sizeof(int)))) int i32x2;
+
+// The row is formed in double precision: half a step of e4m3 decides over an eighth of the value, and in
+// single precision some 40 of the 9.4 million bytes of 16384 tokens fall to the other side.
+// The e of one number alone: of a part, the largest of its numbers'.
+__device__ __forceinline__ int exponent_of(double x) {
+  const uint64_t u = (uint64_t)__builtin_bit_cast(int64_t, x) & ~((uint64_t)1 << 63);
+  const int e = (int)(u >> 52);
+  return e == 2047 ? kLeastScale : e - 1023 - 8 + ((u & (((uint64_t)1 << 52) - 1)) > (uint64_t)3 << 50);
+}
+// The number in fp32 with its last bit set where anything was cut off, so that e4m3's rounding of it is that of x itself.
+// Below 2^-30, which is zero in e4m3: zero.
+__device__ __forceinline__ float cut(double x) {
+  const uint64_t u = (uint64_t)__builtin_bit_cast(int64_t, x);
+  const uint32_t hi = (uint32_t)(u >> 32), lo = (uint32_t)u, mag = hi & 0x7fffffffu;
+  uint32_t f = ((mag - 0x38000000u) << 3) | lo >> 29 | ((lo & 0x1fffffffu) != 0);
+  f = mag < 0x3e100000u ? 0u : mag >= 0x7ff00000u ? 0x7fc00000u : f;
+  return __builtin_bit_cast(float, f | (hi & 0x80000000u));
+}
+// x 2^-e as e4m3 will have it, and four of them
+__device__ __forceinline__ float eighth(double x, int e) {
+  const float f = cut(__builtin_ldexp(x, -e));
+  return f != f ? f : __builtin_amdgcn_fmed3f(f, -448.f, 448.f);
+}
+__device__ __forceinline__ int four(const double (&x)[4], int e) {
+  int y = __builtin_amdgcn_cvt_pk_fp8_f32(eighth(x[0], e), eighth(x[1], e), 0, false);
+  return __builtin_amdgcn_cvt_pk_fp8_f32(eighth(x[2], e), eighth(x[3], e), y, true);
+}
+__device__ __forceinline__ int within(int e) { return min(max(e, kLeastScale), kMostScale); }
+
+constexpr int kWaves = 4;  // per workgroup
+// A wave per token and turn, a chunk of 8 numbers per lane (CH above 512); then its lanes take a pair of the
+// shared key each, of 64 / (d_rope / 2) tokens at a time.
+template <typename T, int TPW, int CH>
+__global__ __launch_bounds__(64 * kWaves) void append_q8_kernel(AppendQ8Args args) {
+  const AppendArgs& a = args.a;
+  const int l = threadIdx.x & 63;
+  const int64_t t0 = ((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) * TPW;
+  if (t0 >= a.T) return;  // wave-uniform; the kernel has no barrier
+  const int nch = a.d_c / 8, width = a.d_c + a.d_rope;
+  uint8_t* cache = (uint8_t*)a.cache;
+  auto row_of = [&](int slot) {
+    return cache + (int64_t)(slot / a.page) * a.page_stride + (int64_t)(slot % a.page) * width;
+  };
+
+  float v[TPW][CH][8];
+  int slot[TPW];
+#pragma unroll
+  for (int i = 0; i < TPW; ++i) {
+    slot[i] = t0 + i < a.T ? a.slot[t0 + i] : -1;
+    if ((unsigned)slot[i] >= (unsigned)a.n_slots) slot[i] = -1;
+    const T* x = (const T*)a.latent + (t0 + i < a.T ? t0 + i : t0) * a.latent_stride;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int ch = l + 64 * k;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][k][e] = 0.f;
+      if (ch < nch) load8(x + 8 * ch, v[i][k]);
+    }
+  }
+  float g[CH][8];
+#pragma unroll
+  for (int k = 0; k < CH; ++k) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) g[k][e] = 1.f;
+    if (a.gamma && l + 64 * k < nch) load8((const T*)a.gamma + 8 * (l + 64 * k), g[k]);
+  }
+#pragma unroll
+  for (int i = 0; i < TPW; ++i) {
+    if (slot[i] < 0) continue;  // wave-uniform
+    double ss = 0.;
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = __builtin_fma((double)v[i][k][e], (double)v[i][k][e], ss);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) ss += __shfl_xor(ss, o);
+    const double r = 1. / sqrt(ss / (double)a.d_c + (double)a.eps);
+    double y[CH][2][4];
+    int most = kLeastScale;
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double x = (double)v[i][k][e] * r * (double)g[k][e];
+        y[k][e / 4][e % 4] = x;
+        if (l + 64 * k < nch) most = max(most, exponent_of(x));
+      }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) most = max(most, __shfl_xor(most, o));
+    const int e = within(most);
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+      if (l + 64 * k < nch) *reinterpret_cast<i32x2*>(row_of(slot[i]) + 8 * (l + 64 * k)) = i32x2{four(y[k][0], e), four(y[k][1], e)};
+    if (l == 0) args.scales[2 * (int64_t)slot[i]] = (uint8_t)(e + kScaleBias);
+  }
+
+  const int pairs = a.d_rope / 2, p = l % pairs;  // pairs divides 64
+  const double freq = rope_freq(p, a.d_rope, a.log2_base);
+  for (int i = l / pairs; i < TPW; i += 64 / pairs) {
+    const int64_t t = t0 + i;
+    if (t >= a.T) break;
+    const int s = a.slot[t];
+    if ((unsigned)s >= (unsigned)a.n_slots) continue;
+    double cs, sn;
+    rope_sincos(a.position_offset + a.position[t], freq, cs, sn);
+    const T* x = (const T*)a.kpe + t * a.kpe_stride + 2 * p;
+    const double x0 = to_f32(x[0]), x1 = to_f32(x[1]);
+    const double y[4] = {x0 * cs - x1 * sn, x0 * sn + x1 * cs, 0., 0.};
+    int most = max(exponent_of(y[0]), exponent_of(y[1]));
+    for (int o = 1; o < pairs; o <<= 1) most = max(most, __shfl_xor(most, o));  // (the lanes of a token are all here)
+    const int e = within(most);
+    *reinterpret_cast<uint16_t*>(row_of(s) + a.d_c + 2 * p) = (uint16_t)four(y, e);
+    if (p == 0) args.scales[2 * (int64_t)s + 1] = (uint8_t)(e + kScaleBias);
+  }
+}
+
+// Rows back as numbers: a workgroup looks up the places of `rows` of them, then each thread takes 8 numbers of a row at a
+// time, several on their way at once.
+constexpr int kReadThreads = 256, kReadRows = 32;
+template <typename T>
+__global__ __launch_bounds__(kReadThreads) void read_q8_kernel(ReadQ8Args a, int rows) {
+  __shared__ const uint8_t* s_src[kReadRows];
+  __shared__ int s_exp[kReadRows];
+  __shared__ float s_fill[kReadRows];
+  const int64_t t0 = (int64_t)blockIdx.x * rows;
+  const int have = (int)min((int64_t)rows, a.T - t0), W = a.d_c + a.d_rope;
+  if ((int)threadIdx.x < have) {
+    const int64_t t = t0 + threadIdx.x;
+    const int pos = a.position[t];
+    const uint8_t* src = nullptr;
+    float fill = 0.f;
+    int exps = 0;
+    if (pos >= 0) {
+      fill = NAN;
+      const int64_t r = a.row_request ? a.row_request[t] : t;
+      if ((uint64_t)r < (uint64_t)a.R && pos < a.width * a.page) {
+        const int pg = (int)((uint64_t)(uint32_t)pos * a.page_magic >> a.page_shift), off = pos - pg * a.page;
+        const int id = a.table[r * a.width + pg];
+        if ((unsigned)id < (unsigned)a.n_pages) {
+          src = a.cache + id * a.page_stride + (int64_t)off * W;
+          exps = *reinterpret_cast<const uint16_t*>(a.scales + 2 * ((int64_t)id * a.page + off));
+        }
+      }
+    }
+    s_src[threadIdx.x] = src;
+    s_exp[threadIdx.x] = exps;
+    s_fill[threadIdx.x] = fill;
+  }
+  __syncthreads();
+  const int nch = W / 8;
+#pragma unroll 4
+  for (int x = threadIdx.x; x < have * nch; x += kReadThreads) {
+    const int i = x / nch, c = 8 * (x - i * nch);
+    const uint8_t* src = s_src[i];
+    float y[8];
+    if (src) {
+      const i32x2 b = *reinterpret_cast<const i32x2*>(src + c);
+      const int e = (c < a.d_c ? s_exp[i] & 255 : s_exp[i] >> 8) - kScaleBias;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(b[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(b[k], true);
+        y[4 * k] = __builtin_ldexpf(lo[0], e);
+        y[4 * k + 1] = __builtin_ldexpf(lo[1], e);
+        y[4 * k + 2] = __builtin_ldexpf(hi[0], e);
+        y[4 * k + 3] = __builtin_ldexpf(hi[1], e);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = s_fill[i];
+    }
+    T* to = c < a.d_c ? (T*)a.c_kv + (t0 + i) * a.d_c + c : (T*)a.k_pe + (t0 + i) * a.d_rope + (c - a.d_c);
+    store8(to, y);
+  }
+}
+
+template <typename T, int TPW>
+void launch_append_q8_t(const AppendQ8Args& a, hipStream_t st) {
+  const int per = kWaves * TPW;
+  const unsigned wgs = (unsigned)(((int64_t)a.a.T + per - 1) / per);
+  if (a.a.d_c <= 512) append_q8_kernel<T, TPW, 1><<<wgs, 64 * kWaves, 0, st>>>(a);
+  else append_q8_kernel<T, TPW, 2><<<wgs, 64 * kWaves, 0, st>>>(a);
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_append_q8(const AppendQ8Args& a, hipStream_t st) {
+  if (a.a.T <= 16 * kCus) launch_append_q8_t<T, 1>(a, st);
+  else launch_append_q8_t<T, 2>(a, st);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_read_q8(const ReadQ8Args& a, hipStream_t st) {
+  const int rows = a.T >= 4 * kCus * kReadRows ? kReadRows : 4;
+  read_q8_kernel<T><<<(unsigned)(((int64_t)a.T + rows - 1) / rows), kReadThreads, 0, st>>>(a, rows);
+  return hipGetLastError();
+}
+
+template hipError_t launch_append_q8<bf16>(const AppendQ8Args&, hipStream_t);
+template hipError_t launch_append_q8<float>(const AppendQ8Args&, hipStream_t);
+template hipError_t launch_read_q8<bf16>(const ReadQ8Args&, hipStream_t);
+template hipError_t launch_read_q8<float>(const ReadQ8Args&, hipStream_t);
+
+}  // namespace laga
