@@ -419,8 +419,8 @@ LAGA_API laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologu
  *   cache   [n_pages][page_size, d_c + d_rope]  e4m3 (finite, 448 the largest; one byte), rows
  *                      contiguous, pages page_stride BYTES apart (a multiple of 16; 0:
  *                      page_size * (d_c + d_rope), which then has to be one)
- *   scales  [n_pages][page_size][2]  uint8, contiguous: byte x stands for 2^(x - 127), [0] for the
- *                      latent's numbers and [1] for the key's
+ *   scales  [n_pages][page_size][2]  uint8, contiguous: byte x stands for 2^(x - 127), 255 for NaN;
+ *                      [0] is the latent's, [1] the key's
  * so element j of the latent is cache[j] * 2^(scales[0] - 127). laga_paged_t and the conventions
  * of the calls above hold as they are (dtype: of q, W_kv_b, out and the tokens), pages are planned
  * and released by the same calls, and the limits are theirs.

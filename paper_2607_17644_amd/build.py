@@ -38,7 +38,7 @@ FLAGS = [
 # softmax / dZ arithmetic on the accumulators needs no AGPR<->VGPR copies).
 EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
          for f in ("attn_fwd.hip", "attn_fwd_half.hip", "attn_bwd_dq.hip", "attn_bwd_dq_half.hip", "attn_bwd_kv.hip",
-                   "attn_bwd_half.hip")}
+                   "attn_bwd_half.hip", "paged_q8.hip")}
 
 
 def _compile(src: str) -> str:

@@ -140,7 +140,7 @@ struct PagedArgs {
   int heads_per_wg;  // heads of a head block
   int workers;       // of each head block
   int groups;        // of 32 heads in heads_per_wg, for few tiles (wide kernel), or 0
-  // a cache in 8 bits: qa is fp32, and
+  // a cache in 8 bits: qa is fp32 [T][(d_c + d_rope) / 4][H][4], and
   const uint8_t* scales;  // [n_pages][page][2]
   float* qa_max;          // [T][H][qa_blocks(d_c)]: largest magnitudes of qa's blocks of kQaBlock columns, and of the band's
 };
@@ -216,11 +216,11 @@ inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
   return p;
 }
 
-// A cache in 8 bits: a wave has 16 heads, with all that they need in its registers up to d_c = 512; above, two waves halve
-// the columns of their sums.
+// A cache in 8 bits: a wave has 16 heads, with all that they need in its registers up to d_c = 512; above, the four waves of
+// a workgroup share the columns of their sums.
 inline PagedPlan paged_plan_q8(int H, int d_c) {
   PagedPlan p{};
-  const int most = d_c <= 512 ? 64 : 32;
+  const int most = d_c <= 512 ? 64 : 16;
   p.head_blocks = (H + most - 1) / most;
   p.heads_per_wg = (H + p.head_blocks - 1) / p.head_blocks;
   const int w = kCus / p.head_blocks / 8 * 8;  // whole rounds over the 8 XCDs

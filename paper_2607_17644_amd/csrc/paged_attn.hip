@@ -66,7 +66,11 @@ __device__ __forceinline__ void band_parts(float y, bf16 (&part)[3]) {
   }
 }
 
-// Q8 (here and below): qa stays in fp32, and the largest magnitude of each row of a block is left beside it.
+// Q8 (here and below): qa stays in fp32, four of a head's next to the same four of the next head's, as the split reads them,
+// and the largest magnitude of each row of a block is left beside it.
+__device__ __forceinline__ f32x4* q8_place(const PagedArgs& a, int t, int h, int c) {
+  return (f32x4*)a.qa + ((int64_t)t * ((a.d_c + a.d_rope) / 4) + c / 4) * a.H + h;
+}
 template <typename T, int DN, bool Q8>
 __device__ void absorb_product(const PagedArgs& a, int blk, int cblocks, int tpart, int tparts) {
   constexpr int E = 16 / sizeof(T), CPR = DN / E, PO = kAbsorbRows + 4;  // chunks of a row; pitch of the results
@@ -123,7 +127,7 @@ __device__ void absorb_product(const PagedArgs& a, int blk, int cblocks, int tpa
         if (c == 0) a.qa_max[th * qa_blocks(a.d_c) + c0 / kQaBlock] = top;
         if (c < nc)
 #pragma unroll
-          for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>((float*)a.qa + th * W + c0 + c + i) = *reinterpret_cast<f32x4*>(y + i);
+          for (int i = 0; i < E; i += 4) *q8_place(a, t0 + r, h, c0 + c + i) = *reinterpret_cast<f32x4*>(y + i);
       } else {
         store_parts<T, E>(a, th * W + c0 + c, y);
       }
@@ -164,7 +168,8 @@ __device__ void absorb_band(const PagedArgs& a, int t) {
         for (int o = 1; o < pairs; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));  // (the lanes of a head are all here)
         const int blocks = qa_blocks(a.d_c);
         if (i == 0) a.qa_max[th * blocks + blocks - 1] = top;
-        *reinterpret_cast<float2*>((float*)a.qa + at) = float2{y[0], y[1]};
+        float2* to = (float2*)q8_place(a, t, h0 + u * step, a.d_c + (2 * i & ~3));
+        to[i & 1] = float2{y[0], y[1]};
       } else if constexpr (kTwo<T>) {
         bf16 part[2][3];
 #pragma unroll

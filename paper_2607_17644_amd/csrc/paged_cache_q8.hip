@@ -12,9 +12,12 @@ namespace laga {
 namespace {
 
 typedef __attribute__((__vector_size__(2 * sizeof(int)))) int i32x2;
+typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
 
 // The row is formed in double precision: half a step of e4m3 decides over an eighth of the value, and in
-// single precision some 40 of the 9.4 million bytes of 16384 tokens fall to the other side.
+// single precision some 40 of the 9.4 million bytes of 16384 tokens fall to the other side. (Single precision with a
+// check for numbers that are near such a place, and double for rows that have one, took 20 us for 16384 tokens, as this
+// does: the band's frequencies, the reductions and the check itself remain.)
 // The e of one number alone: of a part, the largest of its numbers'.
 __device__ __forceinline__ int exponent_of(double x) {
   const uint64_t u = (uint64_t)__builtin_bit_cast(int64_t, x) & ~((uint64_t)1 << 63);
@@ -128,24 +131,22 @@ __global__ __launch_bounds__(64 * kWaves) void append_q8_kernel(AppendQ8Args arg
   }
 }
 
-// Rows back as numbers: a workgroup looks up the places of `rows` of them, then each thread takes 8 numbers of a row at a
+// Rows back as numbers: a workgroup looks up the places of `rows` of them, then each thread takes 16 numbers of a row at a
 // time, several on their way at once.
 constexpr int kReadThreads = 256, kReadRows = 32;
 template <typename T>
 __global__ __launch_bounds__(kReadThreads) void read_q8_kernel(ReadQ8Args a, int rows) {
   __shared__ const uint8_t* s_src[kReadRows];
-  __shared__ int s_exp[kReadRows];
-  __shared__ float s_fill[kReadRows];
+  __shared__ float s_power[kReadRows][2];
   const int64_t t0 = (int64_t)blockIdx.x * rows;
   const int have = (int)min((int64_t)rows, a.T - t0), W = a.d_c + a.d_rope;
   if ((int)threadIdx.x < have) {
     const int64_t t = t0 + threadIdx.x;
     const int pos = a.position[t];
     const uint8_t* src = nullptr;
-    float fill = 0.f;
-    int exps = 0;
+    int exps = kScaleBias | kScaleBias << 8;
     if (pos >= 0) {
-      fill = NAN;
+      exps = 255 | 255 << 8;
       const int64_t r = a.row_request ? a.row_request[t] : t;
       if ((uint64_t)r < (uint64_t)a.R && pos < a.width * a.page) {
         const int pg = (int)((uint64_t)(uint32_t)pos * a.page_magic >> a.page_shift), off = pos - pg * a.page;
@@ -157,34 +158,36 @@ __global__ __launch_bounds__(kReadThreads) void read_q8_kernel(ReadQ8Args a, int
       }
     }
     s_src[threadIdx.x] = src;
-    s_exp[threadIdx.x] = exps;
-    s_fill[threadIdx.x] = fill;
+    // (byte 0: 2^-127; 255: NaN)
+    for (int k = 0; k < 2; ++k) {
+      const int b = exps >> 8 * k & 255;
+      s_power[threadIdx.x][k] = __builtin_bit_cast(float, b << 23 | ((b + 1 & 254) == 0 ? 1 << 22 : 0));
+    }
   }
   __syncthreads();
-  const int nch = W / 8;
+  const int nch = W / 16;
 #pragma unroll 4
   for (int x = threadIdx.x; x < have * nch; x += kReadThreads) {
-    const int i = x / nch, c = 8 * (x - i * nch);
+    const int i = x / nch, c = 16 * (x - i * nch);
     const uint8_t* src = s_src[i];
-    float y[8];
-    if (src) {
-      const i32x2 b = *reinterpret_cast<const i32x2*>(src + c);
-      const int e = (c < a.d_c ? s_exp[i] & 255 : s_exp[i] >> 8) - kScaleBias;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        typedef float f32x2 __attribute__((ext_vector_type(2)));
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(b[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(b[k], true);
-        y[4 * k] = __builtin_ldexpf(lo[0], e);
-        y[4 * k + 1] = __builtin_ldexpf(lo[1], e);
-        y[4 * k + 2] = __builtin_ldexpf(hi[0], e);
-        y[4 * k + 3] = __builtin_ldexpf(hi[1], e);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = s_fill[i];
-    }
+    i32x4 b = {};  // a row that is not there: 0, times 1 or NaN
+    if (src) b = *reinterpret_cast<const i32x4*>(src + c);
+    const float power = s_power[i][c >= a.d_c];
     T* to = c < a.d_c ? (T*)a.c_kv + (t0 + i) * a.d_c + c : (T*)a.k_pe + (t0 + i) * a.d_rope + (c - a.d_c);
-    store8(to, y);
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+      typedef float f32x2 __attribute__((ext_vector_type(2)));
+      float y[8];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(b[k + u], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(b[k + u], true);
+        y[4 * u] = lo[0] * power;
+        y[4 * u + 1] = lo[1] * power;
+        y[4 * u + 2] = hi[0] * power;
+        y[4 * u + 3] = hi[1] * power;
+      }
+      store8(to + 4 * k, y);
+    }
   }
 }
 

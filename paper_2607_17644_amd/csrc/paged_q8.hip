@@ -2,13 +2,17 @@
 // for the shared key of each position. (paged_attn.hip has the call's other launches.)
 //
 // The products run on fp16 operands, 16x16x32 at a time: an e4m3 number is an fp16 number, and two fp16 parts of a
-// query value hold 22 bits of it (three bf16 parts would hold 24, for half as many products again). With key j's
-// powers 2^c_j and 2^k_j
+// query value, the row scaled to at most 2, hold 22 bits of it or 2^-25 of the row's largest (three bf16 parts would
+// hold 24, for half as many products again). With key j's powers 2^c_j and 2^k_j
 //
-//   z_j = scale (2^c_j A_j + 2^k_j B_j),  A = qa . c8,  B = q_rope . k8,  O += (p_j 2^(c_j + d)) c8_j
+//   z_j = scale 2^e (2^c_j A_j + 2^k_j B_j),  A = qa . c8,  B = q_rope . k8,  O += (p_j 2^(c_j + d)) c8_j
 //
-// so the powers never meet a number of 8 bits: they are added to the exponents of A, B and p.
+// so the powers never meet a number of 8 bits. A lone wave per SIMD issues an instruction in 4 to 5 cycles, and a product
+// takes the matrix unit 16: the scores, two numbers' conversions beside each product, are bound by it, O, with four, by
+// the instructions.
 #define LAGA_LDS_DMA_ASM 1
+#include <type_traits>
+
 #include "paged_dev.hpp"
 
 namespace laga {
@@ -19,65 +23,103 @@ typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
 typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
 typedef __attribute__((__vector_size__(2 * sizeof(int)))) int i32x2;
 
-__device__ __forceinline__ void mma16(f32x4& acc, const f16x8& a, const f16x8& b) {
+__device__ __forceinline__ void mma(f32x4& acc, const f16x8& a, const f16x8& b) {
   acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, acc, 0, 0, 0);
 }
-// 8 e4m3 numbers in fp16, exactly
-__device__ __forceinline__ f16x8 widen(int lo, int hi) {
-  f16x8 y;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const unsigned x = i < 2 ? lo : hi;
-    const f16x2 v = __builtin_bit_cast(f16x2, i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, true)
-                                                    : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, false));
-    y[2 * i] = v[0];
-    y[2 * i + 1] = v[1];
-  }
-  return y;
+__device__ __forceinline__ void mma(f32x16& acc, const f16x8& a, const f16x8& b) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, acc, 0, 0, 0);
+}
+// e4m3 numbers in fp16, exactly: four of them into elements at .. at + 3, or eight
+__device__ __forceinline__ void widen4(f16x8& y, int at, int x) {
+  const f16x2 lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((unsigned)x, 1.f, false));
+  const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((unsigned)x, 1.f, true));
+  y[at] = lo[0], y[at + 1] = lo[1], y[at + 2] = hi[0], y[at + 3] = hi[1];
 }
 
-// Rows are NK steps of 64 numbers of the latent and one of the band, zeros up to them. Of a workgroup's four waves
-//   HG have 16 heads each, with both parts of their queries and O in registers;
-//   CS = 2 halve the columns of O above d_c = 512, and both form all scores;
-//   KW take a tile of 32 keys each, the next KW tiles after it, and put their sums together at a share's end.
-// So a wave never waits for another's partial scores, and with 16 heads for no other wave at all.
-template <int NK, int HG>
+// A product of the scores' chains. Written out, because the queries are to stay in accumulation registers, which leaves the
+// ordinary ones to O (a rescaled sum would travel from one kind to the other and back); scores_done waits until the
+// last are written. (An operand that a vector instruction wrote may be read two wait states after it.)
+template <bool FIRST, bool ACC>
+__device__ __forceinline__ void score_step(f32x4& s, const f16x8& k, const f16x8& q) {
+  if constexpr (FIRST && ACC) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "a"(q));
+  else if constexpr (FIRST) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "v"(q));
+  else if constexpr (ACC) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "a"(q));
+  else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "v"(q));
+}
+template <bool FIRST>
+__device__ __forceinline__ void score_step(f32x16& s, const f16x8& k, const f16x8& q) {
+  if constexpr (FIRST) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "a"(q));
+  else asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "a"(q));
+}
+__device__ __forceinline__ void scores_done(f32x4 (&a)[2], f32x4 (&b)[2]) {
+  asm volatile("s_nop 15\n\ts_nop 3" : "+v"(a[0]), "+v"(a[1]), "+v"(b[0]), "+v"(b[1]));
+}
+__device__ __forceinline__ void scores_done(f32x16& a, f32x16& b) {
+  asm volatile("s_nop 15\n\ts_nop 7" : "+v"(a), "+v"(b));
+}
+
+// Rows are NK steps of 64 numbers of the latent and one of the band, zeros up to them. A workgroup's four waves:
+// HEADS = 16: KW = 4 tiles of 32 keys are under way at once, one to a wave, in products of 16 x 16; the waves put their
+//   sums together at a share's end, and wait for each other nowhere else. Above d_c = 512, where the queries and O do
+//   not fit in registers, all four share a tile: each forms all of its scores and has a quarter of O's columns.
+// HEADS = 32 or 64: two waves have 32 heads, in products of 32 x 32, for which half as many numbers are widened as for
+//   twice 16 heads. They share both products, each with every second half of the contraction and half of O's
+//   columns, and exchange partial scores through LDS; with 32 heads two such pairs take a tile each.
+// In every form a wave's registers hold its part of the queries, twice, and of O.
+template <int NK, int HEADS>
 struct Q8Cfg {
-  static constexpr int CS = NK > 8 ? 2 : 1;
-  static constexpr int SW = HG * CS;           // waves that share a tile
-  static constexpr int KW = 4 / SW;
-  static constexpr int P = 4 * NK + 4;         // 16-byte chunks of an LDS row; 4 modulo 8, see kTurns
-  static constexpr int NI = kTileKeys * P / 64;  // copies of 64 chunks per tile
-  static constexpr int NJ = (NI + SW - 1) / SW;  // of each wave, at most; NI / SW at least
-  static constexpr int TILE = kTileKeys * P * 16, STAGE = TILE + 256;  // the keys' exponents after their rows
-  static constexpr int kFit = 150 * 1024 / STAGE / KW;
+  static constexpr bool WIDE = HEADS > 16;
+  static constexpr int HG = WIDE ? HEADS / 32 : 1;      // groups of heads
+  static constexpr int CS = WIDE ? 2 : NK > 8 ? 4 : 1;  // waves of a group
+  static constexpr int SW = HG * CS;                    // waves that share a tile
+  static constexpr int KW = 4 / SW;                     // tiles under way at once
+  static constexpr int CH = 4 * NK;            // 16-byte chunks of the latent in an LDS row
+  static constexpr int RPC = 64 / CH;          // rows of a copy of 64 chunks
+  static constexpr int NM = kTileKeys / RPC, NI = NM + 2;  // copies of a tile's latents; with those of its keys
+  static constexpr int NJ = (NI + SW - 1) / SW;            // of each wave, at most; NI / SW at least
+  static constexpr int BAND = kTileKeys * CH * 16, TILE = BAND + kTileKeys * 64;
+  static constexpr int STAGE = TILE + 256;     // the keys' exponents after them
+  static constexpr int kParts = WIDE ? 2 * 4 * 64 * 16 * 4 : 0;  // partial scores of two tiles
+  static constexpr int kFit = (150 * 1024 - kParts) / STAGE / KW;
   static constexpr int NS = kFit < 8 ? kFit : 8;
-  static constexpr int NB = 4 * NK / CS;       // blocks of 16 columns of a wave
-  static constexpr int kRing = KW * NS * STAGE, kSums = KW > 1 ? 4 * NB * 64 * 16 : 0;
-  static constexpr int LDS = kRing > kSums ? kRing : kSums;
-  static_assert(SW * KW == 4 && NS >= 2 && P % 8 == 4);
+  static constexpr int NB = WIDE ? NK : 4 * NK / CS;       // blocks of 32, or 16, columns of a wave
+  static constexpr int kO = 4 * NK / (WIDE ? 1 : CS);      // f32x4 of O in a lane
+  static constexpr int kRing = KW * NS * STAGE, kSums = KW > 1 ? 4 * kO * 64 * 16 : 0;
+  static constexpr int LDS = kRing + kParts > kSums ? kRing + kParts : kSums;
+  static_assert(SW * KW == 4 && NS >= (WIDE ? 3 : 2) && !(WIDE && NK > 8));
 };
 constexpr int kIds = 128;  // page ids of a row that a wave keeps in LDS
 
-// Chunk c of row r is at c ^ f(r), f(r) = entry r / 4 of kTurns: at a pitch of 4 chunks modulo 8 the four rows r % 4 begin a
-// quarter round the banks apart, and f deals the rows of one r % 4 to its four chunks, in both readings: 16 bytes
-// of 16 rows, two neighbouring chunks over the half-waves, and 16 bytes of the 8 rows 4 g .. + 3 and 16 + 4 g .. + 3
-// in each quarter-wave g.
-constexpr unsigned kTurns = 0u << 0 | 2u << 2 | 3u << 4 | 1u << 6 | 1u << 8 | 3u << 10 | 2u << 12 | 0u << 14;
-__device__ __forceinline__ int turn_of(int row) { return kTurns >> (row >> 2) * 2 & 3; }
+// Chunk c of a latent's row r is at c ^ turn(r), of a key's at c ^ band_turn(r). The banks repeat every 16 chunks. In 16 x 16
+// products a pass of ds_read_b128 has rows {0 .. 3, 12 .. 15} at a chunk c and {4 .. 11} at c ^ 1, and a pass of the transposing
+// 8-byte reads the 16 bytes at c of rows {0 .. 7, 16 .. 23} or the others; in 32 x 32 ones {0 .. 3, 12 .. 15, 20 .. 27} or the
+// others at c, and {0 .. 3, 8 .. 11}, or those moved by 4 or 16, at c and c ^ 1. The turns keep each of these apart. They
+// are linear in the bits of r, so that the rows of a copy and its number turn separately.
+template <int NK, bool WIDE>
+__host__ __device__ constexpr int turn(int r) {
+  if (WIDE) return NK > 2 ? (r & 3) << 1 | (r >> 2 & 1) | (r & 8) : (r & 2) | (r >> 2 & 1) | (r & 8) >> 1;
+  return NK > 2 ? (r & 15) ^ (r & 16) >> 1 : (r >> 1 & 7) ^ (r & 16) >> 2;
+}
+template <bool WIDE>
+__host__ __device__ constexpr int band_turn(int r) {
+  return WIDE ? r >> 3 & 3 : (r & 4) >> 1 ^ ((r & 8) >> 3) * 3;
+}
 
-// A probability's fp16 reference: the running maximum is raised only where a score passes it by kRise, and p
-// goes into the product as p 2^(c_j + d + kLift), d such that no p 2^(c_j + d) passes 2^kRise: 2^14 at most, and 11 bits
-// down to 2^-28 of that.
+// A probability's reference m, a whole number, is raised only where a score passes it by kRise, and p goes into the
+// product as p 2^(c_j + d + kLift), d such that no p 2^(c_j + d) passes 2^kRise: 2^14 at most, with 11 bits down to 2^-28 of
+// that.
 constexpr float kRise = 8.f;
 constexpr int kLift = 6;
 
-__device__ __forceinline__ float quad_max(float x) {  // over the four lanes of a head
-  x = fmaxf(x, __shfl_xor(x, 16));
+// over the lanes of a head: four, or two
+template <bool WIDE>
+__device__ __forceinline__ float head_max(float x) {
+  if (!WIDE) x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
 }
-__device__ __forceinline__ float quad_sum(float x) {
-  x += __shfl_xor(x, 16);
+template <bool WIDE>
+__device__ __forceinline__ float head_sum(float x) {
+  if (!WIDE) x += __shfl_xor(x, 16);
   return x + __shfl_xor(x, 32);
 }
 // 2 bytes per lane to LDS, 4 bytes apart
@@ -85,15 +127,24 @@ __device__ __forceinline__ void copy_short(const void* g, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ushort %0, off" ::"v"(g), "s"(to) : "memory", "m0");
 }
 
-// The share of worker w, for heads h0 .. h0 + heads (at most 16 HG). FINE: p in two parts.
-template <int NK, int HG, bool FINE>
-__device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* smem, int32_t (*s_ids)[kIds], int (*s_bad)[8],
-                                          float (*s_ml)[2][16], int w, int h0, int heads, int per, int total) {
-  using C = Q8Cfg<NK, HG>;
-  constexpr int CS = C::CS, SW = C::SW, KW = C::KW, P = C::P, NI = C::NI, NJ = C::NJ, NS = C::NS, NB = C::NB;
-  const int l = threadIdx.x & 63, n = l & 15, g = l >> 4;
+template <int N> struct Count { static constexpr int n = N; };
+struct __attribute__((aligned(16))) Q8Lds {
+  float powers[4][64];  // of a tile's keys, 2^c and then 2^k, for each wave
+  int32_t ids[4][kIds];
+  int bad[4][8];        // keys of a stage's tile that have no page
+  float ml[4][2][32];
+};
+// The share of worker w, for heads h0 .. h0 + heads (HEADS at most). FINE: p in two parts.
+template <int NK, int HEADS, bool FINE>
+__device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* smem, Q8Lds& lds, int w, int h0, int heads, int per,
+                                          int total) {
+  using C = Q8Cfg<NK, HEADS>;
+  constexpr bool WIDE = C::WIDE;
+  constexpr int CS = C::CS, SW = C::SW, KW = C::KW, CH = C::CH, NI = C::NI, NJ = C::NJ, NS = C::NS, NB = C::NB;
+  constexpr int GH = WIDE ? 32 : 16;  // heads of a group
+  const int l = threadIdx.x & 63, n = l % GH, g = l / GH;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kw = wave / SW, sr = wave % SW, hg = sr / CS, cs = sr % CS;
+  const int kw = wave / SW, sr = wave % SW, hg = sr % C::HG, cs = sr / C::HG;
   const int W = a.d_c + a.d_rope;
   const int64_t start = (int64_t)w * per;
   if (start >= total) return;
@@ -101,27 +152,37 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
   Share share = first_share(a, w);
   if (share.first >= end) return;  // (units of no tile)
   const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)smem + kw * NS * C::STAGE;
-  int32_t* ids = s_ids[wave];
+  int32_t* ids = lds.ids[wave];
 
-  // of a tile at LDS address x: rows n and 16 + n of K, from chunk g on; rows key(g, (l & 15) / 2) of C^T, chunk i % 4
-  uint32_t at_k[2], at_v[4];
+  // Of a tile at LDS address x (a multiple of 256), with the row's turn in at_k, at_b and at_v:
+  //   16 heads: step i of row 16 b + n of the latents is at ((x + at_k) ^ 64 (i + STEPS / 2 b modulo STEPS)) + 64 (the rest of i) + 16 b
+  //     rows, of the keys at x + at_b + 16 b rows; chunk i of this wave's columns in the transposing reads of rows 4 g .. and
+  //     16 + 4 g .. at ((x + at_v) ^ 16 (i modulo TURNS)) + 16 (the rest of i)
+  //   32: step i of this wave's half of row n at ((x + at_k) ^ 32 i), of the keys at x + at_b; chunks 2 i and 2 i + 1 of this
+  //     wave's columns in those of rows 16 k + 4 g .. and 16 k + 8 + 4 g .. at ((x + at_v) ^ 32 i) + 16 k rows
+  constexpr int TURNS = NK > 2 ? 16 : 8, STEPS = TURNS / 4;
+  constexpr bool BAND_ACC = NK <= 8;  // (the latent's queries alone fill the accumulation registers above)
+  // Of this wave's jj-th copy, of RPC latents' rows: this lane's row is at_src + jj SW RPC, its chunk at_copy with the turn of
+  // jj SW RPC; of a copy of 16 rows of keys at_key_src and at_band.
+  uint32_t at_k, at_b, at_v, at_copy, at_band;
+  int at_src, at_key_src;
   {
-    const int q = l & 15, vr = 4 * g + (q >> 1 & 3) + 16 * (q >> 3);
-#pragma unroll
-    for (int b = 0; b < 2; ++b) at_k[b] = (16 * b + n) * P * 16 + ((g ^ turn_of(16 * b + n)) * 16);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) at_v[i] = vr * P * 16 + ((i ^ turn_of(vr)) * 16) + 8 * (q & 1) + cs * NB * 16;
-  }
-  // copy j's lane: its row of the tile, and where in a cached row its chunk is
-  constexpr uint32_t kNoPlace = ~0u;
-  int row_of[NJ];
-  uint32_t place[NJ];
-#pragma unroll
-  for (int jj = 0; jj < NJ; ++jj) {
-    const int p = min(sr + SW * jj, NI - 1) * 64 + l, row = p / P, c = (p - row * P) ^ turn_of(row);
-    row_of[jj] = row;
-    place[jj] = c < 4 * NK ? (16 * c < a.d_c ? 16 * c : kNoPlace)
-                           : (16 * (c - 4 * NK) < a.d_rope ? a.d_c + 16 * (c - 4 * NK) : kNoPlace);
+    const int q = l & 15;
+    if constexpr (WIDE) {
+      const int vr = 4 * g + (q >> 1 & 3) + 8 * (q >> 3), first = 2 * NK * cs, turned = first % TURNS, rest = first - turned;
+      at_k = n * CH * 16 + ((turned + g ^ turn<NK, WIDE>(n)) + rest) * 16;
+      at_b = C::BAND + n * 64 + ((2 * cs + g ^ band_turn<WIDE>(n)) * 16);
+      at_v = vr * CH * 16 + ((turned + (l >> 4 & 1) ^ turn<NK, WIDE>(vr)) + rest) * 16 + 8 * (q & 1);
+    } else {
+      const int vr = 4 * g + (q >> 1 & 3) + 16 * (q >> 3);
+      at_k = n * CH * 16 + ((g ^ turn<NK, WIDE>(n)) * 16);
+      at_b = C::BAND + n * 64 + ((g ^ band_turn<WIDE>(n)) * 16);
+      at_v = vr * CH * 16 + (turn<NK, WIDE>(vr) * 16) + 8 * (q & 1) + cs * NB * 16;
+    }
+    at_src = sr * C::RPC + l / CH;
+    at_copy = (l % CH ^ turn<NK, WIDE>(at_src)) * 16;
+    at_key_src = (sr & 1) * 16 + (l >> 2);
+    at_band = a.d_c + min(((l & 3) ^ band_turn<WIDE>(at_key_src)) * 16, a.d_rope - 16);
   }
 
   for (int at = max((int)start, share.first);;) {
@@ -131,46 +192,18 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
     const int visible = min((int64_t)share.visible, (int64_t)it1 * kTileKeys);  // to the end of this share
     const int32_t* pages = a.table + (int64_t)share.request * a.width;
 
-    // the queries of head n: of step i and half u elements 64 i + 16 g + 8 u .., scaled to 2^9 .. 2^10 at most
-    f16x8 qh[NK + 1][2], ql[NK + 1][2];
-    int e_c, e_k;
-    {
-      const int64_t th = (int64_t)t * a.H + h0 + min(16 * hg + n, heads - 1);
-      const int blocks = qa_blocks(a.d_c);
-      const float* tops = a.qa_max + th * blocks;
-      float top = 0.f;
-      for (int i = 0; i + 1 < blocks; ++i) top = fmaxf(top, tops[i]);
-      auto power = [](float x) { return x > 0.f ? max(__builtin_amdgcn_frexp_expf(x), -126) - 10 : 0; };
-      e_c = power(top);
-      e_k = power(tops[blocks - 1]);
-      const float* q = (const float*)a.qa + th * W;
-#pragma unroll
-      for (int i = 0; i <= NK; ++i)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int c = (i < NK ? 64 * i : 0) + 16 * g + 8 * u;
-          const bool there = c < (i < NK ? a.d_c : a.d_rope);
-          const float* from = q + (i < NK ? 0 : a.d_c) + (there ? c : 0);
-          const f32x4 x0 = *reinterpret_cast<const f32x4*>(from), x1 = *reinterpret_cast<const f32x4*>(from + 4);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float x = there ? __builtin_ldexpf(e < 4 ? x0[e & 3] : x1[e & 3], i < NK ? -e_c : -e_k) : 0.f;
-            const _Float16 hi = (_Float16)x;
-            qh[i][u][e] = hi;
-            ql[i][u][e] = (_Float16)(x - (float)hi);
-          }
-        }
-    }
-    f32x4 oacc[NB];
-#pragma unroll
-    for (int i = 0; i < NB; ++i) oacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, lsum = 0.f;  // m a whole number
-    int d = 0;                        // O has p 2^(c_j + d + kLift)
+    float m = -INFINITY, lsum = 0.f;
+    float rise = -INFINITY;  // kRise, once there is a reference
+    int d = 0;
 
     int win = 0, win_end = 0;  // first page of the window, and the first key past it
     auto page_of = [&](int key) { return (int)((uint64_t)(uint32_t)key * a.page_magic >> a.page_shift); };
-    // The copies of tile `it` into stage st. A key past the share's end, or without a page (bad), is copied from zeros.
-    auto fetch = [&](int it, int st) {
+    // The copies of a tile. A key past the share's end, or without a page (bad), is copied from zeros. look: the page of
+    // key l % 32; ready: where the copies come from and go; copy: the jj-th of this wave's, and with the first the keys'
+    // exponents. (Chunks past a row's end repeat its last one: they meet zeros of the queries, and columns that are not
+    // stored.)
+    int look_id, look_pg;
+    auto look = [&](int it) {
       const int k0 = it * kTileKeys;
       if (min(k0 + kTileKeys, visible) > win_end) {
         win = page_of(k0);
@@ -178,206 +211,470 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
         const int have = page_of(visible - 1) + 1;
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int i = l; i < kIds; i += 64) ids[i] = win + i < have ? pages[win + i] : -1;
+        for (int i = fresh_lane(); i < kIds; i += 64) ids[i] = win + i < have ? pages[win + i] : -1;
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
       }
-      const int key = k0 + (l & 31);
-      const bool live = key < visible;
-      const int pg = live ? page_of(key) : win, id = ids[pg - win];
-      const bool ok = live && (unsigned)id < (unsigned)a.n_pages;
-      const int off = key - pg * a.page;
-      const char* src = ok ? (const char*)a.cache + (int64_t)id * a.page_stride + (int64_t)off * W : (const char*)kZeroRow;
-      const char* exps = ok ? (const char*)a.scales + 2 * ((int64_t)id * a.page + off) : (const char*)kZeroRow;
+      const int key = k0 + (fresh_lane() & 31);
+      look_pg = key < visible ? page_of(key) : win;
+      look_id = ids[look_pg - win];
+    };
+    enum { kNone, kFlat, kRows };
+    int mode = kNone, src_lo = 0, src_hi = 0;
+    const char *base = nullptr, *exps_base = nullptr;  // of a tile in one page, whose rows follow each other
+    uint32_t to = 0;
+    auto ready = [&](int it, int stage) {
+      const int k0 = it * kTileKeys, l = fresh_lane(), key = k0 + (l & 31);
+      const bool live = key < visible, ok = live && (unsigned)look_id < (unsigned)a.n_pages;
+      const int off = key - look_pg * a.page;
       const uint32_t bad = (uint32_t)__ballot(live && !ok);
-      if (l == 0) s_bad[wave][st] = (int)bad;
-      const uint32_t tile = ring + st * C::STAGE;
-      const int lo = (int)(uint32_t)(uintptr_t)src, hi = (int)(uint32_t)((uintptr_t)src >> 32);
-#pragma unroll
-      for (int jj = 0; jj < NJ; ++jj) {
-        if (NI % SW == 0 || sr + SW * jj < NI) {
-          const uintptr_t base = (uintptr_t)(uint32_t)__shfl(lo, row_of[jj]) | ((uintptr_t)(uint32_t)__shfl(hi, row_of[jj]) << 32);
-          g2lds16(place[jj] == kNoPlace ? (const char*)kZeroRow : (const char*)base + place[jj],
-                  (void*)(uintptr_t)(tile + (sr + SW * jj) * 1024));
-        }
+      if (l == 0) lds.bad[wave][stage] = (int)bad;
+      to = ring + stage * C::STAGE;
+      const int id0 = uniform(look_id), off0 = uniform(off);
+      if (k0 + kTileKeys <= visible && off0 + kTileKeys <= a.page && !bad) {
+        mode = kFlat;
+        base = (const char*)a.cache + (int64_t)id0 * a.page_stride + (int64_t)off0 * W;
+        exps_base = (const char*)a.scales + 2 * ((int64_t)id0 * a.page + off0);
+      } else {
+        mode = kRows;
+        const uintptr_t src = ok ? (uintptr_t)a.cache + (int64_t)look_id * a.page_stride + (int64_t)off * W : (uintptr_t)kZeroRow;
+        src_lo = (int)(uint32_t)src;
+        src_hi = (int)(uint32_t)(src >> 32);
+        if (sr == 0)
+          copy_short(ok ? (const char*)a.scales + 2 * ((int64_t)look_id * a.page + off) : (const char*)kZeroRow, uniform((int)(to + C::TILE)));
       }
-      if (sr == 0) copy_short(exps, uniform((int)(tile + C::TILE)));
+    };
+    auto copy = [&](int jj) {
+      constexpr int MAIN = C::NM / SW;
+      static_assert(C::NM % SW == 0);
+      if (mode == kNone || (SW == 4 && jj == MAIN && sr > 1)) return;
+      const bool latent = jj < MAIN;
+      const int r0 = latent ? jj * SW * C::RPC : SW == 1 ? (jj - MAIN) * 16 : 0, r = latent ? at_src : at_key_src;
+      const uint32_t off = latent ? min(at_copy ^ (turn<NK, WIDE>(r0) * 16), (uint32_t)a.d_c - 16) : at_band;
+      const uint32_t dst = to + (sr + SW * jj) * 1024;
+      if (mode == kFlat) {
+        if (jj == 0 && sr == 0) copy_short(exps_base + 2 * (l & 31), uniform((int)(to + C::TILE)));
+        g2lds16_so(base + r0 * W, __umul24(r, W) + off, (void*)(uintptr_t)dst);
+      } else {
+        const uintptr_t row = (uintptr_t)(uint32_t)__shfl(src_lo, r0 + r) | ((uintptr_t)(uint32_t)__shfl(src_hi, r0 + r) << 32);
+        g2lds16((const char*)row + off, (void*)(uintptr_t)dst);
+      }
     };
 
     lds_barrier();  // the tiles, sums and page ids before are read
-    const int steps = (it1 - it0 + KW - 1) / KW;
+    const int steps = SW == 1 ? (it1 - it0 - kw + KW - 1) / KW : (it1 - it0 + KW - 1) / KW;
+    // (with more than one wave to a tile, a last one perhaps past the share's end: rows of zeros without weight)
     auto tile_of = [&](int s) { return it0 + KW * s + kw; };
-    constexpr int kAhead = SW == 1 ? NS : NS - 1;  // tiles on their way at a step's begin
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (tile_of(i) < it1) fetch(tile_of(i), i);
-    int st = 0;
-    for (int s = 0; s < steps; ++s) {
-      const int it = tile_of(s);
-      // tile `it` has landed: only the tiles after it may be on their way
-      if (tile_of(s + kAhead - 1) < it1) wait_vmem_le<(kAhead - 1) * (NI / SW + (SW == 1))>();
+    // Tile s has landed: only the AFTER tiles that were asked for after it may be on their way.
+    auto landed = [&](int s, auto after) {
+      constexpr int AFTER = decltype(after)::n;
+      if (s + AFTER < steps) wait_vmem_le<AFTER * (NI / SW + (SW == 1))>();
       else wait_vmem();
-      asm volatile("" ::: "memory");  // (nothing is read before)
-      if constexpr (SW > 1) {
-        lds_barrier();  // ... every wave's copies, and the stage before is read
-        if (tile_of(s + kAhead) < it1) fetch(tile_of(s + kAhead), st == 0 ? NS - 1 : st - 1);
+      if constexpr (SW > 1) lds_barrier();  // every wave's copies (and partial scores)
+      else asm volatile("" ::: "memory");   // (nothing is read before)
+    };
+#pragma unroll 1
+    for (int i = 0; i < min(NS, steps); ++i) {
+      look(tile_of(i));
+      ready(tile_of(i), i);
+#pragma unroll
+      for (int jj = 0; jj < NJ; ++jj) copy(jj);
+    }
+    mode = kNone;
+    // the queries of head n, scaled by 2^-e to 1 .. 2 at most: of step i and half u elements 64 i + 16 g + 8 u .., or of this
+    // wave's half 32 i + 16 g + 8 u ..
+    f16x8 qh[NK + 1][2], ql[NK + 1][2];
+    float mult;  // of a score in base 2
+    {
+      const int64_t th = (int64_t)t * a.H + h0 + min(GH * hg + n, heads - 1);
+      const int blocks = qa_blocks(a.d_c);
+      const float* tops = a.qa_max + th * blocks;
+      const f32x4* q = (const f32x4*)a.qa + (int64_t)t * (W / 4) * a.H + (th - (int64_t)t * a.H);
+      auto at = [&](int i, int u) { return (WIDE ? 32 * (i < NK ? NK * cs + i : cs) : i < NK ? 64 * i : 0) + 16 * g + 8 * u; };
+      auto there = [&](int i, int u) { return at(i, u) < (i < NK ? a.d_c : a.d_rope); };
+      float top = 0.f;
+      for (int i = 0; i < blocks; ++i) top = fmaxf(top, tops[i]);
+      const int e = top > 0.f ? max(__builtin_amdgcn_frexp_expf(top) - 1, -126) : 0;
+      const float down = __builtin_ldexpf(1.f, -e);
+      mult = __builtin_ldexpf(a.scale_log2, e);
+      constexpr int TURN = 9;  // steps whose numbers are on their way at once
+#pragma unroll
+      for (int i0 = 0; i0 <= NK; i0 += TURN) {
+        f32x4 x[TURN][2][2];
+#pragma unroll
+        for (int i = i0; i < min(i0 + TURN, NK + 1); ++i)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const f32x4* from = q + (((i < NK ? 0 : a.d_c) + (there(i, u) ? at(i, u) : 0)) >> 2) * a.H;
+            x[i - i0][u][0] = from[0];
+            x[i - i0][u][1] = from[a.H];
+          }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = i0; i < min(i0 + TURN, NK + 1); ++i)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            typedef float f32x8 __attribute__((ext_vector_type(8)));
+            const float f = there(i, u) ? down : 0.f;
+            f32x8 y, rest;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] = x[i - i0][u][k >> 2][k & 3] * f;
+            qh[i][u] = __builtin_convertvector(y, f16x8);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) rest[k] = y[k] - (float)qh[i][u][k];
+            ql[i][u] = __builtin_convertvector(rest, f16x8);
+            if (i < NK || BAND_ACC) asm volatile("" : "+a"(qh[i][u]), "+a"(ql[i][u]));  // (whole)
+            else asm volatile("" : "+v"(qh[i][u]), "+v"(ql[i][u]));
+            __builtin_amdgcn_sched_barrier(0);
+          }
       }
-      if (it < it1) {
-        const uint32_t tile = ring + st * C::STAGE;
-        f32x4 sc[2], sk[2];
+    }
+    typedef std::conditional_t<WIDE, f32x16, f32x4> acc_t;
+    acc_t oacc[NB];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) sc[b] = sk[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NB; ++i) oacc[i] = acc_t{};
+    int st = 0;
+    uint32_t tile = ring;
+    constexpr int NZ = WIDE ? 16 : 8;  // scores of a lane
+    f32x4 fc[NZ / 4];                  // 2^c of their keys
+    float z[NZ], p[NZ], x[NZ];
+    // this lane's r-th score is of key
+    auto key_of = [&](int r) { return (WIDE ? 8 : 16) * (r >> 2) + 4 * g + (r & 3); };
+    // Scores of tile s into p and what goes into the product, x, under the reference, which is raised where need be.
+    auto weigh = [&](int s, int bad) {
+      const int lim = visible - tile_of(s) * kTileKeys;
+      if (lim < kTileKeys || bad) {
 #pragma unroll
-        for (int i = 0; i <= NK; ++i)
+        for (int r = 0; r < NZ; ++r) z[r] = key_of(r) < lim ? (bad >> key_of(r) & 1 ? NAN : z[r]) : -INFINITY;
+      }
+      float most_t = -INFINITY, most_x = 0.f;
+      auto under = [&](float m_use, float f) {
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const i32x4 x = *(__attribute__((address_space(3))) const i32x4*)(uintptr_t)(tile + at_k[b] + 64 * i);
-            f32x4& acc = i < NK ? sc[b] : sk[b];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const f16x8 k = widen(x[2 * u], x[2 * u + 1]);
-              mma16(acc, k, qh[i][u]);
-              mma16(acc, k, ql[i][u]);
-            }
-          }
-        // lane: head n, keys 16 b + 4 g + r
-        int ec[2][4];
-        float z[2][4];
-        const int lim = visible - it * kTileKeys - 4 * g;
-        const int bad = uniform(s_bad[wave][st]);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const i32x4 x = *(__attribute__((address_space(3))) const i32x4*)(uintptr_t)(tile + C::TILE + 64 * b + 16 * g);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            ec[b][r] = (x[r] & 255) - kScaleBias;
-            const int ek = (x[r] >> 8 & 255) - kScaleBias;
-            z[b][r] = a.scale_log2 * (__builtin_ldexpf(sc[b][r], ec[b][r] + e_c) + __builtin_ldexpf(sk[b][r], ek + e_k));
-          }
+        for (int r = 0; r < NZ; ++r) {
+          const float t = __builtin_fmaf(z[r], mult, -m_use);
+          most_t = fmaxf(most_t, t);
+          p[r] = fast_exp2(t);
+          x[r] = p[r] * f * fc[r >> 2][r & 3];
+          most_x = fmaxf(most_x, x[r]);
         }
-        if (lim + 4 * g < kTileKeys || bad) {
+      };
+      under(m == -INFINITY ? 0.f : m, __builtin_ldexpf(1.f, d + kLift));
+      if (__ballot(most_t > rise || most_x > 0x1p14f)) {
+        // m to the whole number at or above every score, and d so that the largest p 2^(c_j + d) is 1 at most
+        float top = -INFINITY;
 #pragma unroll
-          for (int b = 0; b < 2; ++b)
+        for (int r = 0; r < NZ; ++r) top = fmaxf(top, z[r] * mult);
+        const float m_new = fmaxf(m, ceilf(head_max<WIDE>(top))), m_use = m_new == -INFINITY ? 0.f : m_new;
+        float lift = -1e5f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int k = 16 * b + r;
-              z[b][r] = k < lim ? (bad >> (k + 4 * g) & 1 ? NAN : z[b][r]) : -INFINITY;
-            }
+        for (int r = 0; r < NZ; ++r)
+          lift = fmaxf(lift, __builtin_fmaf(z[r], mult, -m_use) + (float)__builtin_amdgcn_frexp_expf(fc[r >> 2][r & 3]));
+        int ref = (int)ceilf(fminf(head_max<WIDE>(lift), 1e5f));
+        const int fell = m == -INFINITY ? -100000 : (int)fmaxf(m - m_use, -1e5f);
+        if (m != -INFINITY) {
+          ref = max(ref, fell - d);
+          lsum = __builtin_ldexpf(lsum, fell);
         }
-        float m_use = m == -INFINITY ? 0.f : m, most = m == -INFINITY ? INFINITY : -INFINITY;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float over = z[b][r] - m_use;
-            most = fmaxf(most, fmaxf(over, over + (float)(ec[b][r] + d)));
-          }
-        if (__ballot(most > kRise)) {
-          // m to the whole number at or above every score, and d so that the largest p 2^(c_j + d) is at most 1
-          float top = -INFINITY;
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, z[b][r]);
-          const float m_new = fmaxf(m, ceilf(quad_max(top)));
-          m_use = m_new == -INFINITY ? 0.f : m_new;
-          float lift = -1e5f;
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) lift = fmaxf(lift, z[b][r] - m_use + (float)ec[b][r]);
-          int ref = (int)ceilf(fminf(quad_max(lift), 1e5f));
-          const float fall = m == -INFINITY ? -INFINITY : m - m_use;  // <= 0
-          const int fell = (int)fmaxf(fall, -1e5f);
-          if (m != -INFINITY) ref = max(ref, fell - d);
-          const float f = m == -INFINITY ? 0.f : __builtin_ldexpf(1.f, fell - ref - d);
-          if (m != -INFINITY) lsum = __builtin_ldexpf(lsum, fell);
-#pragma unroll
-          for (int i = 0; i < NB; ++i) oacc[i] *= f;
-          d = -ref;
-          m = m_new;
-        }
-        f16x8 ph, pl;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float p = fast_exp2(z[b][r] - m_use);
-            lsum += p;
-            const float x = __builtin_ldexpf(p, ec[b][r] + d + kLift);
-            ph[4 * b + r] = (_Float16)x;
-            if constexpr (FINE) pl[4 * b + r] = (_Float16)(x - (float)ph[4 * b + r]);
-          }
+        ref = min(max(ref, -120), 129);
+        const float f = m == -INFINITY ? 0.f : __builtin_ldexpf(1.f, fell - ref - d);
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-          const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-              (__attribute__((address_space(3))) i32x2*)(uintptr_t)(tile + at_v[i % 4] + 64 * (i / 4)));
-          const f16x8 v = widen(x[0], x[1]);
-          mma16(oacc[i], v, ph);
-          if constexpr (FINE) mma16(oacc[i], v, pl);
+          oacc[i] *= f;
+          if (WIDE || i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        d = -ref;
+        m = m_new;
+        rise = m == -INFINITY ? -INFINITY : kRise;
+        under(m_use, __builtin_ldexpf(1.f, d + kLift));
+      }
+#pragma unroll
+      for (int r = 0; r < NZ; r += 4) lsum += (p[r] + p[r + 1]) + (p[r + 2] + p[r + 3]);
+    };
+    // eight of them as an operand, and what its rounding left
+    auto operand = [&](int first, f16x8& hi, f16x8& lo) {
+      typedef float f32x8 __attribute__((ext_vector_type(8)));
+      f32x8 y;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = x[first + e];
+      hi = __builtin_convertvector(y, f16x8);
+      if constexpr (FINE) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] -= (float)hi[e];
+        lo = __builtin_convertvector(y, f16x8);
+      }
+    };
+    // The keys' powers (byte 0: 2^-127; 255: NaN), by way of LDS to the lanes that need them
+    auto give_powers = [&](int exps) {
+      const int b = l < 32 ? exps & 255 : exps >> 8 & 255;
+      lds.powers[wave][l] = __builtin_bit_cast(float, b << 23 | ((b + 1 & 254) == 0 ? 1 << 22 : 0));
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    };
+    auto powers = [&](int of, int r) { return *reinterpret_cast<const f32x4*>(&lds.powers[wave][32 * of + key_of(r)]); };
+    auto raw_at = [&](uint32_t at) { return *(__attribute__((address_space(3))) const i32x4*)(uintptr_t)at; };
+    auto columns_at = [&](uint32_t at) { return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(uintptr_t)at); };
+    constexpr int PER = (NJ + NK) / (NK + 1);  // copies beside a step
+    static_assert(PER == 1 || PER == 2);
+    int exps, bads;
+    auto tile_first = [&]() {
+      exps = *(__attribute__((address_space(3))) const int*)(uintptr_t)(tile + C::TILE + 4 * (fresh_lane() & 31));
+      bads = lds.bad[wave][st];
+    };
+    // the copies of step s are those of the tile that takes the place of the one before its own
+    auto ask = [&](int s) {
+      if (s > 0 && s - 1 + NS < steps) ready(tile_of(s - 1 + NS), st == 0 ? NS - 1 : st - 1);
+      else mode = kNone;
+    };
+
+    if constexpr (!WIDE) {
+      auto k_read = [&](int i, int b) {
+        return raw_at(i < NK ? ((tile + at_k) ^ (64 * ((i + b * STEPS / 2) % STEPS))) + 64 * (i / STEPS * STEPS) + 16 * b * CH * 16
+                             : tile + at_b + 16 * b * 64);
+      };
+      auto v_read = [&](int i) { return columns_at(((tile + at_v) ^ (16 * (i % TURNS))) + 16 * (i / TURNS * TURNS)); };
+      constexpr int RA = NK > 2 ? 3 : 2;  // steps whose numbers are on their way
+      i32x4 raw[RA][2];
+      auto k_first = [&]() {
+#pragma unroll
+        for (int i = 0; i < RA; ++i)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) raw[i][b] = k_read(i, b);
+        tile_first();
+      };
+      if (steps > 0) {
+        landed(0, Count<NS - 1>{});
+        k_first();
+      }
+      for (int s = 0; s < steps; ++s) {
+        // Scores, step by step: beside the eight products of one step the next one's numbers are widened, later ones'
+        // read, and now and then a copy is asked for.
+        const int bad = uniform(bads);
+        ask(s);
+        f32x4 sc[2], sk[2], fk[2];
+        f16x8 k[2][2][2];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) widen4(k[0][j >> 2][j >> 1 & 1], 4 * (j & 1), raw[0][j >> 2][j & 3]);
+        asm volatile("s_nop 1" : "+v"(k[0][0][0]), "+v"(k[0][1][0]), "+v"(k[0][0][1]), "+v"(k[0][1][1]));
+#pragma unroll
+        for (int i = 0; i <= NK; ++i) {
+          f32x4(&acc)[2] = i < NK ? sc : sk;
+          if (i + RA <= NK)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) raw[i % RA][b] = k_read(i + RA, b);
+          if (i == 0) {
+            give_powers(exps);
+          } else if (i == 1) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) fc[b] = powers(0, 4 * b), fk[b] = powers(1, 4 * b);
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int b = j & 1, u = j >> 2;
+            const f16x8& q = j >> 1 & 1 ? ql[i][u] : qh[i][u];
+            if (j < 2 && i == NK) score_step<true, BAND_ACC>(acc[b], k[i & 1][b][u], q);
+            else if (i == NK) score_step<false, BAND_ACC>(acc[b], k[i & 1][b][u], q);
+            else if (j < 2 && i == 0) score_step<true, true>(acc[b], k[i & 1][b][u], q);
+            else score_step<false, true>(acc[b], k[i & 1][b][u], q);
+            if (i < NK) {
+              f16x8& y = k[i + 1 & 1][j >> 2][j >> 1 & 1];
+              widen4(y, 4 * (j & 1), raw[(i + 1) % RA][j >> 2][j & 3]);
+              if (j & 1) asm volatile("" : "+v"(y));  // (here, not where it is used)
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (j % (8 / PER) == 8 / PER - 1 && PER * i + j / (8 / PER) < NJ) copy(PER * i + j / (8 / PER));
+          }
+        }
+        // O's first numbers, on their way beside the softmax
+        constexpr int AHEAD = 4;
+        i32x2 vr[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) vr[i] = v_read(i);
+        scores_done(sc, sk);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) z[r] = __builtin_fmaf(sk[r >> 2][r & 3], fk[r >> 2][r & 3], sc[r >> 2][r & 3] * fc[r >> 2][r & 3]);
+        weigh(s, bad);
+        f16x8 ph, pl, v[2];
+        operand(0, ph, pl);
+        // O's products likewise, the numbers read AHEAD of them; when the tile's last are, the next tile's first
+        widen4(v[0], 0, vr[0][0]);
+        widen4(v[0], 4, vr[0][1]);
+        auto o_step = [&](int i) {
+          if (i + AHEAD < NB) vr[i % AHEAD] = v_read(i + AHEAD);
+          mma(oacc[i], v[i & 1], ph);
+          if (i + 1 < NB) {
+            widen4(v[i + 1 & 1], 0, vr[(i + 1) % AHEAD][0]);
+            widen4(v[i + 1 & 1], 4, vr[(i + 1) % AHEAD][1]);
+          }
+          if constexpr (FINE) mma(oacc[i], v[i & 1], pl);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+#pragma unroll
+        for (int i = 0; i < NB - AHEAD; ++i) o_step(i);
+        if (s + 1 < steps) {
+          if constexpr (SW == 1) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this stage is read
+          landed(s + 1, Count<NS - 2>{});  // (and by every wave)
+          st = st + 1 == NS ? 0 : st + 1;
+          tile = ring + st * C::STAGE;
+          k_first();
+          if (s + NS < steps) look(tile_of(s + NS));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = NB - AHEAD; i < NB; ++i) o_step(i);
+      }
+    } else {
+      f32x4* parts = (f32x4*)(smem + C::kRing);
+      auto k_read = [&](int i) { return raw_at(i < NK ? (tile + at_k) ^ (32 * i) : tile + at_b); };
+      constexpr int RA = 3;
+      i32x4 raw[RA];
+      auto k_first = [&]() {
+#pragma unroll
+        for (int i = 0; i < RA; ++i) raw[i] = k_read(i);
+        tile_first();
+      };
+      // This wave's half of a tile's scores to z and to the other wave, as above.
+      auto scores = [&](int turn_of) {
+        f32x16 sc, sk;
+        f32x4 fk[4];
+        f16x8 k[2][2];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) widen4(k[0][j >> 1], 4 * (j & 1), raw[0][j]);
+        asm volatile("s_nop 1" : "+v"(k[0][0]), "+v"(k[0][1]));
+#pragma unroll
+        for (int i = 0; i <= NK; ++i) {
+          f32x16& acc = i < NK ? sc : sk;
+          if (i + RA <= NK) raw[i % RA] = k_read(i + RA);
+          if (i == 0) {
+            give_powers(exps);
+          } else if (i == 1) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) fc[r] = powers(0, 4 * r), fk[r] = powers(1, 4 * r);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f16x8& q = j & 1 ? ql[i][j >> 1] : qh[i][j >> 1];
+            if (j == 0 && (i == 0 || i == NK)) score_step<true>(acc, k[i & 1][j >> 1], q);
+            else score_step<false>(acc, k[i & 1][j >> 1], q);
+            if (i < NK) {
+              f16x8& y = k[i + 1 & 1][j >> 1];
+              widen4(y, 4 * (j & 1), raw[(i + 1) % RA][j]);
+              if (j & 1) asm volatile("" : "+v"(y));  // (here, not where it is used)
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (j % (4 / PER) == 4 / PER - 1 && PER * i + j / (4 / PER) < NJ) copy(PER * i + j / (4 / PER));
+          }
+        }
+        scores_done(sc, sk);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z[r] = __builtin_fmaf(sk[r], fk[r >> 2][r & 3], sc[r] * fc[r >> 2][r & 3]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) parts[((turn_of * 4 + wave) * 4 + r) * 64 + l] = f32x4{z[4 * r], z[4 * r + 1], z[4 * r + 2], z[4 * r + 3]};
+      };
+      if (steps > 0) {
+        landed(0, Count<NS - 1>{});
+        k_first();
+        mode = kNone;
+        scores(0);
+        if (NS < steps) look(tile_of(NS));
+        landed(1, Count<NS - 2>{});
+      }
+      // Step s: tile s's weights and O, then the scores of the tile after it, whose copies have landed.
+      for (int s = 0; s < steps; ++s) {
+        const int bad = uniform(bads), other = wave ^ C::HG;
+        f32x4 theirs[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) theirs[r] = parts[(((s & 1) * 4 + other) * 4 + r) * 64 + l];
+        constexpr int AHEAD = 4;
+        auto v_read = [&](int i) { return columns_at(((tile + at_v) ^ (32 * (i % NB))) + i / NB * 16 * CH * 16); };
+        i32x2 vr[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) vr[i] = v_read(i);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z[r] += theirs[r >> 2][r & 3];
+        weigh(s, bad);
+        f16x8 ph[2], pl[2], v[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) operand(8 * k, ph[k], pl[k]);
+        widen4(v[0], 0, vr[0][0]);
+        widen4(v[0], 4, vr[0][1]);
+#pragma unroll
+        for (int i = 0; i < 2 * NB; ++i) {
+          if (i + AHEAD < 2 * NB) vr[i % AHEAD] = v_read(i + AHEAD);
+          mma(oacc[i % NB], v[i & 1], ph[i / NB]);
+          if (i + 1 < 2 * NB) {
+            widen4(v[i + 1 & 1], 0, vr[(i + 1) % AHEAD][0]);
+            widen4(v[i + 1 & 1], 4, vr[(i + 1) % AHEAD][1]);
+          }
+          if constexpr (FINE) mma(oacc[i % NB], v[i & 1], pl[i / NB]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (s + 1 < steps) {
+          const int was = st;
+          st = st + 1 == NS ? 0 : st + 1;
+          tile = ring + st * C::STAGE;
+          k_first();
+          // (the place of tile s - 1 is free: every wave has passed the barrier after it)
+          if (s > 0 && s - 1 + NS < steps) ready(tile_of(s - 1 + NS), was == 0 ? NS - 1 : was - 1);
+          else mode = kNone;
+          scores(s + 1 & 1);
+          if (s + NS < steps) look(tile_of(s + NS));
+          landed(s + 2, Count<NS - 3>{});
         }
       }
-      if constexpr (SW == 1) {
-        if (tile_of(s + NS) < it1) {
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this stage is read
-          fetch(tile_of(s + NS), st);
-        }
-      }
-      st = st + 1 == NS ? 0 : st + 1;
     }
 
-    // lane: head n, columns 16 i + 4 g + r
-    float ltot = quad_sum(lsum);
-    int lower = -(d + kLift);
+    // lane: head n, columns 16 i + 4 g + r of its wave's, or 32 i + 8 (r / 4) + 4 g + r % 4: O's f32x4 number j
+    float ltot = head_sum<WIDE>(lsum);
+    const int lower = -(d + kLift);
+    auto quad_of = [&](int j) {
+      if constexpr (WIDE) return f32x4{oacc[j >> 2][4 * (j & 3)], oacc[j >> 2][4 * (j & 3) + 1], oacc[j >> 2][4 * (j & 3) + 2], oacc[j >> 2][4 * (j & 3) + 3]};
+      else return oacc[j];
+    };
     const bool whole = it0 == 0 && it1 == row_end - row_first;
+    float f;
+    f32x4* sums = (f32x4*)smem;
     if constexpr (KW > 1) {
       // the waves' sums under their common maximum
       lds_barrier();  // every tile is read
-      if (g == 0) s_ml[wave][0][n] = m, s_ml[wave][1][n] = ltot;
+      if (g == 0) lds.ml[wave][0][n] = m, lds.ml[wave][1][n] = ltot;
       lds_barrier();
       float top = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < KW; ++u) top = fmaxf(top, s_ml[u * SW + sr][0][n]);
+      for (int u = 0; u < KW; ++u) top = fmaxf(top, lds.ml[u * SW + sr][0][n]);
       auto factor = [&](float x) { return x == -INFINITY ? 0.f : __builtin_ldexpf(1.f, (int)fmaxf(x - top, -1e5f)); };
       float sum = 0.f;
 #pragma unroll
       for (int u = 0; u < KW; ++u) {
-        const float lu = s_ml[u * SW + sr][1][n];
-        sum += lu == 0.f ? 0.f : lu * factor(s_ml[u * SW + sr][0][n]);
+        const float lu = lds.ml[u * SW + sr][1][n];
+        sum += lu == 0.f ? 0.f : lu * factor(lds.ml[u * SW + sr][0][n]);
       }
-      const float f = factor(m);
-      f32x4* sums = (f32x4*)smem;
+      const float mine = __builtin_ldexpf(factor(m), lower);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        f32x4 x;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = __builtin_ldexpf(oacc[i][r], lower) * f;
-        sums[(wave * NB + i) * 64 + l] = x;
-      }
+      for (int j = 0; j < C::kO; ++j) sums[(wave * C::kO + j) * 64 + l] = quad_of(j) * mine;
       m = top;
       ltot = sum;
+      f = whole ? 1.f / ltot : 1.f;
       lds_barrier();
+    } else {
+      f = __builtin_ldexpf(whole ? 1.f / ltot : 1.f, lower);
     }
-    const int h = h0 + 16 * hg + n;
-    const float f = whole ? 1.f / ltot : 1.f;
-    if (16 * hg + n < heads) {
+    const int h = h0 + GH * hg + n;
+    if (GH * hg + n < heads) {
       const int64_t place_of = whole ? (int64_t)t * a.H + h : (int64_t)partial_place(w, per, row_first) * a.H + h;
-      float* o = (whole ? a.obar : a.part_o) + place_of * a.d_c + 16 * NB * cs + 4 * g;
+      float* o = (whole ? a.obar : a.part_o) + place_of * a.d_c + 4 * g;
 #pragma unroll
-      for (int j = 0; j < NB / KW; ++j) {
-        const int i = KW > 1 ? KW * j + kw : j;
-        if (16 * (NB * cs + i) >= a.d_c) continue;
-        f32x4 x;
+      for (int i = 0; i < C::kO / KW; ++i) {
+        const int j = KW > 1 ? KW * i + kw : i, c = WIDE ? 32 * (NB * cs + (j >> 2)) + 8 * (j & 3) : 16 * (NB * cs + j);
+        if (c >= a.d_c) continue;
+        f32x4 y;
         if constexpr (KW > 1) {
-          const f32x4* sums = (const f32x4*)smem;
-          x = sums[(sr * NB + i) * 64 + l];
+          y = sums[(sr * C::kO + j) * 64 + l];
 #pragma unroll
-          for (int u = 1; u < KW; ++u) x += sums[((u * SW + sr) * NB + i) * 64 + l];
+          for (int u = 1; u < KW; ++u) y += sums[((u * SW + sr) * C::kO + j) * 64 + l];
         } else {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x[r] = __builtin_ldexpf(oacc[j][r], lower);
+          y = quad_of(j);
         }
-        *reinterpret_cast<f32x4*>(o + 16 * i) = f32x4{x[0] * f, x[1] * f, x[2] * f, x[3] * f};
+        *reinterpret_cast<f32x4*>(o + c) = f32x4{y[0] * f, y[1] * f, y[2] * f, y[3] * f};
       }
       if (kw == 0 && cs == 0 && g == 0) {
         if (!whole) {
@@ -395,24 +692,24 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
   }
 }
 
-template <int NK, int HG, bool FINE>
+template <int NK, int HEADS, bool FINE>
 __global__ __launch_bounds__(256, 1) void q8_kernel(PagedArgs a, int head_blocks) {
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[Q8Cfg<NK, HG>::LDS];
-  __shared__ int32_t s_ids[4][kIds];
-  __shared__ int s_bad[4][8];
-  __shared__ float s_ml[4][2][16];
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[Q8Cfg<NK, HEADS>::LDS];
+  __shared__ Q8Lds lds;
   // the head blocks of a worker follow each other on one XCD: its L2 serves all but the first
   const int id = blockIdx.x, hb = id / 8 % head_blocks, w = id / (8 * head_blocks) * 8 + id % 8;
   const int h0 = hb * a.heads_per_wg;
-  q8_shares<NK, HG, FINE>(a, smem, s_ids, s_bad, s_ml, w, h0, min(a.heads_per_wg, a.H - h0), uniform(a.sched[0]), uniform(a.sched[1]));
+  q8_shares<NK, HEADS, FINE>(a, smem, lds, w, h0, min(a.heads_per_wg, a.H - h0), uniform(a.sched[0]), uniform(a.sched[1]));
 }
 
 template <int NK, bool FINE>
 void launch_q8(const PagedArgs& a, int head_blocks, hipStream_t st) {
   const unsigned wgs = (unsigned)(head_blocks * a.workers);
-  if (a.heads_per_wg <= 16) q8_kernel<NK, 1, FINE><<<wgs, 256, 0, st>>>(a, head_blocks);
-  else if (NK > 8 || a.heads_per_wg <= 32) q8_kernel<NK, 2, FINE><<<wgs, 256, 0, st>>>(a, head_blocks);
-  else if constexpr (NK <= 8) q8_kernel<NK, 4, FINE><<<wgs, 256, 0, st>>>(a, head_blocks);
+  if (a.heads_per_wg <= 16) q8_kernel<NK, 16, FINE><<<wgs, 256, 0, st>>>(a, head_blocks);
+  else if constexpr (NK <= 8) {
+    if (a.heads_per_wg <= 32) q8_kernel<NK, 32, FINE><<<wgs, 256, 0, st>>>(a, head_blocks);
+    else q8_kernel<NK, 64, FINE><<<wgs, 256, 0, st>>>(a, head_blocks);
+  }
 }
 
 }  // namespace

@@ -673,3 +673,34 @@ def test_shares_of_many_pages(widths, d_c, heads, page, lengths):
     print(f"out is off by {(off / own) ** 0.5:.4f} of its rounding")
     # p in fp16 adds an eighth of a rounding to each weight: sqrt(1 + 1/64), and the rest 2%
     assert off ** 0.5 <= 1.03 * own ** 0.5
+
+
+def test_a_scale_of_nan():
+    """Byte 255 is NaN, byte 0 is 2^-127, in the read and in the rows that see them."""
+    import paper_2607_17644_amd as L
+    x = make([40, 70], 16, heads=4)
+    a = call(x)
+    y = dict(x, scales=x["scales"].clone())
+    y["scales"][int(x["table"][0, 1]), 3, 1] = 255
+    b = call(y)
+    assert b[0][0].isnan().all() and b[1][0].isnan().all() and torch.equal(a[0][1], b[0][1])
+    y["scales"][int(x["table"][0, 1]), 3, 1] = 0
+    check(y)
+    p = dataclasses.replace(x["p"], rows=3)
+    y["scales"][int(x["table"][0, 1]), 4, 0] = 255
+    c, k = L.laga_cache_read_q8(p, x["cache"], y["scales"], i32(x["table"]), i32([20, 19, 18]), row_request=i32([0, 0, 0]))
+    assert c[0].isnan().all() and not k[0].isnan().any() and (k[1].abs() <= 2.0 ** -118).all() and not c[1].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_append_near_where_two_roundings_meet(dtype):
+    """Many rows, so that numbers fall as near to the middle of two as single precision can tell, and largest numbers near
+    the end of a scale; and rows of few different numbers, which meet there exactly."""
+    y = append_inputs(3000, 16, "v3", 512, dtype, seed=11)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    some = torch.tensor([1.0, 1.0625, 1.125, 1.1875, -1.0625, 1.75, -1.75, 0.0], device="cuda")
+    y["x"][:500] = some[torch.randint(0, 8, (500, 576), generator=gen, device="cuda")].to(y["x"].dtype)
+    y["position"][:250] = 0
+    y["position"][2000:] = np.arange(1000) * 131
+    check_append(y)
+    check_append(y, gamma=False, eps=0.0)
