@@ -423,7 +423,7 @@ LAGA_API laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologu
  *                      [0] is the latent's, [1] the key's
  * so element j of the latent is cache[j] * 2^(scales[0] - 127). laga_paged_t and the conventions
  * of the calls above hold as they are (dtype: of q, W_kv_b, out and the tokens), pages are planned
- * and released by the same calls, and the limits are theirs.
+ * and released by the same calls, and the limits are theirs (rows * (table_width * page_size / 32 + 15) below 2^31).
  *
  * laga_cache_append_q8: laga_cache_append, its row quantised as it is written. With a the
  * largest finite magnitude of a part's elements, the part's scale is 2^e, e the least whole

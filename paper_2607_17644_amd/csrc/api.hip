@@ -203,7 +203,9 @@ size_t elem_size(const laga_paged_t* p) { return p->dtype == LAGA_DTYPE_BF16 ? 2
 // A cache in 8 bits: its rows are bytes, and a page begins at one divisible by 16.
 laga_status_t validate_paged_q8(const laga_paged_t* p, PagedDims* d) {
   const laga_status_t s = validate_paged(p, d);
-  return s == LAGA_OK && d->page_stride % 16 != 0 ? LAGA_ERR_UNSUPPORTED : s;
+  if (s != LAGA_OK) return s;
+  const int64_t tiles = (d->width * (int64_t)d->page + kTileKeys - 1) / kTileKeys;
+  return d->page_stride % 16 != 0 || d->T * (tiles + kQ8RowCost) >= kMaxElems ? LAGA_ERR_UNSUPPORTED : LAGA_OK;
 }
 
 // [schedule | absorbed queries | their second and third parts (bf16) | whole rows | partials: outputs, statistics]
@@ -479,6 +481,7 @@ laga_status_t laga_paged_attn_q8(const laga_paged_t* p, const laga_prologue_t* c
   PagedArgs a = paged_args(p, cfg, d, plan);
   a.q = q; a.w = w_kv_b; a.cache = cache; a.scales = scales; a.table = block_table; a.row_request = row_request;
   a.position = position; a.out = out; a.lse = lse;
+  a.row_cost = plan.heads_per_wg > 16 ? kQ8WideRowCost : kQ8RowCost;
   a.sched = (int32_t*)(wsb + ws.sched); a.qa = wsb + ws.qa; a.qa_max = (float*)(wsb + ws.qa_max);
   a.obar = (float*)(wsb + ws.obar); a.part_o = (float*)(wsb + ws.part_o); a.part_ml = (float*)(wsb + ws.part_ml);
   hipStream_t st = (hipStream_t)stream;

@@ -143,6 +143,7 @@ struct PagedArgs {
   // a cache in 8 bits: qa is fp32 [T][(d_c + d_rope) / 4][H][4], and
   const uint8_t* scales;  // [n_pages][page][2]
   float* qa_max;          // [T][H][qa_blocks(d_c)]: largest magnitudes of qa's blocks of kQaBlock columns, and of the band's
+  int row_cost;           // units of a row besides its tiles
 };
 constexpr int kQaBlock = 128;
 __host__ __device__ inline int qa_blocks(int d_c) { return (d_c + kQaBlock - 1) / kQaBlock + 1; }
@@ -216,6 +217,8 @@ inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
   return p;
 }
 
+// A cache in 8 bits: units of a row as above.
+constexpr int kQ8RowCost = 14, kQ8WideRowCost = 5;
 // A cache in 8 bits: a wave has 16 heads, with all that they need in its registers up to d_c = 512; above, the four waves of
 // a workgroup share the columns of their sums.
 inline PagedPlan paged_plan_q8(int H, int d_c) {

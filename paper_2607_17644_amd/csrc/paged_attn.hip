@@ -216,7 +216,12 @@ __device__ void lay_out_tiles(const PagedArgs& a) {
   again = __syncthreads_or(again);
   tiles = rows = 0;
   for (int w = 0; w < kAbsorbWaves; ++w) tiles += sm[w], rows += sm[kAbsorbWaves + w];
-  const Shares sh = shares_of(tiles, rows, a.workers, a.groups);
+  Shares sh = shares_of(tiles, rows, a.workers, a.groups);
+  if (a.row_cost > 0) {
+    sh.cost = a.row_cost;
+    sh.total = tiles + rows * sh.cost;
+    sh.per = units_per_worker(sh.total, sh.workers);
+  }
   __syncthreads();
   int sum = 0;
   for (int base = 0; base < a.T; base += NT) {

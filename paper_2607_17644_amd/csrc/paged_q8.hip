@@ -219,46 +219,37 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
       look_pg = key < visible ? page_of(key) : win;
       look_id = ids[look_pg - win];
     };
-    enum { kNone, kFlat, kRows };
-    int mode = kNone, src_lo = 0, src_hi = 0;
-    const char *base = nullptr, *exps_base = nullptr;  // of a tile in one page, whose rows follow each other
+    bool asking = false;
+    int src_lo = 0, src_hi = 0;  // where row l % 32 is
+    int row_lo = 0, row_hi = 0;  // and this lane's row of the next copy
     uint32_t to = 0;
+    constexpr int MAIN = C::NM / SW;  // of this wave's copies, those of latents
+    static_assert(C::NM % SW == 0);
+    auto next_row = [&](int jj) {
+      const int r = jj < MAIN ? at_src + jj * SW * C::RPC : at_key_src + (SW == 1 ? (jj - MAIN) * 16 : 0);
+      row_lo = __builtin_amdgcn_ds_bpermute(4 * r, src_lo);
+      row_hi = __builtin_amdgcn_ds_bpermute(4 * r, src_hi);
+    };
     auto ready = [&](int it, int stage) {
-      const int k0 = it * kTileKeys, l = fresh_lane(), key = k0 + (l & 31);
+      const int key = it * kTileKeys + (fresh_lane() & 31);
       const bool live = key < visible, ok = live && (unsigned)look_id < (unsigned)a.n_pages;
       const int off = key - look_pg * a.page;
-      const uint32_t bad = (uint32_t)__ballot(live && !ok);
-      if (l == 0) lds.bad[wave][stage] = (int)bad;
-      to = ring + stage * C::STAGE;
-      const int id0 = uniform(look_id), off0 = uniform(off);
-      if (k0 + kTileKeys <= visible && off0 + kTileKeys <= a.page && !bad) {
-        mode = kFlat;
-        base = (const char*)a.cache + (int64_t)id0 * a.page_stride + (int64_t)off0 * W;
-        exps_base = (const char*)a.scales + 2 * ((int64_t)id0 * a.page + off0);
-      } else {
-        mode = kRows;
-        const uintptr_t src = ok ? (uintptr_t)a.cache + (int64_t)look_id * a.page_stride + (int64_t)off * W : (uintptr_t)kZeroRow;
-        src_lo = (int)(uint32_t)src;
-        src_hi = (int)(uint32_t)(src >> 32);
-        if (sr == 0)
-          copy_short(ok ? (const char*)a.scales + 2 * ((int64_t)look_id * a.page + off) : (const char*)kZeroRow, uniform((int)(to + C::TILE)));
-      }
+      const uintptr_t src = ok ? (uintptr_t)a.cache + (int64_t)look_id * a.page_stride + (int64_t)off * W : (uintptr_t)kZeroRow;
+      src_lo = (int)(uint32_t)src;
+      src_hi = (int)(uint32_t)(src >> 32);
+      lds.bad[wave][stage] = (int)(uint32_t)__ballot(live && !ok);  // (the same from every lane)
+      to = ring + stage * C::STAGE + sr * 1024;
+      if (sr == 0)
+        copy_short(ok ? (const char*)a.scales + 2 * ((int64_t)look_id * a.page + off) : (const char*)kZeroRow, uniform((int)(to + C::TILE)));
+      next_row(0);
+      asking = true;
     };
     auto copy = [&](int jj) {
-      constexpr int MAIN = C::NM / SW;
-      static_assert(C::NM % SW == 0);
-      if (mode == kNone || (SW == 4 && jj == MAIN && sr > 1)) return;
-      const bool latent = jj < MAIN;
-      const int r0 = latent ? jj * SW * C::RPC : SW == 1 ? (jj - MAIN) * 16 : 0, r = latent ? at_src : at_key_src;
-      const uint32_t off = latent ? min(at_copy ^ (turn<NK, WIDE>(r0) * 16), (uint32_t)a.d_c - 16) : at_band;
-      const uint32_t dst = to + (sr + SW * jj) * 1024;
-      if (mode == kFlat) {
-        if (jj == 0 && sr == 0) copy_short(exps_base + 2 * (l & 31), uniform((int)(to + C::TILE)));
-        g2lds16_so(base + r0 * W, __umul24(r, W) + off, (void*)(uintptr_t)dst);
-      } else {
-        const uintptr_t row = (uintptr_t)(uint32_t)__shfl(src_lo, r0 + r) | ((uintptr_t)(uint32_t)__shfl(src_hi, r0 + r) << 32);
-        g2lds16((const char*)row + off, (void*)(uintptr_t)dst);
-      }
+      if (!asking || (SW == 4 && jj == MAIN && sr > 1)) return;
+      const uint32_t off = jj < MAIN ? min(at_copy ^ (turn<NK, WIDE>(jj * SW * C::RPC) * 16), (uint32_t)a.d_c - 16) : at_band;
+      const uintptr_t row = (uintptr_t)(uint32_t)row_lo | ((uintptr_t)(uint32_t)row_hi << 32);
+      g2lds16((const char*)row + off, (void*)(uintptr_t)(to + SW * jj * 1024));
+      if (jj + 1 < NJ) next_row(jj + 1);
     };
 
     lds_barrier();  // the tiles, sums and page ids before are read
@@ -273,16 +264,8 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
       if constexpr (SW > 1) lds_barrier();  // every wave's copies (and partial scores)
       else asm volatile("" ::: "memory");   // (nothing is read before)
     };
-#pragma unroll 1
-    for (int i = 0; i < min(NS, steps); ++i) {
-      look(tile_of(i));
-      ready(tile_of(i), i);
-#pragma unroll
-      for (int jj = 0; jj < NJ; ++jj) copy(jj);
-    }
-    mode = kNone;
-    // the queries of head n, scaled by 2^-e to 1 .. 2 at most: of step i and half u elements 64 i + 16 g + 8 u .., or of this
-    // wave's half 32 i + 16 g + 8 u ..
+    // The queries of head n, scaled by 2^-e to 1 .. 2 at most: of step i and half u elements 64 i + 16 g + 8 u .., or of this
+    // wave's half 32 i + 16 g + 8 u ... They are read first, and widened while the first tiles are on their way.
     f16x8 qh[NK + 1][2], ql[NK + 1][2];
     float mult;  // of a score in base 2
     {
@@ -292,15 +275,9 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
       const f32x4* q = (const f32x4*)a.qa + (int64_t)t * (W / 4) * a.H + (th - (int64_t)t * a.H);
       auto at = [&](int i, int u) { return (WIDE ? 32 * (i < NK ? NK * cs + i : cs) : i < NK ? 64 * i : 0) + 16 * g + 8 * u; };
       auto there = [&](int i, int u) { return at(i, u) < (i < NK ? a.d_c : a.d_rope); };
-      float top = 0.f;
-      for (int i = 0; i < blocks; ++i) top = fmaxf(top, tops[i]);
-      const int e = top > 0.f ? max(__builtin_amdgcn_frexp_expf(top) - 1, -126) : 0;
-      const float down = __builtin_ldexpf(1.f, -e);
-      mult = __builtin_ldexpf(a.scale_log2, e);
       constexpr int TURN = 9;  // steps whose numbers are on their way at once
-#pragma unroll
-      for (int i0 = 0; i0 <= NK; i0 += TURN) {
-        f32x4 x[TURN][2][2];
+      f32x4 x[TURN][2][2];
+      auto read = [&](int i0) {
 #pragma unroll
         for (int i = i0; i < min(i0 + TURN, NK + 1); ++i)
 #pragma unroll
@@ -309,6 +286,27 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
             x[i - i0][u][0] = from[0];
             x[i - i0][u][1] = from[a.H];
           }
+      };
+      float top = 0.f;
+      for (int i = 0; i < blocks; ++i) top = fmaxf(top, tops[i]);
+      read(0);
+      if (steps > 0) look(tile_of(0));
+      wait_vmem();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll 1
+      for (int i = 0; i < min(NS, steps); ++i) {
+        if (i > 0) look(tile_of(i));
+        ready(tile_of(i), i);
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) copy(jj);
+      }
+      asking = false;
+      const int e = top > 0.f ? max(__builtin_amdgcn_frexp_expf(top) - 1, -126) : 0;
+      const float down = __builtin_ldexpf(1.f, -e);
+      mult = __builtin_ldexpf(a.scale_log2, e);
+#pragma unroll
+      for (int i0 = 0; i0 <= NK; i0 += TURN) {
+        if (i0 > 0) read(i0);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = i0; i < min(i0 + TURN, NK + 1); ++i)
@@ -423,7 +421,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
     // the copies of step s are those of the tile that takes the place of the one before its own
     auto ask = [&](int s) {
       if (s > 0 && s - 1 + NS < steps) ready(tile_of(s - 1 + NS), st == 0 ? NS - 1 : st - 1);
-      else mode = kNone;
+      else asking = false;
     };
 
     if constexpr (!WIDE) {
@@ -573,7 +571,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
       if (steps > 0) {
         landed(0, Count<NS - 1>{});
         k_first();
-        mode = kNone;
+        asking = false;
         scores(0);
         if (NS < steps) look(tile_of(NS));
         landed(1, Count<NS - 2>{});
@@ -615,7 +613,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
           k_first();
           // (the place of tile s - 1 is free: every wave has passed the barrier after it)
           if (s > 0 && s - 1 + NS < steps) ready(tile_of(s - 1 + NS), was == 0 ? NS - 1 : was - 1);
-          else mode = kNone;
+          else asking = false;
           scores(s + 1 & 1);
           if (s + NS < steps) look(tile_of(s + NS));
           landed(s + 2, Count<NS - 3>{});
