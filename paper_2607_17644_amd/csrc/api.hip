@@ -432,7 +432,12 @@ laga_status_t laga_cache_append_q8(const laga_paged_t* p, const laga_prologue_t*
   if (s == LAGA_OK) s = append_args(d, cfg, latent_raw, latent_stride, gamma, kpe_raw, kpe_stride, position, slot, cache, &a.a);
   if (s != LAGA_OK) return s;
   if (misaligned(scales)) return LAGA_ERR_ALIGN;
+  constexpr double kTurn = 0.15915494309189533576888376337251;  // 1 / (2 pi)
+  static_assert(64 / 2 <= kMostPairs, "d_rope is 64 at most");
   a.scales = scales;
+  page_division(d.page, &a.page_magic, &a.page_shift);
+  a.mean = 1. / d.d_c;
+  for (int i = 0; i < d.dr / 2; ++i) a.freq[i] = exp2(-(2. * i / d.dr) * a.a.log2_base) * kTurn;
   hipStream_t st = (hipStream_t)stream;
   return from_hip(p->dtype == LAGA_DTYPE_BF16 ? launch_append_q8<bf16>(a, st) : launch_append_q8<float>(a, st));
 }

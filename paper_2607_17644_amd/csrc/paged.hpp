@@ -69,9 +69,13 @@ hipError_t launch_append(const AppendArgs& a, hipStream_t st);
 // [n_pages][page][2], the exponents + kScaleBias of the powers of two that its latent and its shared key stand for.
 constexpr int kScaleBias = 127;
 constexpr int kLeastScale = -100, kMostScale = 119;  // exponents that are written
+constexpr int kMostPairs = 32;  // of a band
 struct AppendQ8Args {
   AppendArgs a;
   uint8_t* scales;
+  uint32_t page_magic, page_shift;  // slot / page
+  double mean;                      // 1 / d_c
+  double freq[kMostPairs];          // of the band's pairs, in turns per position
 };
 template <typename T>
 hipError_t launch_append_q8(const AppendQ8Args& a, hipStream_t st);

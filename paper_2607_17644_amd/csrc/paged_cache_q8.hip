@@ -4,9 +4,10 @@
 //   e = the least whole number with a <= 448 2^e (448 the largest e4m3 number), kLeastScale at least, kMostScale at most
 //   byte j = e4m3(x_j 2^-e), to nearest, ties to even, at most 448 in magnitude; NaN where x_j is no finite number
 // A power of two leaves every bit of the mantissa to the number, and its product with one is exact in bf16 and fp32.
+#include <type_traits>
+
 #include "common.hpp"
 #include "paged.hpp"
-#include "rope.hpp"
 
 namespace laga {
 namespace {
@@ -14,33 +15,33 @@ namespace {
 typedef __attribute__((__vector_size__(2 * sizeof(int)))) int i32x2;
 typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
 
-// The row is formed in double precision: half a step of e4m3 decides over an eighth of the value, and in
-// single precision some 40 of the 9.4 million bytes of 16384 tokens fall to the other side. (Single precision with a
-// check for numbers that are near such a place, and double for rows that have one, took 20 us for 16384 tokens, as this
-// does: the band's frequencies, the reductions and the check itself remain.)
+// The row is formed in double precision: half a step of e4m3 decides over an eighth of the value, and in single precision
+// some 40 of the 9.4 million bytes of 16384 tokens fall to the other side. What bounds a prompt's append is therefore its
+// vector instructions (830 a wave of two tokens; 81 % of the cycles issue one when it was 900): 16384 tokens 16.8 us, 19.5
+// before the place below (which was the number's bits shifted into fp32's), the largest magnitude in place of the largest
+// exponent and the band's frequencies from the host; 13.0 to a cache in bf16. (Single precision with a check for numbers
+// that are near such a place, and double for rows that have one, took 20.)
 // The e of one number alone: of a part, the largest of its numbers'.
 __device__ __forceinline__ int exponent_of(double x) {
   const uint64_t u = (uint64_t)__builtin_bit_cast(int64_t, x) & ~((uint64_t)1 << 63);
   const int e = (int)(u >> 52);
   return e == 2047 ? kLeastScale : e - 1023 - 8 + ((u & (((uint64_t)1 << 52) - 1)) > (uint64_t)3 << 50);
 }
-// The number in fp32 with its last bit set where anything was cut off, so that e4m3's rounding of it is that of x itself.
-// Below 2^-30, which is zero in e4m3: zero.
-__device__ __forceinline__ float cut(double x) {
-  const uint64_t u = (uint64_t)__builtin_bit_cast(int64_t, x);
-  const uint32_t hi = (uint32_t)(u >> 32), lo = (uint32_t)u, mag = hi & 0x7fffffffu;
-  uint32_t f = ((mag - 0x38000000u) << 3) | lo >> 29 | ((lo & 0x1fffffffu) != 0);
-  f = mag < 0x3e100000u ? 0u : mag >= 0x7ff00000u ? 0x7fc00000u : f;
-  return __builtin_bit_cast(float, f | (hi & 0x80000000u));
+// x 2^-e at the nearest e4m3 number, even at ties: its last place is an eighth of its leading one, 2^-9 at least, and a
+// sum with 1.5 2^52 of that place ends there. ANY: x may be infinite, or above 448 2^e.
+template <bool ANY>
+__device__ __forceinline__ float eighth(double x, double down) {
+  const double y = x * down;
+  const uint32_t hi = (uint32_t)((uint64_t)__builtin_bit_cast(int64_t, y) >> 32);
+  const double place = __builtin_bit_cast(double, (uint64_t)(max(hi & 0x7ff00000u, (1023u - 6) << 20) + (49u << 20 | 1u << 19)) << 32);
+  float f = (float)((y + place) - place);
+  if constexpr (ANY) f = !(__builtin_fabs(y) < __builtin_inf()) ? __builtin_nanf("") : __builtin_amdgcn_fmed3f(f, -448.f, 448.f);
+  return __builtin_copysignf(f, __builtin_bit_cast(float, hi));
 }
-// x 2^-e as e4m3 will have it, and four of them
-__device__ __forceinline__ float eighth(double x, int e) {
-  const float f = cut(__builtin_ldexp(x, -e));
-  return f != f ? f : __builtin_amdgcn_fmed3f(f, -448.f, 448.f);
-}
-__device__ __forceinline__ int four(const double (&x)[4], int e) {
-  int y = __builtin_amdgcn_cvt_pk_fp8_f32(eighth(x[0], e), eighth(x[1], e), 0, false);
-  return __builtin_amdgcn_cvt_pk_fp8_f32(eighth(x[2], e), eighth(x[3], e), y, true);
+template <bool ANY>
+__device__ __forceinline__ int four(const double* x, double down) {
+  int y = __builtin_amdgcn_cvt_pk_fp8_f32(eighth<ANY>(x[0], down), eighth<ANY>(x[1], down), 0, false);
+  return __builtin_amdgcn_cvt_pk_fp8_f32(eighth<ANY>(x[2], down), eighth<ANY>(x[3], down), y, true);
 }
 __device__ __forceinline__ int within(int e) { return min(max(e, kLeastScale), kMostScale); }
 
@@ -56,14 +57,15 @@ __global__ __launch_bounds__(64 * kWaves) void append_q8_kernel(AppendQ8Args arg
   const int nch = a.d_c / 8, width = a.d_c + a.d_rope;
   uint8_t* cache = (uint8_t*)a.cache;
   auto row_of = [&](int slot) {
-    return cache + (int64_t)(slot / a.page) * a.page_stride + (int64_t)(slot % a.page) * width;
+    const int pg = (int)((uint64_t)(uint32_t)slot * args.page_magic >> args.page_shift);
+    return cache + pg * a.page_stride + (int64_t)(slot - pg * a.page) * width;
   };
 
   float v[TPW][CH][8];
   int slot[TPW];
 #pragma unroll
   for (int i = 0; i < TPW; ++i) {
-    slot[i] = t0 + i < a.T ? a.slot[t0 + i] : -1;
+    slot[i] = __builtin_amdgcn_readfirstlane(t0 + i < a.T ? a.slot[t0 + i] : -1);
     if ((unsigned)slot[i] >= (unsigned)a.n_slots) slot[i] = -1;
     const T* x = (const T*)a.latent + (t0 + i < a.T ? t0 + i : t0) * a.latent_stride;
 #pragma unroll
@@ -81,52 +83,84 @@ __global__ __launch_bounds__(64 * kWaves) void append_q8_kernel(AppendQ8Args arg
     for (int e = 0; e < 8; ++e) g[k][e] = 1.f;
     if (a.gamma && l + 64 * k < nch) load8((const T*)a.gamma + 8 * (l + 64 * k), g[k]);
   }
+  double sum[TPW], y[TPW][CH][8];
+  int most[TPW];
 #pragma unroll
   for (int i = 0; i < TPW; ++i) {
-    if (slot[i] < 0) continue;  // wave-uniform
-    double ss = 0.;
+    sum[i] = 0.;
 #pragma unroll
     for (int k = 0; k < CH; ++k)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = __builtin_fma((double)v[i][k][e], (double)v[i][k][e], ss);
+      for (int e = 0; e < 8; ++e) sum[i] = __builtin_fma((double)v[i][k][e], (double)v[i][k][e], sum[i]);
+  }
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) ss += __shfl_xor(ss, o);
-    const double r = 1. / sqrt(ss / (double)a.d_c + (double)a.eps);
-    double y[CH][2][4];
-    int most = kLeastScale;
+  for (int o = 32; o >= 1; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) sum[i] += __shfl_xor(sum[i], o);
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < TPW; ++i) {
+    const double r = rsqrt(__builtin_fma(sum[i], args.mean, (double)a.eps));
+    double top = 0.;
 #pragma unroll
     for (int k = 0; k < CH; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const double x = (double)v[i][k][e] * r * (double)g[k][e];
-        y[k][e / 4][e % 4] = x;
-        if (l + 64 * k < nch) most = max(most, exponent_of(x));
+        y[i][k][e] = (double)v[i][k][e] * r * (double)g[k][e];
+        top = __builtin_fmax(top, __builtin_fabs(y[i][k][e]));
       }
+    most[i] = exponent_of(top);
+    if (__ballot(top == __builtin_inf())) {
+      any = true;
+      most[i] = kLeastScale;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) most = max(most, __shfl_xor(most, o));
-    const int e = within(most);
+      for (int k = 0; k < CH; ++k)
 #pragma unroll
-    for (int k = 0; k < CH; ++k)
-      if (l + 64 * k < nch) *reinterpret_cast<i32x2*>(row_of(slot[i]) + 8 * (l + 64 * k)) = i32x2{four(y[k][0], e), four(y[k][1], e)};
-    if (l == 0) args.scales[2 * (int64_t)slot[i]] = (uint8_t)(e + kScaleBias);
+        for (int e = 0; e < 8; ++e) most[i] = max(most[i], exponent_of(y[i][k][e]));
+    }
   }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) most[i] = max(most[i], __shfl_xor(most[i], o));
+#pragma unroll
+  for (int i = 0; i < TPW; ++i) any = any || most[i] >= kMostScale;
+  auto write = [&](auto is_any) {
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+      if (slot[i] < 0) continue;  // wave-uniform
+      const int e = within(most[i]);
+      const double down = __builtin_ldexp(1., -e);
+#pragma unroll
+      for (int k = 0; k < CH; ++k)
+        if (l + 64 * k < nch)
+          *reinterpret_cast<i32x2*>(row_of(slot[i]) + 8 * (l + 64 * k)) =
+              i32x2{four<decltype(is_any)::value>(y[i][k], down), four<decltype(is_any)::value>(y[i][k] + 4, down)};
+      if (l == 0) args.scales[2 * (int64_t)slot[i]] = (uint8_t)(e + kScaleBias);
+    }
+  };
+  if (any) write(std::true_type{});  // (the same on all lanes)
+  else write(std::false_type{});
 
-  const int pairs = a.d_rope / 2, p = l % pairs;  // pairs divides 64
-  const double freq = rope_freq(p, a.d_rope, a.log2_base);
-  for (int i = l / pairs; i < TPW; i += 64 / pairs) {
+  const int pairs = a.d_rope / 2, p = l & pairs - 1, log2_pairs = __ffs(pairs) - 1;  // a power of two, 32 at most
+  const double freq = args.freq[p];
+  for (int i = l >> log2_pairs; i < TPW; i += 64 >> log2_pairs) {
     const int64_t t = t0 + i;
     if (t >= a.T) break;
     const int s = a.slot[t];
     if ((unsigned)s >= (unsigned)a.n_slots) continue;
-    double cs, sn;
-    rope_sincos(a.position_offset + a.position[t], freq, cs, sn);
+    double turns = (double)(a.position_offset + a.position[t]) * freq, cs, sn;
+    turns -= rint(turns);
+    sincospi(2. * turns, &sn, &cs);
     const T* x = (const T*)a.kpe + t * a.kpe_stride + 2 * p;
     const double x0 = to_f32(x[0]), x1 = to_f32(x[1]);
-    const double y[4] = {x0 * cs - x1 * sn, x0 * sn + x1 * cs, 0., 0.};
+    const double y[2] = {x0 * cs - x1 * sn, x0 * sn + x1 * cs};
     int most = max(exponent_of(y[0]), exponent_of(y[1]));
     for (int o = 1; o < pairs; o <<= 1) most = max(most, __shfl_xor(most, o));  // (the lanes of a token are all here)
     const int e = within(most);
-    *reinterpret_cast<uint16_t*>(row_of(s) + a.d_c + 2 * p) = (uint16_t)four(y, e);
+    const double down = __builtin_ldexp(1., -e);
+    *reinterpret_cast<uint16_t*>(row_of(s) + a.d_c + 2 * p) =
+        (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(eighth<true>(y[0], down), eighth<true>(y[1], down), 0, false);
     if (p == 0) args.scales[2 * (int64_t)s + 1] = (uint8_t)(e + kScaleBias);
   }
 }
@@ -201,6 +235,8 @@ void launch_append_q8_t(const AppendQ8Args& a, hipStream_t st) {
 
 }  // namespace
 
+// Two tokens a wave share the band's frequencies and the lanes of its turn, once the waves fill the GPU: 16384 tokens 16.8 us,
+// 18.5 with one, 17.5 with four; 64 tokens 4.8 with one.
 template <typename T>
 hipError_t launch_append_q8(const AppendQ8Args& a, hipStream_t st) {
   if (a.a.T <= 16 * kCus) launch_append_q8_t<T, 1>(a, st);

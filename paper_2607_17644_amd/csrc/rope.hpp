@@ -18,12 +18,5 @@ __device__ __forceinline__ void rope_sincos(int64_t pos, double freq, float& c, 
   a -= kTwoPi * rint(a / kTwoPi);
   sincosf((float)a, &s, &c);
 }
-// the same in double precision
-__device__ __forceinline__ void rope_sincos(int64_t pos, double freq, double& c, double& s) {
-  constexpr double kTwoPi = 6.283185307179586476925286766559;
-  double a = (double)pos * freq;
-  a -= kTwoPi * rint(a / kTwoPi);
-  sincos(a, &s, &c);
-}
 
 }  // namespace laga
