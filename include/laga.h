@@ -418,7 +418,7 @@ LAGA_API laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologu
  * numbers of 8 bits, and one scale for each of its two parts, the latent and the shared key:
  *   cache   [n_pages][page_size, d_c + d_rope]  e4m3 (finite, 448 the largest; one byte), rows
  *                      contiguous, pages page_stride BYTES apart (a multiple of 16; 0:
- *                      page_size * (d_c + d_rope), which then has to be one)
+ *                      page_size * (d_c + d_rope), which is one)
  *   scales  [n_pages][page_size][2]  uint8, contiguous: byte x stands for 2^(x - 127), 255 for NaN;
  *                      [0] is the latent's, [1] the key's
  * so element j of the latent is cache[j] * 2^(scales[0] - 127). laga_paged_t and the conventions

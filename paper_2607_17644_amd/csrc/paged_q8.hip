@@ -7,9 +7,16 @@
 //
 //   z_j = scale 2^e (2^c_j A_j + 2^k_j B_j),  A = qa . c8,  B = q_rope . k8,  O += (p_j 2^(c_j + d)) c8_j
 //
-// so the powers never meet a number of 8 bits. A lone wave per SIMD issues an instruction in 4 to 5 cycles, and a product
-// takes the matrix unit 16: the scores, two numbers' conversions beside each product, are bound by it, O, with four, by
-// the instructions.
+// so the powers never meet a number of 8 bits. A lone wave per SIMD (its registers hold a head group's queries and sums) issues
+// an instruction in 4 to 5 cycles, a 16 x 16 product takes the matrix unit 16 and a 32 x 32 one 32: two numbers' conversions
+// beside each 16 x 16 product of the scores hide behind it, O's four do not.
+//
+// Measured (d_c = 512, d_rope = 64, 578 bytes a key): 64 requests of up to 8192 keys, 16 heads, 51 us, 167 MB at 3.4 TB/s over
+// the launch and 4.6 to 5.1 within a share: bound by memory there, by the shares' starts and ends else (77 us from a
+// cache in bf16). 61 requests, 128 heads: 186 us, 2 requests of up to 100000 keys 101 (169 and 89 in bf16): a step
+// of 32 keys and 64 heads takes 5000 cycles, 1660 of them products; an instruction is issued in 51 % of the cycles, 136
+// conversions per wave among them. Tried there and slower: four waves to 32 heads (240 us), scores beside the products
+// of O (200; its registers are moved about), no gain from fewer exponentials or conflicts (there are none).
 #define LAGA_LDS_DMA_ASM 1
 #include <type_traits>
 
