@@ -17,9 +17,9 @@ typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
 
 // The row is formed in double precision: half a step of e4m3 decides over an eighth of the value, and in single precision
 // some 40 of the 9.4 million bytes of 16384 tokens fall to the other side. What bounds a prompt's append is therefore its
-// vector instructions (830 a wave of two tokens; 81 % of the cycles issue one when it was 900): 16384 tokens 16.8 us, 19.5
-// before the place below (which was the number's bits shifted into fp32's), the largest magnitude in place of the largest
-// exponent and the band's frequencies from the host; 13.0 to a cache in bf16. (Single precision with a check for numbers
+// vector instructions (632 a wave of two tokens, in 67 % of the cycles): 16384 tokens 16.8 us, 19.5 before the place
+// below (which was the number's bits shifted into fp32's), the largest magnitude in place of the largest exponent and the
+// band's frequencies from the host; 13.0 to a cache in bf16. (Single precision with a check for numbers
 // that are near such a place, and double for rows that have one, took 20.)
 // The e of one number alone: of a part, the largest of its numbers'.
 __device__ __forceinline__ int exponent_of(double x) {
