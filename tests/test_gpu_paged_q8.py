@@ -192,6 +192,20 @@ def test_append_of_a_prompt():
     check_append(append_inputs(4101, 64, "v3", 512, "bf16", seed=3))
 
 
+@pytest.mark.parametrize("widths,d_c,dtype", [("v3", 1024, "fp32"), ("v3", 512, "bf16"), ("half", 416, "bf16"), ("small", 32, "fp32")])
+def test_append_of_a_prompt_with_rows_and_weights_out_of_range(widths, d_c, dtype):
+    """Two tokens to a wave: of a pair the one not finite, or a row of zeros, the other as ever; and weights that make every row
+    infinite in places, or larger than a scale reaches."""
+    y = append_inputs(4099, 48, widths, d_c, dtype, seed=d_c)
+    x = y["x"]
+    x[0, 1], x[3, 0], x[6], x[9], x[12, 2], x[15, d_c], x[18, d_c + 1] = (float(v) for v in ("inf", "nan", "0", "inf", "-inf", "inf", "nan"))
+    check_append(y)
+    y["gamma"][0] = 3e38
+    check_append(y)
+    y["gamma"][1], y["gamma"][2] = float("inf"), float("nan")
+    check_append(y)
+
+
 def test_append_at_the_edges_of_numbers():
     """Rows of zeros; a largest number that is 448 2^e, and the next one; numbers that are half-way between two; values that
     are not finite, alone and everywhere; magnitudes from 2^-140 to 2^127."""
