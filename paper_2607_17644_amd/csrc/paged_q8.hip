@@ -11,9 +11,9 @@
 // an instruction in 4 to 5 cycles, a 16 x 16 product takes the matrix unit 16 and a 32 x 32 one 32: two numbers' conversions
 // beside each 16 x 16 product of the scores hide behind it, O's four do not.
 //
-// Measured (d_c = 512, d_rope = 64, 578 bytes a key): 64 requests of up to 8192 keys, 16 heads, 51 us, 167 MB at 3.4 TB/s over
+// Measured (d_c = 512, d_rope = 64, 578 bytes a key): 64 requests of up to 8192 keys, 16 heads, 46 us, 167 MB at 3.6 TB/s over
 // the launch and 4.6 to 5.1 within a share: bound by memory there, by the shares' starts and ends else (77 us from a
-// cache in bf16). 61 requests, 128 heads: 186 us, 2 requests of up to 100000 keys 101 (169 and 89 in bf16): a step
+// cache in bf16). 61 requests, 128 heads: 184 us, 2 requests of up to 100000 keys 99 (169 and 89 in bf16): a step
 // of 32 keys and 64 heads takes 5000 cycles, 1660 of them products; an instruction is issued in 51 % of the cycles, 136
 // conversions per wave among them. Tried there and slower: four waves to 32 heads (240 us), scores beside the products
 // of O (200; its registers are moved about), no gain from fewer exponentials or conflicts (there are none).
@@ -134,6 +134,11 @@ __device__ __forceinline__ void copy_short(const void* g, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ushort %0, off" ::"v"(g), "s"(to) : "memory", "m0");
 }
 
+// 16 bytes per lane to LDS that nothing else is likely to read (a hint)
+__device__ __forceinline__ void copy_past(const void* g, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(g), "s"(to) : "memory", "m0");
+}
+
 template <int N> struct Count { static constexpr int n = N; };
 struct __attribute__((aligned(16))) Q8Lds {
   float powers[4][64];  // of a tile's keys, 2^c and then 2^k, for each wave
@@ -141,8 +146,8 @@ struct __attribute__((aligned(16))) Q8Lds {
   int bad[4][8];        // keys of a stage's tile that have no page
   float ml[4][2][32];
 };
-// The share of worker w, for heads h0 .. h0 + heads (HEADS at most). FINE: p in two parts.
-template <int NK, int HEADS, bool FINE>
+// The share of worker w, for heads h0 .. h0 + heads (HEADS at most). FINE: p in two parts. PAST: nothing else reads the tiles.
+template <int NK, int HEADS, bool FINE, bool PAST>
 __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* smem, Q8Lds& lds, int w, int h0, int heads, int per,
                                           int total) {
   using C = Q8Cfg<NK, HEADS>;
@@ -255,7 +260,10 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
       if (!asking || (SW == 4 && jj == MAIN && sr > 1)) return;
       const uint32_t off = jj < MAIN ? min(at_copy ^ (turn<NK, WIDE>(jj * SW * C::RPC) * 16), (uint32_t)a.d_c - 16) : at_band;
       const uintptr_t row = (uintptr_t)(uint32_t)row_lo | ((uintptr_t)(uint32_t)row_hi << 32);
-      g2lds16((const char*)row + off, (void*)(uintptr_t)(to + SW * jj * 1024));
+      const char* from = (const char*)row + off;
+      const int at = (int)(to + SW * jj * 1024);
+      if constexpr (PAST) copy_past(from, uniform(at));
+      else g2lds16(from, (void*)(uintptr_t)(uint32_t)at);
       if (jj + 1 < NJ) next_row(jj + 1);
     };
 
@@ -702,7 +710,14 @@ __global__ __launch_bounds__(256, 1) void q8_kernel(PagedArgs a, int head_blocks
   // the head blocks of a worker follow each other on one XCD: its L2 serves all but the first
   const int id = blockIdx.x, hb = id / 8 % head_blocks, w = id / (8 * head_blocks) * 8 + id % 8;
   const int h0 = hb * a.heads_per_wg;
-  q8_shares<NK, HEADS, FINE>(a, smem, lds, w, h0, min(a.heads_per_wg, a.H - h0), uniform(a.sched[0]), uniform(a.sched[1]));
+  const int heads = min(a.heads_per_wg, a.H - h0), per = uniform(a.sched[0]), total = uniform(a.sched[1]);
+  // Copies past the caches (a hint), where no other row of the request and no other head block reads the tiles again. Us of the split
+  // with it and without: 64 rows x up to 8192 keys, 16 heads 46 and 51, 256 x up to 4000, 8 heads 83 and 88, as in a model whose
+  // other layers' caches are read in between; where the same cache of 53 to 167 MB is read call after call, from the last-level
+  // cache, a call takes 42 and 41, 63 and 59. 61 rows, 128 heads: 189 both ways.
+  if constexpr (HEADS <= 16 && NK <= 8)
+    if (uniform(a.sched[4]) == 0 && heads == a.H) return q8_shares<NK, HEADS, FINE, true>(a, smem, lds, w, h0, heads, per, total);
+  q8_shares<NK, HEADS, FINE, false>(a, smem, lds, w, h0, heads, per, total);
 }
 
 template <int NK, bool FINE>
