@@ -442,7 +442,7 @@ LAGA_API laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologu
  *
  * laga_paged_attn_q8: laga_paged_attn on the numbers that the cache stands for. A NaN
  * among the visible ones makes the rows that see it NaN, as would an infinity's product with zero. Statistics, sums and
- * joins are fp32, the products take the queries with 22 bits or more and, in bf16, a probability with 11. */
+ * joins are fp32, the products take the queries and the probabilities with 22 bits or more. */
 LAGA_API laga_status_t laga_cache_append_q8(const laga_paged_t* p, const laga_prologue_t* cfg,
                                             const void* latent_raw, int64_t latent_stride,
                                             const void* gamma, const void* kpe_raw, int64_t kpe_stride,

@@ -243,7 +243,6 @@ inline PagedPlan paged_plan_q8(int H, int d_c) {
 void launch_paged_wide(const PagedArgs& a, int head_blocks, hipStream_t st);
 template <typename T>
 hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t st);
-template <typename T>
 void launch_paged_split_q8(const PagedArgs& a, int head_blocks, hipStream_t st);
 template <typename T>
 hipError_t launch_paged_attn_q8(const PagedArgs& a, hipStream_t st);

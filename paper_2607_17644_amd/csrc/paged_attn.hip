@@ -659,7 +659,7 @@ hipError_t launch_paged_t(const PagedArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   const int hb = (a.H + a.heads_per_wg - 1) / a.heads_per_wg;
   const unsigned wgs = (unsigned)(hb * a.workers);
-  if constexpr (Q8) launch_paged_split_q8<T>(a, hb, st);
+  if constexpr (Q8) launch_paged_split_q8(a, hb, st);
   else if (a.wide) launch_paged_wide(a, hb, st);
   else if (a.d_c <= 128) split_kernel<T, 1><<<wgs, 256, 0, st>>>(a, hb);
   else if (a.d_c <= 256) split_kernel<T, 2><<<wgs, 256, 0, st>>>(a, hb);

@@ -113,8 +113,9 @@ __host__ __device__ constexpr int band_turn(int r) {
 }
 
 // A probability's reference m, a whole number, is raised only where a score passes it by kRise, and p goes into the
-// product as p 2^(c_j + d + kLift), d such that no p 2^(c_j + d) passes 2^kRise: 2^14 at most, with 11 bits down to 2^-28 of
-// that.
+// product as p 2^(c_j + d + kLift), d such that no p 2^(c_j + d) passes 2^kRise: 2^14 at most. As two fp16 parts, 22 bits of
+// it or 2^-25: one part alone, 11 bits, left 5 to 11 % of the outputs in bf16 a rounding off the nearest (0.1 % now), at 9 % less
+// time with 128 heads (205 us of 61 x up to 8192 keys, now 223), the same with 16 (60.0, 60.6).
 constexpr float kRise = 8.f;
 constexpr int kLift = 6;
 
@@ -146,8 +147,9 @@ struct __attribute__((aligned(16))) Q8Lds {
   int bad[4][8];        // keys of a stage's tile that have no page
   float ml[4][2][32];
 };
-// The share of worker w, for heads h0 .. h0 + heads (HEADS at most). FINE: p in two parts. PAST: nothing else reads the tiles.
-template <int NK, int HEADS, bool FINE, bool PAST>
+// The share of worker w, for heads h0 .. h0 + heads (HEADS at most). FULL: d_c = 64 NK and d_rope = 64. PAST: nothing else reads
+// the tiles.
+template <int NK, int HEADS, bool FULL, bool PAST>
 __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* smem, Q8Lds& lds, int w, int h0, int heads, int per,
                                           int total) {
   using C = Q8Cfg<NK, HEADS>;
@@ -157,7 +159,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
   const int l = threadIdx.x & 63, n = l % GH, g = l / GH;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kw = wave / SW, sr = wave % SW, hg = sr % C::HG, cs = sr / C::HG;
-  const int W = a.d_c + a.d_rope;
+  const int d_c = FULL ? 64 * NK : a.d_c, d_rope = FULL ? 64 : a.d_rope, W = d_c + d_rope;
   const int64_t start = (int64_t)w * per;
   if (start >= total) return;
   const int end = (int)min((int64_t)total, start + per);
@@ -194,7 +196,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
     at_src = sr * C::RPC + l / CH;
     at_copy = (l % CH ^ turn<NK, WIDE>(at_src)) * 16;
     at_key_src = (sr & 1) * 16 + (l >> 2);
-    at_band = a.d_c + min(((l & 3) ^ band_turn<WIDE>(at_key_src)) * 16, a.d_rope - 16);
+    at_band = d_c + min(((l & 3) ^ band_turn<WIDE>(at_key_src)) * 16, d_rope - 16);
   }
 
   for (int at = max((int)start, share.first);;) {
@@ -258,7 +260,8 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
     };
     auto copy = [&](int jj) {
       if (!asking || (SW == 4 && jj == MAIN && sr > 1)) return;
-      const uint32_t off = jj < MAIN ? min(at_copy ^ (turn<NK, WIDE>(jj * SW * C::RPC) * 16), (uint32_t)a.d_c - 16) : at_band;
+      const uint32_t chunk = at_copy ^ (turn<NK, WIDE>(jj * SW * C::RPC) * 16);
+      const uint32_t off = jj < MAIN ? (FULL ? chunk : min(chunk, (uint32_t)d_c - 16)) : at_band;
       const uintptr_t row = (uintptr_t)(uint32_t)row_lo | ((uintptr_t)(uint32_t)row_hi << 32);
       const char* from = (const char*)row + off;
       const int at = (int)(to + SW * jj * 1024);
@@ -285,11 +288,11 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
     float mult = 0.f;  // of a score in base 2
     if (steps > 0) {
       const int64_t th = (int64_t)t * a.H + h0 + min(GH * hg + n, heads - 1);
-      const int blocks = qa_blocks(a.d_c);
+      const int blocks = qa_blocks(d_c);
       const float* tops = a.qa_max + th * blocks;
       const f32x4* q = (const f32x4*)a.qa + (int64_t)t * (W / 4) * a.H + (th - (int64_t)t * a.H);
       auto at = [&](int i, int u) { return (WIDE ? 32 * (i < NK ? NK * cs + i : cs) : i < NK ? 64 * i : 0) + 16 * g + 8 * u; };
-      auto there = [&](int i, int u) { return at(i, u) < (i < NK ? a.d_c : a.d_rope); };
+      auto there = [&](int i, int u) { return FULL || at(i, u) < (i < NK ? d_c : d_rope); };
       constexpr int TURN = 9;  // steps whose numbers are on their way at once
       f32x4 x[TURN][2][2];
       auto read = [&](int i0) {
@@ -297,7 +300,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
         for (int i = i0; i < min(i0 + TURN, NK + 1); ++i)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const f32x4* from = q + (((i < NK ? 0 : a.d_c) + (there(i, u) ? at(i, u) : 0)) >> 2) * a.H;
+            const f32x4* from = q + (((i < NK ? 0 : d_c) + (there(i, u) ? at(i, u) : 0)) >> 2) * a.H;
             x[i - i0][u][0] = from[0];
             x[i - i0][u][1] = from[a.H];
           }
@@ -410,11 +413,9 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = x[first + e];
       hi = __builtin_convertvector(y, f16x8);
-      if constexpr (FINE) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] -= (float)hi[e];
-        lo = __builtin_convertvector(y, f16x8);
-      }
+      for (int e = 0; e < 8; ++e) y[e] -= (float)hi[e];
+      lo = __builtin_convertvector(y, f16x8);
     };
     // The keys' powers (byte 0: 2^-127; 255: NaN), by way of LDS to the lanes that need them
     auto give_powers = [&](int exps) {
@@ -518,7 +519,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
             widen4(v[i + 1 & 1], 0, vr[(i + 1) % AHEAD][0]);
             widen4(v[i + 1 & 1], 4, vr[(i + 1) % AHEAD][1]);
           }
-          if constexpr (FINE) mma(oacc[i], v[i & 1], pl);
+          mma(oacc[i], v[i & 1], pl);
           __builtin_amdgcn_sched_barrier(0);
         };
 #pragma unroll
@@ -618,7 +619,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
             widen4(v[i + 1 & 1], 0, vr[(i + 1) % AHEAD][0]);
             widen4(v[i + 1 & 1], 4, vr[(i + 1) % AHEAD][1]);
           }
-          if constexpr (FINE) mma(oacc[i % NB], v[i & 1], pl[i / NB]);
+          mma(oacc[i % NB], v[i & 1], pl[i / NB]);
           __builtin_amdgcn_sched_barrier(0);
         }
         if (s + 1 < steps) {
@@ -646,7 +647,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
     const bool whole = it0 == 0 && it1 == row_end - row_first;
     const int h = h0 + GH * hg + n;
     const int64_t place_of = whole ? (int64_t)t * a.H + h : (int64_t)partial_place(w, per, row_first) * a.H + h;
-    float* o = (whole ? a.obar : a.part_o) + place_of * a.d_c + 4 * g;
+    float* o = (whole ? a.obar : a.part_o) + place_of * d_c + 4 * g;
     auto column_of = [&](int j) { return WIDE ? 32 * (NB * cs + (j >> 2)) + 8 * (j & 3) : 16 * (NB * cs + j); };
     if (KW > 1 && it1 - it0 > 1) {
       // the waves' sums under their common maximum (a lone tile is the first wave's: 1000 keys, 16 heads 11.9 us, 14.6 by this way)
@@ -675,7 +676,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
 #pragma unroll
         for (int i = 0; i < C::kO / KW; ++i) {
           const int j = KW * i + kw;
-          if (column_of(j) >= a.d_c) continue;
+          if (!FULL && column_of(j) >= d_c) continue;
           f32x4 y = sums[(sr * C::kO + j) * 64 + l];
 #pragma unroll
           for (int u = 1; u < KW; ++u) y += sums[((u * SW + sr) * C::kO + j) * 64 + l];
@@ -686,7 +687,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
       const float f = __builtin_ldexpf(whole ? 1.f / ltot : 1.f, lower);
 #pragma unroll
       for (int j = 0; j < C::kO; ++j)
-        if (column_of(j) < a.d_c) *reinterpret_cast<f32x4*>(o + column_of(j)) = quad_of(j) * f;
+        if (FULL || column_of(j) < d_c) *reinterpret_cast<f32x4*>(o + column_of(j)) = quad_of(j) * f;
     }
     if (kw == 0 && cs == 0 && g == 0 && GH * hg + n < heads) {
       if (!whole) {
@@ -703,7 +704,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
   }
 }
 
-template <int NK, int HEADS, bool FINE>
+template <int NK, int HEADS, bool FULL>
 __global__ __launch_bounds__(256, 1) void q8_kernel(PagedArgs a, int head_blocks) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[Q8Cfg<NK, HEADS>::LDS];
   __shared__ Q8Lds lds;
@@ -716,31 +717,34 @@ __global__ __launch_bounds__(256, 1) void q8_kernel(PagedArgs a, int head_blocks
   // other layers' caches are read in between; where the same cache of 53 to 167 MB is read call after call, from the last-level
   // cache, a call takes 42 and 41, 63 and 59. 61 rows, 128 heads: 189 both ways.
   if constexpr (HEADS <= 16 && NK <= 8)
-    if (uniform(a.sched[4]) == 0 && heads == a.H) return q8_shares<NK, HEADS, FINE, true>(a, smem, lds, w, h0, heads, per, total);
-  q8_shares<NK, HEADS, FINE, false>(a, smem, lds, w, h0, heads, per, total);
+    if (uniform(a.sched[4]) == 0 && heads == a.H) return q8_shares<NK, HEADS, FULL, true>(a, smem, lds, w, h0, heads, per, total);
+  q8_shares<NK, HEADS, FULL, false>(a, smem, lds, w, h0, heads, per, total);
 }
 
-template <int NK, bool FINE>
+template <int NK, bool FULL>
 void launch_q8(const PagedArgs& a, int head_blocks, hipStream_t st) {
   const unsigned wgs = (unsigned)(head_blocks * a.workers);
-  if (a.heads_per_wg <= 16) q8_kernel<NK, 16, FINE><<<wgs, 256, 0, st>>>(a, head_blocks);
+  if (a.heads_per_wg <= 16) q8_kernel<NK, 16, FULL><<<wgs, 256, 0, st>>>(a, head_blocks);
   else if constexpr (NK <= 8) {
-    if (a.heads_per_wg <= 32) q8_kernel<NK, 32, FINE><<<wgs, 256, 0, st>>>(a, head_blocks);
-    else q8_kernel<NK, 64, FINE><<<wgs, 256, 0, st>>>(a, head_blocks);
+    if (a.heads_per_wg <= 32) q8_kernel<NK, 32, FULL><<<wgs, 256, 0, st>>>(a, head_blocks);
+    else q8_kernel<NK, 64, FULL><<<wgs, 256, 0, st>>>(a, head_blocks);
   }
+}
+// Widths that fill the steps need no care at a row's end. Us of a call with it and without: 1 x 1000 keys, 16 heads 20.9 and 22.2; 64 x
+// up to 8192, 16 heads 59.0 and 60.6; 256 x up to 4000, 8 heads 95.9 and 98.4; with 128 heads no difference.
+template <int NK>
+void launch_q8(const PagedArgs& a, int head_blocks, hipStream_t st) {
+  if (a.d_c == 64 * NK && a.d_rope == 64) launch_q8<NK, true>(a, head_blocks, st);
+  else launch_q8<NK, false>(a, head_blocks, st);
 }
 
 }  // namespace
 
-template <typename T>
 void launch_paged_split_q8(const PagedArgs& a, int head_blocks, hipStream_t st) {
-  constexpr bool FINE = sizeof(T) == 4;
-  if (a.d_c <= 128) launch_q8<2, FINE>(a, head_blocks, st);
-  else if (a.d_c <= 256) launch_q8<4, FINE>(a, head_blocks, st);
-  else if (a.d_c <= 512) launch_q8<8, FINE>(a, head_blocks, st);
-  else launch_q8<16, FINE>(a, head_blocks, st);
+  if (a.d_c <= 128) launch_q8<2>(a, head_blocks, st);
+  else if (a.d_c <= 256) launch_q8<4>(a, head_blocks, st);
+  else if (a.d_c <= 512) launch_q8<8>(a, head_blocks, st);
+  else launch_q8<16>(a, head_blocks, st);
 }
-template void launch_paged_split_q8<bf16>(const PagedArgs&, int, hipStream_t);
-template void launch_paged_split_q8<float>(const PagedArgs&, int, hipStream_t);
 
 }  // namespace laga
