@@ -142,7 +142,7 @@ __device__ __forceinline__ void copy_past(const void* g, uint32_t to) {
 
 template <int N> struct Count { static constexpr int n = N; };
 struct __attribute__((aligned(16))) Q8Lds {
-  float powers[4][64];  // of a tile's keys, 2^c and then 2^k, for each wave
+  int32_t powers[4][64];  // of a tile's keys, c and then k, for each wave
   int32_t ids[4][kIds];
   int bad[4][8];        // keys of a stage's tile that have no page
   float ml[4][2][32];
@@ -285,7 +285,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
     // The queries of head n, scaled by 2^-e to 1 .. 2 at most: of step i and half u elements 64 i + 16 g + 8 u .., or of this
     // wave's half 32 i + 16 g + 8 u ... They are read first, and widened while the first tiles are on their way.
     f16x8 qh[NK + 1][2], ql[NK + 1][2];
-    float mult = 0.f;  // of a score in base 2
+    int e = 0;
     if (steps > 0) {
       const int64_t th = (int64_t)t * a.H + h0 + min(GH * hg + n, heads - 1);
       const int blocks = qa_blocks(d_c);
@@ -319,9 +319,8 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
         for (int jj = 0; jj < NJ; ++jj) copy(jj);
       }
       asking = false;
-      const int e = top > 0.f ? max(__builtin_amdgcn_frexp_expf(top) - 1, -126) : 0;
+      e = top > 0.f ? max(__builtin_amdgcn_frexp_expf(top) - 1, -126) : 0;
       const float down = __builtin_ldexpf(1.f, -e);
-      mult = __builtin_ldexpf(a.scale_log2, e);
 #pragma unroll
       for (int i0 = 0; i0 <= NK; i0 += TURN) {
         if (i0 > 0) read(i0);
@@ -352,8 +351,10 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
     int st = 0;
     uint32_t tile = ring;
     constexpr int NZ = WIDE ? 16 : 8;  // scores of a lane
-    f32x4 fc[NZ / 4];                  // 2^c of their keys
+    i32x4 pc[NZ / 4];                  // c of their keys
     float z[NZ], p[NZ], x[NZ];
+    // 2^(c + e) A + 2^(k + e) B: the powers added up first, so that nothing passes fp32's range but a score that does
+    auto score = [&](float A, int c, float B, int k) { return __builtin_ldexpf(A, c + e) + __builtin_ldexpf(B, k + e); };
     // this lane's r-th score is of key
     auto key_of = [&](int r) { return (WIDE ? 8 : 16) * (r >> 2) + 4 * g + (r & 3); };
     // Scores of tile s into p and what goes into the product, x, under the reference, which is raised where need be.
@@ -364,27 +365,27 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
         for (int r = 0; r < NZ; ++r) z[r] = key_of(r) < lim ? (bad >> key_of(r) & 1 ? NAN : z[r]) : -INFINITY;
       }
       float most_t = -INFINITY, most_x = 0.f;
-      auto under = [&](float m_use, float f) {
+      auto under = [&](float m_use, int lift) {
 #pragma unroll
         for (int r = 0; r < NZ; ++r) {
-          const float t = __builtin_fmaf(z[r], mult, -m_use);
+          const float t = __builtin_fmaf(z[r], a.scale_log2, -m_use);
           most_t = fmaxf(most_t, t);
           p[r] = fast_exp2(t);
-          x[r] = p[r] * f * fc[r >> 2][r & 3];
+          x[r] = __builtin_ldexpf(p[r], pc[r >> 2][r & 3] + lift);
           most_x = fmaxf(most_x, x[r]);
         }
       };
-      under(m == -INFINITY ? 0.f : m, __builtin_ldexpf(1.f, d + kLift));
+      under(m == -INFINITY ? 0.f : m, d + kLift);
       if (__ballot(most_t > rise || most_x > 0x1p14f)) {
         // m to the whole number at or above every score, and d so that the largest p 2^(c_j + d) is 1 at most
         float top = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < NZ; ++r) top = fmaxf(top, z[r] * mult);
+        for (int r = 0; r < NZ; ++r) top = fmaxf(top, z[r] * a.scale_log2);
         const float m_new = fmaxf(m, ceilf(head_max<WIDE>(top))), m_use = m_new == -INFINITY ? 0.f : m_new;
         float lift = -1e5f;
 #pragma unroll
         for (int r = 0; r < NZ; ++r)
-          lift = fmaxf(lift, __builtin_fmaf(z[r], mult, -m_use) + (float)__builtin_amdgcn_frexp_expf(fc[r >> 2][r & 3]));
+          lift = fmaxf(lift, __builtin_fmaf(z[r], a.scale_log2, -m_use) + (float)(pc[r >> 2][r & 3] + 1));
         int ref = (int)ceilf(fminf(head_max<WIDE>(lift), 1e5f));
         const int fell = m == -INFINITY ? -100000 : (int)fmaxf(m - m_use, -1e5f);
         if (m != -INFINITY) {
@@ -401,7 +402,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
         d = -ref;
         m = m_new;
         rise = m == -INFINITY ? -INFINITY : kRise;
-        under(m_use, __builtin_ldexpf(1.f, d + kLift));
+        under(m_use, d + kLift);
       }
 #pragma unroll
       for (int r = 0; r < NZ; r += 4) lsum += (p[r] + p[r + 1]) + (p[r + 2] + p[r + 3]);
@@ -417,14 +418,16 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
       for (int e = 0; e < 8; ++e) y[e] -= (float)hi[e];
       lo = __builtin_convertvector(y, f16x8);
     };
-    // The keys' powers (byte 0: 2^-127; 255: NaN), by way of LDS to the lanes that need them
+    // The keys' powers, by way of LDS to the lanes that need them; of which one is NaN (byte 255)
     auto give_powers = [&](int exps) {
       const int b = l < 32 ? exps & 255 : exps >> 8 & 255;
-      lds.powers[wave][l] = __builtin_bit_cast(float, b << 23 | ((b + 1 & 254) == 0 ? 1 << 22 : 0));
+      lds.powers[wave][l] = b - kScaleBias;
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
+      const uint64_t nan = __ballot(b == 255);
+      return (int)((uint32_t)nan | (uint32_t)(nan >> 32));
     };
-    auto powers = [&](int of, int r) { return *reinterpret_cast<const f32x4*>(&lds.powers[wave][32 * of + key_of(r)]); };
+    auto powers = [&](int of, int r) { return *reinterpret_cast<const i32x4*>(&lds.powers[wave][32 * of + key_of(r)]); };
     auto raw_at = [&](uint32_t at) { return *(__attribute__((address_space(3))) const i32x4*)(uintptr_t)at; };
     auto columns_at = [&](uint32_t at) { return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(uintptr_t)at); };
     constexpr int PER = (NJ + NK) / (NK + 1);  // copies beside a step
@@ -462,9 +465,10 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
       for (int s = 0; s < steps; ++s) {
         // Scores, step by step: beside the eight products of one step the next one's numbers are widened, later ones'
         // read, and now and then a copy is asked for.
-        const int bad = uniform(bads);
+        int bad = uniform(bads);
         ask(s);
-        f32x4 sc[2], sk[2], fk[2];
+        f32x4 sc[2], sk[2];
+        i32x4 pk[2];
         f16x8 k[2][2][2];
 #pragma unroll
         for (int j = 0; j < 8; ++j) widen4(k[0][j >> 2][j >> 1 & 1], 4 * (j & 1), raw[0][j >> 2][j & 3]);
@@ -476,10 +480,10 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
 #pragma unroll
             for (int b = 0; b < 2; ++b) raw[i % RA][b] = k_read(i + RA, b);
           if (i == 0) {
-            give_powers(exps);
+            bad |= give_powers(exps);
           } else if (i == 1) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) fc[b] = powers(0, 4 * b), fk[b] = powers(1, 4 * b);
+            for (int b = 0; b < 2; ++b) pc[b] = powers(0, 4 * b), pk[b] = powers(1, 4 * b);
           }
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -505,7 +509,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
         for (int i = 0; i < AHEAD; ++i) vr[i] = v_read(i);
         scores_done(sc, sk);
 #pragma unroll
-        for (int r = 0; r < 8; ++r) z[r] = __builtin_fmaf(sk[r >> 2][r & 3], fk[r >> 2][r & 3], sc[r >> 2][r & 3] * fc[r >> 2][r & 3]);
+        for (int r = 0; r < 8; ++r) z[r] = score(sc[r >> 2][r & 3], pc[r >> 2][r & 3], sk[r >> 2][r & 3], pk[r >> 2][r & 3]);
         weigh(s, bad);
         f16x8 ph, pl, v[2];
         operand(0, ph, pl);
@@ -549,7 +553,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
       // This wave's half of a tile's scores to z and to the other wave, as above.
       auto scores = [&](int turn_of) {
         f32x16 sc, sk;
-        f32x4 fk[4];
+        i32x4 pk[4];
         f16x8 k[2][2];
 #pragma unroll
         for (int j = 0; j < 4; ++j) widen4(k[0][j >> 1], 4 * (j & 1), raw[0][j]);
@@ -559,10 +563,10 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
           f32x16& acc = i < NK ? sc : sk;
           if (i + RA <= NK) raw[i % RA] = k_read(i + RA);
           if (i == 0) {
-            give_powers(exps);
+            bads |= give_powers(exps);
           } else if (i == 1) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) fc[r] = powers(0, 4 * r), fk[r] = powers(1, 4 * r);
+            for (int r = 0; r < 4; ++r) pc[r] = powers(0, 4 * r), pk[r] = powers(1, 4 * r);
           }
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -580,7 +584,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
         }
         scores_done(sc, sk);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) z[r] = __builtin_fmaf(sk[r], fk[r >> 2][r & 3], sc[r] * fc[r >> 2][r & 3]);
+        for (int r = 0; r < 16; ++r) z[r] = score(sc[r], pc[r >> 2][r & 3], sk[r], pk[r >> 2][r & 3]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) parts[((turn_of * 4 + wave) * 4 + r) * 64 + l] = f32x4{z[4 * r], z[4 * r + 1], z[4 * r + 2], z[4 * r + 3]};
       };
