@@ -442,7 +442,9 @@ LAGA_API laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologu
  *
  * laga_paged_attn_q8: laga_paged_attn on the numbers that the cache stands for. A NaN
  * among the visible ones makes the rows that see it NaN, as would an infinity's product with zero. Statistics, sums and
- * joins are fp32, the products take the queries and the probabilities with 22 bits or more. */
+ * joins are fp32, the products take a query's number with 22 bits down to 2^-17 of its
+ * part's largest (q_rope, or q_nope times W_k) and within 2^-39 of that below, and a probability times its key's
+ * power with 22 bits or within 2^-29 of the largest so far. */
 LAGA_API laga_status_t laga_cache_append_q8(const laga_paged_t* p, const laga_prologue_t* cfg,
                                             const void* latent_raw, int64_t latent_stride,
                                             const void* gamma, const void* kpe_raw, int64_t kpe_stride,

@@ -2,10 +2,11 @@
 // for the shared key of each position. (paged_attn.hip has the call's other launches.)
 //
 // The products run on fp16 operands, 16x16x32 at a time: an e4m3 number is an fp16 number, and two fp16 parts of a
-// query value, the row scaled to at most 2, hold 22 bits of it or 2^-25 of the row's largest (three bf16 parts would
-// hold 24, for half as many products again). With key j's powers 2^c_j and 2^k_j
+// query value, its part of the row (qa or the band) scaled by 2^-e or 2^-f to 2^15 at most, hold 22 bits of it down to 2^-17 of the
+// part's largest and 2^-39 of that below (three bf16 parts would hold 24, for half as many products again). With key j's
+// powers 2^c_j and 2^k_j
 //
-//   z_j = scale 2^e (2^c_j A_j + 2^k_j B_j),  A = qa . c8,  B = q_rope . k8,  O += (p_j 2^(c_j + d)) c8_j
+//   z_j = scale (2^(c_j + e) A_j + 2^(k_j + f) B_j),  A = 2^-e qa . c8,  B = 2^-f q_rope . k8,  O += (p_j 2^(c_j + d)) c8_j
 //
 // so the powers never meet a number of 8 bits. A lone wave per SIMD (its registers hold a head group's queries and sums) issues
 // an instruction in 4 to 5 cycles, a 16 x 16 product takes the matrix unit 16 and a 32 x 32 one 32: two numbers' conversions
@@ -282,10 +283,10 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
       if constexpr (SW > 1) lds_barrier();  // every wave's copies (and partial scores)
       else asm volatile("" ::: "memory");   // (nothing is read before)
     };
-    // The queries of head n, scaled by 2^-e to 1 .. 2 at most: of step i and half u elements 64 i + 16 g + 8 u .., or of this
-    // wave's half 32 i + 16 g + 8 u ... They are read first, and widened while the first tiles are on their way.
+    // The queries of head n, each part scaled by 2^-e of its own to 2^14 .. 2^15 at most: of step i and half u elements 64 i + 16 g
+    // + 8 u .., or of this wave's half 32 i + 16 g + 8 u ... They are read first, and widened while the first tiles are on their way.
     f16x8 qh[NK + 1][2], ql[NK + 1][2];
-    int e = 0;
+    int ec = 0, ek = 0;
     if (steps > 0) {
       const int64_t th = (int64_t)t * a.H + h0 + min(GH * hg + n, heads - 1);
       const int blocks = qa_blocks(d_c);
@@ -306,7 +307,8 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
           }
       };
       float top = 0.f;
-      for (int i = 0; i < blocks; ++i) top = fmaxf(top, tops[i]);
+      for (int i = 0; i < blocks - 1; ++i) top = fmaxf(top, tops[i]);
+      const float band_top = tops[blocks - 1];
       read(0);
       look(tile_of(0));
       wait_vmem();
@@ -319,8 +321,8 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
         for (int jj = 0; jj < NJ; ++jj) copy(jj);
       }
       asking = false;
-      e = top > 0.f ? max(__builtin_amdgcn_frexp_expf(top) - 1, -126) : 0;
-      const float down = __builtin_ldexpf(1.f, -e);
+      ec = top > 0.f ? __builtin_amdgcn_frexp_expf(top) - 15 : 0;
+      ek = band_top > 0.f ? __builtin_amdgcn_frexp_expf(band_top) - 15 : 0;
 #pragma unroll
       for (int i0 = 0; i0 <= NK; i0 += TURN) {
         if (i0 > 0) read(i0);
@@ -330,10 +332,10 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             typedef float f32x8 __attribute__((ext_vector_type(8)));
-            const float f = there(i, u) ? down : 0.f;
+            const int up = there(i, u) ? -(i < NK ? ec : ek) : -1000;  // (to zero)
             f32x8 y, rest;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] = x[i - i0][u][k >> 2][k & 3] * f;
+            for (int k = 0; k < 8; ++k) y[k] = __builtin_ldexpf(x[i - i0][u][k >> 2][k & 3], up);
             qh[i][u] = __builtin_convertvector(y, f16x8);
 #pragma unroll
             for (int k = 0; k < 8; ++k) rest[k] = y[k] - (float)qh[i][u][k];
@@ -353,8 +355,8 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
     constexpr int NZ = WIDE ? 16 : 8;  // scores of a lane
     i32x4 pc[NZ / 4];                  // c of their keys
     float z[NZ], p[NZ], x[NZ];
-    // 2^(c + e) A + 2^(k + e) B: the powers added up first, so that nothing passes fp32's range but a score that does
-    auto score = [&](float A, int c, float B, int k) { return __builtin_ldexpf(A, c + e) + __builtin_ldexpf(B, k + e); };
+    // The powers are added up first, so that nothing passes fp32's range but a score that does
+    auto score = [&](float A, int c, float B, int k) { return __builtin_ldexpf(A, c + ec) + __builtin_ldexpf(B, k + ek); };
     // this lane's r-th score is of key
     auto key_of = [&](int r) { return (WIDE ? 8 : 16) * (r >> 2) + 4 * g + (r & 3); };
     // Scores of tile s into p and what goes into the product, x, under the reference, which is raised where need be.

@@ -5,7 +5,7 @@ import dataclasses
 import pytest
 import torch
 
-from test_gpu_paged_q8 import call, make
+from test_gpu_paged_q8 import call, check, eight, make
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +48,28 @@ def test_the_largest_latents(heads, dtype, d_c):
 def test_small_numbers_under_large_queries(heads, dtype):
     x = make([300, 31, 70], 16, heads=heads, dtype=dtype, seed=heads)
     same(call(x), call(moved(x, q_nope=50, q_rope=50, latent=-70, key=-70, scale=20)), -70)
+
+
+@pytest.mark.parametrize("heads,dtype", FORMS)
+@pytest.mark.parametrize("power", [12, -12, 50, -80])
+def test_the_query_s_two_parts_have_sizes_of_their_own(heads, dtype, power):
+    x = make([300, 31, 70], 16, heads=heads, dtype=dtype, seed=heads)
+    y = moved(x, q_rope=power, key=-power)
+    same(check(x, base=10000.0) if heads < 64 else call(x, base=10000.0), call(y, base=10000.0))
+
+
+@pytest.mark.parametrize("widths,d_c,heads,dtype", [("v3", 512, 4, "bf16"), ("v3", 512, 20, "bf16"), ("v3", 512, 40, "fp32"), ("v3", 1024, 3, "fp32"),
+                                                    ("half", 416, 24, "bf16"), ("small", 64, 4, "fp32")])
+@pytest.mark.parametrize("power", [6, 12])
+def test_columns_of_many_sizes(widths, d_c, heads, dtype, power):
+    """Every second number of the latents smaller by 2^power, and what the query has for it larger: their products count alike."""
+    x = make([200, 31, 70], 16, widths, d_c, heads, dtype, seed=d_c)
+    p = x["p"]
+    v = x["cache"].float()
+    v[..., :d_c] *= torch.exp2(x["scales"][..., :1].float() - 127)
+    v[..., d_c:] *= torch.exp2(x["scales"][..., 1:].float() - 127)
+    v[..., :d_c:2] *= 2.0 ** -power
+    cache, scales = eight(v, d_c)
+    w = x["w"].clone().view(d_c, heads, p.d_nope + p.d_v)
+    w[::2, :, :p.d_nope] *= 2.0 ** power
+    check(dict(x, cache=cache, scales=scales, w=w.view(d_c, -1)))
