@@ -595,7 +595,6 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
         k_first();
         asking = false;
         scores(0);
-        if (NS < steps) look(tile_of(NS));
         landed(1, Count<NS - 2>{});
       }
       // Step s: tile s's weights and O, then the scores of the tile after it, whose copies have landed.
