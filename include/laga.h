@@ -435,8 +435,9 @@ LAGA_API laga_status_t laga_paged_attn(const laga_paged_t* p, const laga_prologu
  * laga_cache_read_q8: cached positions back as numbers, row t the position[t] of request
  * row_request[t] (NULL: of request t):
  *   c_kv [rows, d_c], k_pe [rows, d_rope]  element dtype
- * for instance all of a request's before the next chunk of its prompt goes through
- * laga_reconstruct_kv and laga_attn_fwd. Exact in both element types (in bf16 and fp32 an e4m3
+ * to export or inspect a request, to write it to a cache in other bits, or to compute over its whole
+ * sequence again (laga_reconstruct_kv, laga_attn_fwd: as many queries as keys). A chunk of a prompt over
+ * its cached prefix goes through laga_paged_attn_q8, a row per new token. Exact in both element types (in bf16 and fp32 an e4m3
  * number times a power of two that the append writes has all its bits). A row at a negative position is 0; one
  * outside the table, or whose page lies outside the pool, NaN.
  *
