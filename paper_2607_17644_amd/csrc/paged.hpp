@@ -222,13 +222,13 @@ inline PagedPlan paged_plan(int H, int d_c, int d_rope, int elem_size) {
 }
 
 // A cache in 8 bits: units of a row as above, up to 16 heads per workgroup, whose shares begin with three to eight tiles for each wave
-// and end with the waves' sums in LDS, and beyond. Us of the split with 14 and 5, with 6 and 3, with 20 and 8: 64 x up to
-// 8192 keys, 16 heads 51, 55, 53; 256 x up to 4000, 8 heads 88, 91, 90; 61 x up to 8192, 128 heads 187, 192, 189; 99 x up to
-// 3001, 24 heads 34, 35, 33 (through the caches, all).
+// and end with the waves' sums in LDS, and beyond. Us of a call with 14 and 5, with 6 and 3, with 20 and 8: 64 x up to
+// 8192 keys, 16 heads 59.4, 63.8, 61.5; 256 x up to 4000, 8 heads 96.9, 100.5, 99.7; 61 x up to 8192, 128 heads 227, 227, 231; 99 x
+// up to 3001, 24 heads 73.9, 74.5, 72.1.
 constexpr int kQ8RowCost = 14, kQ8WideRowCost = 5;
 // Up to 64 heads per workgroup, in products of 32 x 32 above 16: a tile is copied once for them, and its numbers are widened for 32
-// heads at once. With 16 for each of more workgroups 61 x up to 8192 keys, 128 heads took 233 us (now 184), 2 x up to 100000
-// 115 (99); 99 x up to 3001 keys, 24 heads 34 (34). Above d_c = 512 the queries and sums of 16 heads are all that
+// heads at once. With 16 for each of more workgroups a call of 61 x up to 8192 keys, 128 heads took 258 us (now 227), 2 x up to 100000
+// 130 (124); 99 x up to 3001 keys, 24 heads 74 (74). Above d_c = 512 the queries and sums of 16 heads are all that
 // a workgroup's registers hold.
 inline PagedPlan paged_plan_q8(int H, int d_c) {
   PagedPlan p{};

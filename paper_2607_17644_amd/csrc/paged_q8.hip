@@ -10,14 +10,15 @@
 //
 // so the powers never meet a number of 8 bits. A lone wave per SIMD (its registers hold a head group's queries and sums) issues
 // an instruction in 4 to 5 cycles, a 16 x 16 product takes the matrix unit 16 and a 32 x 32 one 32: two numbers' conversions
-// beside each 16 x 16 product of the scores hide behind it, O's four do not.
+// beside each 16 x 16 product of the scores hide behind it, and O's four behind its pairs of products.
 //
-// Measured (d_c = 512, d_rope = 64, 578 bytes a key): 64 requests of up to 8192 keys, 16 heads, 46 us, 167 MB at 3.6 TB/s over
-// the launch and 4.6 to 5.1 within a share: bound by memory there, by the shares' starts and ends else (77 us from a
-// cache in bf16). 61 requests, 128 heads: 184 us, 2 requests of up to 100000 keys 99 (169 and 89 in bf16): a step
-// of 32 keys and 64 heads takes 5000 cycles, 1660 of them products; an instruction is issued in 51 % of the cycles, 136
-// conversions per wave among them. Tried there and slower: four waves to 32 heads (240 us), scores beside the products
-// of O (200; its registers are moved about), no gain from fewer exponentials or conflicts (there are none).
+// Measured (d_c = 512, d_rope = 64, 578 bytes a key): 64 requests of up to 8192 keys, 16 heads, 47 us, 167 MB at 3.6 TB/s over
+// the launch: bound by memory within a share, by the shares' starts and ends else (77 us from a
+// cache in bf16). 61 requests, 128 heads: 218 us, 2 requests of up to 100000 keys 113 (169 and 89 in bf16): a step
+// of 32 keys and 64 heads takes about 5700 cycles, 2180 of them products; an instruction is issued in 51 % of the cycles, 136
+// conversions per wave among them. Tried there and slower, when p was one part and the split took 184 us: four waves to 32
+// heads (240), scores beside the products of O (200; its registers are moved about), no gain from fewer exponentials or
+// conflicts (there are none). (What a first part leaves, by one mixed fma in place of a conversion and a difference: 0.3 % of a call.)
 #define LAGA_LDS_DMA_ASM 1
 #include <type_traits>
 
@@ -655,7 +656,7 @@ __device__ __forceinline__ void q8_shares(const PagedArgs& a, unsigned char* sme
     float* o = (whole ? a.obar : a.part_o) + place_of * d_c + 4 * g;
     auto column_of = [&](int j) { return WIDE ? 32 * (NB * cs + (j >> 2)) + 8 * (j & 3) : 16 * (NB * cs + j); };
     if (KW > 1 && it1 - it0 > 1) {
-      // the waves' sums under their common maximum (a lone tile is the first wave's: 1000 keys, 16 heads 11.9 us, 14.6 by this way)
+      // the waves' sums under their common maximum (a lone tile is the first wave's: 2.7 us less for 1000 keys, 16 heads, 10.9 now)
       f32x4* sums = (f32x4*)smem;
       lds_barrier();  // every tile is read
       if (g == 0) lds.ml[wave][0][n] = m, lds.ml[wave][1][n] = ltot;
@@ -717,10 +718,10 @@ __global__ __launch_bounds__(256, 1) void q8_kernel(PagedArgs a, int head_blocks
   const int id = blockIdx.x, hb = id / 8 % head_blocks, w = id / (8 * head_blocks) * 8 + id % 8;
   const int h0 = hb * a.heads_per_wg;
   const int heads = min(a.heads_per_wg, a.H - h0), per = uniform(a.sched[0]), total = uniform(a.sched[1]);
-  // Copies past the caches (a hint), where no other row of the request and no other head block reads the tiles again. Us of the split
-  // with it and without: 64 rows x up to 8192 keys, 16 heads 46 and 51, 256 x up to 4000, 8 heads 83 and 88, as in a model whose
-  // other layers' caches are read in between; where the same cache of 53 to 167 MB is read call after call, from the last-level
-  // cache, a call takes 42 and 41, 63 and 59. 61 rows, 128 heads: 189 both ways.
+  // Copies past the caches (a hint), where no other row of the request and no other head block reads the tiles again. Us of a call
+  // with it and without: 64 rows x up to 8192 keys, 16 heads 59 and 65, 256 x up to 4000, 8 heads 97 and 104, as in a model whose
+  // other layers' caches are read in between; where the same cache is read call after call, from the last-level
+  // cache, 41 and 39.5 (53 MB, 16 heads), 60 and 58 (106 MB, 8 heads), 60.3 and 57.4 (167 MB, 16 heads).
   if constexpr (HEADS <= 16 && NK <= 8)
     if (uniform(a.sched[4]) == 0 && heads == a.H) return q8_shares<NK, HEADS, FULL, true>(a, smem, lds, w, h0, heads, per, total);
   q8_shares<NK, HEADS, FULL, false>(a, smem, lds, w, h0, heads, per, total);
